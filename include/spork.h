@@ -20,6 +20,10 @@
  *     log-probability of every probe position and, per probe, the smallest
  *     top-1 probability over its tool-name span without the span's first
  *     token, compared with a threshold.
+ *   - spork_tables_step, spork_chunk_attn: a step whose lengths only the GPU
+ *     knows (the accept lengths of spork_verify_accept, for one): block tables
+ *     and slots by the block manager's rules, and the attention of prompt chunks
+ *     and single tokens over them, without a host plan.
  *   - spork_ngram_propose: the n-gram (prompt-lookup) draft proposer of the
  *     engine's n-gram speculative decoding (Sections 4.3 and 6.1), a second
  *     source of the drafts spork_verify_accept checks.
@@ -379,6 +383,130 @@ int spork_ngram_propose(const int32_t* tokens, const int64_t* seq_off, int32_t n
                         int64_t max_len, int32_t n_min, int32_t n_max, int32_t k,
                         int32_t* drafts, int32_t* n_drafts, void* workspace, size_t ws_bytes,
                         hipStream_t stream);
+
+/* ======================================================================== *
+ *  Steps whose lengths live on the GPU: block tables and slots built there,
+ *  and the attention of their new tokens, with nothing planned on the host.
+ *  Every call below can be captured in a HIP graph and replayed: lengths,
+ *  forks and tables may differ from replay to replay.
+ * ======================================================================== */
+
+/* Block tables in device memory, owned by the caller. Row s is a sequence
+ * (or a place for one); entries 0 .. held[s]-1 of its table row are its
+ * blocks in order. The rules are the block manager's (above). */
+typedef struct spork_tables {
+  int32_t num_blocks; /* blocks of the pools */
+  int32_t block_size; /* tokens per block */
+  int32_t n_seqs;     /* rows */
+  int32_t max_blocks; /* entries of a row */
+  int32_t* table;      /* device [n_seqs][max_blocks] */
+  int32_t* held;       /* device [n_seqs] */
+  int32_t* refcount;   /* device [num_blocks]: table entries that hold the block */
+  int32_t* free_queue; /* device [num_blocks]: a ring */
+  int32_t* queue;      /* device [2]: index of the ring's front, free blocks */
+} spork_tables;
+
+/* Empty tables: no row holds a block, every block is free, in free_order
+ * (device, num_blocks entries, a permutation of 0..num_blocks-1, which is not
+ * checked; NULL = 0,1,2,...) from the front. The table entries are not
+ * touched. One launch. */
+int spork_tables_init(const spork_tables* tables, const int32_t* free_order, hipStream_t stream);
+
+/* Workspace of spork_tables_step (any call with these num_blocks and n_seqs). */
+int spork_tables_workspace_bytes(const spork_tables* tables, size_t* bytes);
+
+/* The workspace's words must be zero when a step starts, and every step
+ * leaves them zero. Zero them once after allocating a workspace, and before
+ * it serves tables with another num_blocks. One launch, no memset. */
+int spork_tables_workspace_clear(const spork_tables* tables, void* workspace, size_t ws_bytes,
+                                 hipStream_t stream);
+
+/* One step of all rows: from the tokens each one had to those it now has.
+ * lens, n_new (device int32 [n_seqs]): tokens that stay, tokens that are
+ * appended. parents (device int32 [n_seqs], NULL = no forks): row s with
+ * parents[s] >= 0 becomes a fork of row parents[s] at its first lens[s]
+ * tokens (which the parent's blocks before the step must hold) and gives up
+ * what it held; a parent must not be forked in the same step. In this order,
+ * with b(x) = ceil(x / block_size):
+ *   1. forks: a forked row takes over the parent's first b(lens[s]) entries;
+ *      each of those blocks gains one reference;
+ *   2. releases, in row order and in a row in table order: entries behind a
+ *      row's first b(lens[s]) (a rollback, or an end with lens[s] = n_new[s]
+ *      = 0) and all old entries of a forked row; blocks that reach zero
+ *      references go to the back of the free queue;
+ *   3. appends, in row order: a row with n_new[s] > 0 that ends inside a
+ *      block which other rows also reference takes the queue's front as its
+ *      private copy (one copies entry); then one front per block that its
+ *      new tokens open.
+ * A row that neither changes nor appends has its own length in lens and 0 in
+ * n_new. Outputs (device):
+ *   slots[max_tokens] int64: the slot of every new token, in row order;
+ *     -1 behind the last one (spork_kv_write skips those). NULL if
+ *     max_tokens = 0;
+ *   positions[max_tokens] int32 (nullable): its position; -1 behind the last;
+ *   row_off[n_seqs+1] int32: offset of each row's new tokens, and their sum;
+ *   kv_len[n_seqs] int32: lens + n_new;
+ *   copies[n_seqs][3] int32: (src, dst, n_valid) of the first *n_copies
+ *     copies, in row order, the rest untouched, for spork_kv_copy_batch
+ *     before the new tokens are written;
+ *   status int32: SPORK_OK; SPORK_E_INVAL for a negative or unsound length,
+ *     fork, table entry of a touched row, or queue, SPORK_E_CAPACITY for a row
+ *     beyond max_blocks or more new tokens than max_tokens, SPORK_E_NOBLOCKS
+ *     when the queue is too short (the lowest code if several apply). Then
+ *     the tables are unchanged, row_off and kv_len are 0, slots and positions
+ *     -1 and *n_copies 0, so that the calls behind it on the stream do
+ *     nothing.
+ * The tables' own consistency (refcounts, queue contents) is not checked;
+ * a bad one never reads or writes outside the buffers.
+ * workspace (device, 256-byte aligned; words zero on entry, see above; steps
+ * that share it must not overlap). Four launches. Same inputs, same tables:
+ * no result depends on the order of atomics. */
+int spork_tables_step(const spork_tables* tables, const int32_t* lens, const int32_t* n_new,
+                      const int32_t* parents, int32_t max_tokens, int64_t* slots, int32_t* positions,
+                      int32_t* row_off, int32_t* kv_len, int32_t* copies, int32_t* n_copies,
+                      int32_t* status, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* The copies of a step: for each of the first *n_copies (device int32, at
+ * most max_copies) entries (src, dst, n_valid) of copies (device
+ * [max_copies][3]), slots 0..n_valid-1 of block src into block dst, every
+ * head, both pools. Entries with a block outside the pools, src = dst or
+ * n_valid outside 1..block_size are skipped. No dst may be another entry's
+ * src or dst. One launch. */
+int spork_kv_copy_batch(const spork_shape* shape, void* k_cache, void* v_cache, int32_t num_blocks,
+                        const int32_t* copies, const int32_t* n_copies, int32_t max_copies,
+                        hipStream_t stream);
+
+/* Workspace of spork_chunk_attn (any call with this head_dim). */
+int spork_chunk_workspace_bytes(const spork_shape* shape, int32_t n_seqs, int32_t n_rows, size_t* bytes);
+
+/* Attention of the new tokens of a ragged batch over the paged cache: prompt
+ * chunks of any length beside single tokens (head_dim 64 or 128, block_size
+ * 16 or 32, at most 256 query heads per KV head).
+ * q (device, n_rows rows of [Hq][D] dtype, q_stride elements apart, rows
+ * 16-byte aligned: the query part of a fused projection's rows will do);
+ * k_cache, v_cache (device pools of num_blocks blocks; the rows' own keys and
+ * values are written before the call); table (device int32
+ * [n_seqs][max_blocks]), row_off (device int32 [n_seqs+1]), kv_len (device
+ * int32 [n_seqs]): as spork_tables_step makes them. Sequence s owns query rows
+ * row_off[s] .. row_off[s+1]-1, the last of its kv_len[s] positions: row r of
+ * n attends to positions 0 .. kv_len[s] - n + r. A row with no position to
+ * attend to (kv_len[s] < n) gives zeros and an lse of -inf. A sequence without
+ * rows is not read.
+ * out (device [n_rows][Hq][D] dtype), lse (device [n_rows][Hq] float32, natural
+ * log, nullable). Rows that no sequence owns are left as they are.
+ * Keys and values of positions below kv_len must be finite (an infinity or NaN
+ * in one may show in rows that don't attend to it); whatever else the blocks
+ * hold is not seen. Offsets are clamped to n_rows, lengths to what max_blocks
+ * entries hold and table entries to the pools, so bad ones give wrong rows but
+ * no access out of bounds.
+ * workspace (device, 256-byte aligned, any contents; calls that share it must
+ * not overlap). Two launches: partial attention, then the log-sum-exp merge
+ * of what the split cut. The split follows from the lengths alone: same
+ * inputs, same bits. */
+int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, const void* k_cache,
+                     const void* v_cache, int32_t num_blocks, const int32_t* table, int32_t max_blocks,
+                     const int32_t* row_off, const int32_t* kv_len, int32_t n_seqs, int32_t n_rows,
+                     void* out, float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ======================================================================== *
  *  Kernel timing (benchmarks).

@@ -1,0 +1,744 @@
+// gfx950 attention of the new tokens of a ragged batch, prompt chunks and single
+// tokens alike, over the paged cache. Lengths, offsets and block tables are read
+// on the device; nothing of the work split comes from the host.
+//
+//   o_r = sum_{t <= p_r} softmax_t(scale q_r.k_t) v_t,  p_r = kv_len - rows + r
+//
+// Tiles. The query rows of a sequence times the G query heads of a KV head are
+// its packed rows; a tile is up to 256 of them (whole query rows), in row tiles
+// of 32, against the positions up to its last row's. A sequence of up to 256
+// packed rows is one tile per KV head: then there are row tiles for only some of
+// the workgroup's 8 waves, and the others take other tokens of the tile (8, 4 or
+// 2 ways), joined through LDS at its end.
+//
+// Slices. All tiles in a row, each as long as it costs (a start-up plus its
+// tokens), make a line that is cut into equal slices, one per compute unit. A
+// slice computes its place by itself, from a sum over the sequences' lengths, so
+// the split costs no launch and no atomics, and the same lengths are always cut
+// alike. A tile that a cut goes through has pieces in several slices; every
+// slice writes at most two pieces (its first tile's and its last's), so the
+// workspace does not grow with the batch. The merge launch joins them by
+// log-sum-exp. Neighbouring slices (the row tiles of one sequence and KV head,
+// which read the same keys and values) go to one die, whose L2 they share.
+//
+// Each wave streams its 32-token stages (fp32: 16) of K and V into a slot of its
+// own in LDS by direct loads (lane i of an instruction lands at its base + 16 i)
+// and reads them from there as operands; the loads of the next stage are in
+// flight while it computes, and no wave waits for another inside a tile.
+//   bf16  S^T = K Q^T and O^T += V^T P^T in 32x32x16 products. A-row r of the
+//         scores is token 16*(r/16) + 8*(r/4%2) + 4*(r/8%2) + r%4, so that a lane
+//         receives its query row's scores of tokens 16h + 8g + j (element 8h + j,
+//         g = lane / 32), which are its operand of the second product.
+//   fp32  16x16x4 products, two row tiles of 16 per wave; tokens 4g + i
+//         (g = lane / 16) likewise.
+// Softmax in base 2 with a lazily moved reference: it moves, and the accumulator
+// is rescaled, only where a lane's probabilities of a stage sum past 2^8.
+// Probabilities enter the second product in the input type (bf16: rounded to
+// nearest, 2^-9 of each; the row sum is of the unrounded ones); sums, reference
+// and accumulators are fp32.
+#include "chunk_kernels.h"
+#include "device_common.h"
+
+namespace spork {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+constexpr int kWaves = 8;
+constexpr int kDies = 8;
+constexpr float kSlack = 8.0f;    // base-2 headroom before the reference moves
+constexpr float kSlackSum = 256.0f;
+
+// The line's unit is half the time that a token takes where HBM bounds it.
+constexpr int kTileCost = 256;      // a tile's start-up
+constexpr int kMinSlice = 512;      // least length of a slice
+constexpr int kMinPiece = 64;       // tokens: a cut closer to a tile's end moves to it
+__device__ __forceinline__ int token_cost(int row_tiles) { return row_tiles <= 2 ? 2 : row_tiles <= 4 ? 3 : 4; }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (static_cast<int64_t>(uniform(static_cast<int>(x >> 32))) << 32) |
+         static_cast<uint32_t>(uniform(static_cast<int>(x)));
+}
+
+// A sequence's tiles and their cost on the line.
+struct Seq {
+  int row0, rows, kv;
+  int per;    // query rows of a tile
+  int tiles;  // per KV head
+  int cost;   // of a token
+  int64_t head_cost;
+  // positions that tile j sees
+  __device__ __forceinline__ int end(int j) const { return max(0, kv - rows + min(rows, (j + 1) * per)); }
+  // cost of the tiles before tile j
+  __device__ __forceinline__ int64_t before(int j) const {
+    const int64_t base = kv - rows;
+    const int whole = min(j, tiles - 1);  // tiles that end at a multiple of `per`
+    const int first = base >= 0 ? 0 : static_cast<int>(-base / per);  // the first of them that sees something
+    int64_t tokens = 0;
+    if (whole > first)
+      tokens = (whole - first) * base +
+               per * (static_cast<int64_t>(whole) * (whole + 1) / 2 - static_cast<int64_t>(first) * (first + 1) / 2);
+    if (j == tiles) tokens += max(0, kv);
+    return static_cast<int64_t>(j) * kTileCost + tokens * cost;
+  }
+};
+
+// Offsets and lengths are clamped to what the buffers hold.
+__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
+  Seq s;
+  const int group = a.hq / a.hkv;
+  s.row0 = min(max(a.row_off[i], 0), a.n_rows);
+  s.rows = max(0, min(max(a.row_off[i + 1], 0), a.n_rows) - s.row0);
+  s.kv = min(max(a.kv_len[i], 0), a.max_blocks * a.block_size);
+  s.per = kChunkTileRows / group;
+  s.tiles = (s.rows + s.per - 1) / s.per;
+  s.cost = token_cost((min(s.rows, s.per) * group + 31) / 32);
+  s.head_cost = s.tiles > 0 ? s.before(s.tiles) : 0;
+  return s;
+}
+
+// Token at which a cut at `y` of a tile's cost goes through its `end` tokens.
+__device__ __forceinline__ int cut(int64_t y, int64_t tile_cost, int cost, int end) {
+  if (y <= 0) return 0;
+  if (y >= tile_cost) return end;
+  const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) / cost) & ~31;
+  return t < kMinPiece ? 0 : t > end - kMinPiece ? end : t;
+}
+
+// --------------------------------------------------------------------------
+// The stage engines: a wave's loads, products and softmax.
+// --------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+
+// Where a stage's blocks lie: the table row, and the entries that exist.
+struct Pages {
+  const int32_t* table;
+  int last, num_blocks;
+  __device__ __forceinline__ int entry(int i) const {
+    return min(static_cast<uint32_t>(table[min(i, last)]), static_cast<uint32_t>(num_blocks - 1));
+  }
+};
+
+// Byte `off` of a block, 16 bytes per lane, to `dst` (+ 16 bytes per lane).
+__device__ __forceinline__ void load_lds(const char* block, uint32_t bytes, uint32_t off, void* dst) {
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(block), 0, bytes, 0x00027000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(dst), 16, off, 0, 0, 0);
+}
+
+template <typename T, int D, int BS>
+struct Engine;
+
+template <int D, int BS>
+struct Engine<__bf16, D, BS> {
+  static constexpr int kTokens = 32;                // of a stage
+  static constexpr int kUnits = 1;                  // rows of a lane
+  static constexpr int kChunksPerToken = D / 8;     // 16-byte chunks
+  static constexpr int kHalf = kTokens * D / 8;     // chunks of K, and of V
+  static constexpr int kLoads = kHalf / 64;         // instructions of K, and of V
+  static constexpr int kSteps = D / 16, kCt = D / 32;
+  bf16x8 q[kSteps];
+  f32x16 o[kCt];
+  float m[1], l[1];
+  int hz[1];  // last visible position of the lane's row
+
+  static __device__ __forceinline__ int row(int lane, int) { return lane & 31; }
+  static __device__ __forceinline__ int out_row(int lane, int) { return lane & 31; }
+  static __device__ __forceinline__ int out_unit(int) { return 0; }
+  static __device__ __forceinline__ int out_channel(int lane, int i) { return 32 * (i / 4) + 8 * (i % 4) + 4 * (lane >> 5); }
+  __device__ __forceinline__ f32x4 get(int i) const {
+    const f32x16& v = o[i / 4];
+    const int e = 4 * (i % 4);
+    return f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+  }
+  __device__ __forceinline__ void set(int i, f32x4 x) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[i / 4][4 * (i % 4) + k] = x[k];
+  }
+  __device__ __forceinline__ float row_sum(int) const { return l[0] + __shfl_xor(l[0], 32); }
+
+  // K: chunk t * kChunksPerToken + (c ^ swizzle(t)) holds channels 8c .. 8c + 7 of
+  // token t. V: chunk 2d + q of half h (16-token blocks) or 4d + (q ^ swizzle(d)),
+  // tokens 8q .. of channel d. The swizzles spread the lanes of an operand read
+  // over the banks.
+  static __device__ __forceinline__ int kswz(int t) {
+    return ((t & 7) | ((t >> 1) & 8)) & (kChunksPerToken - 1);
+  }
+  static __device__ __forceinline__ int vswz(int d) { return BS == 16 ? (d >> 3) & 1 : (d >> 3) & 3; }
+
+  __device__ __forceinline__ void load_q(const __bf16* p, int lane, int) {
+    const int g = lane >> 5;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 16 * s + 8 * g));
+  }
+  __device__ __forceinline__ void clear() {
+    m[0] = kNegInf;
+    l[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kCt; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
+  }
+
+  // Stage at token tb (a multiple of 32) into the wave's slot.
+  static __device__ __forceinline__ void issue(const ChunkArgs& a, const Pages& pg, int head, int tb, int lane, uint4* slot) {
+    constexpr uint32_t kBytes = BS * D * 2;
+    const size_t per_block = static_cast<size_t>(a.hkv) * kBytes, at = static_cast<size_t>(head) * kBytes;
+    constexpr int kBlocks = kTokens / BS;  // 2 or 1
+    const char *kb[kBlocks], *vb[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      const size_t e = static_cast<size_t>(uniform(pg.entry(tb / BS + b)));
+      kb[b] = static_cast<const char*>(a.k_cache) + e * per_block + at;
+      vb[b] = static_cast<const char*>(a.v_cache) + e * per_block + at;
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int chunk = 64 * k + lane, t = chunk / kChunksPerToken, c = chunk % kChunksPerToken;
+      load_lds(kb[64 * k / kChunksPerToken / BS], kBytes, 2u * ((t % BS) * D + 8 * (c ^ kswz(t))), slot + 64 * k);
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int chunk = 64 * k + lane;
+      int d, c;
+      if (BS == 16) {
+        d = (chunk % (kHalf / 2)) >> 1;
+        c = (chunk & 1) ^ vswz(d);
+      } else {
+        d = chunk >> 2;
+        c = (chunk & 3) ^ vswz(d);
+      }
+      load_lds(vb[BS == 16 ? 64 * k / (kHalf / 2) : 0], kBytes, 2u * (d * BS + 8 * c), slot + kHalf + 64 * k);
+    }
+  }
+
+  struct Ops {
+    uint4 k[kSteps], v[2 * kCt];
+  };
+  static __device__ __forceinline__ void read(const uint4* slot, int lane, Ops& x) {
+    const int r = lane & 31, g = lane >> 5;
+    const int t = 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) x.k[s] = slot[t * kChunksPerToken + ((2 * s + g) ^ kswz(t))];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int ct = 0; ct < kCt; ++ct) {
+        const int d = 32 * ct + r;
+        x.v[h * kCt + ct] = slot[kHalf + (BS == 16 ? h * (kHalf / 2) + 2 * d + (g ^ vswz(d)) : 4 * d + ((2 * h + g) ^ vswz(d)))];
+      }
+  }
+
+  // Zero the elements of an 8-token chunk from position `first` on that lie at or
+  // past `end`.
+  static __device__ __forceinline__ uint4 zero_past(uint4 v, int first, int end) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] &= (first + 2 * i < end ? 0x0000FFFFu : 0u) | (first + 2 * i + 1 < end ? 0xFFFF0000u : 0u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+
+  // Scores, softmax and P.V of the stage at tb; positions from `end` on are not
+  // there, `masked`: a row of the wave doesn't see all of the stage.
+  __device__ __forceinline__ void compute(Ops& x, int tb, int end, bool masked, float c, int lane, bool) {
+    const int g = lane >> 5;
+    f32x16 sc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x.k[s]), q[s], sc, 0, 0, 0);
+    float sv[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sv[e] = sc[e];
+    if (masked) {
+      const int hi = min(end - 1, hz[0]) - tb - 8 * g;  // the last visible one, from the lane's first
+      const float none = c < 0.0f ? -kNegInf : kNegInf;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sv[e] = 16 * (e >> 3) + (e & 7) > hi ? none : sv[e];
+    }
+    float ps = 0.0f;
+    uint32_t pw[8];
+    auto probs = [&](float ref) __attribute__((always_inline)) {
+      ps = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float p0 = exp2_fast(__builtin_fmaf(sv[e], c, -ref)), p1 = exp2_fast(__builtin_fmaf(sv[e + 1], c, -ref));
+        ps += p0 + p1;
+        pw[e / 2] = pack2(p0, p1);
+      }
+    };
+    probs(m[0]);
+    if (__builtin_expect(__ballot(!(ps <= kSlackSum)) != 0, 0)) {
+      float mx = sv[0] * c;
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sv[e] * c);
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      if (mx > m[0] + kSlack) {
+        const float alpha = exp2_fast(m[0] - mx);
+        l[0] *= alpha;
+#pragma unroll
+        for (int i = 0; i < kCt; ++i) o[i] *= alpha;
+        m[0] = mx;
+      }
+      probs(m[0] == kNegInf ? 0.0f : m[0]);
+    }
+    l[0] += ps;
+    if (tb + kTokens > end) {  // what lies behind the end may be anything: 0 * NaN
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) x.v[h * kCt + ct] = zero_past(x.v[h * kCt + ct], tb + 16 * h + 8 * g, end);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int ct = 0; ct < kCt; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(x.v[h * kCt + ct]), __builtin_bit_cast(bf16x8, u32x4{pw[4 * h], pw[4 * h + 1], pw[4 * h + 2], pw[4 * h + 3]}),
+            o[ct], 0, 0, 0);
+  }
+};
+
+template <int D, int BS>
+struct Engine<float, D, BS> {
+  static constexpr int kTokens = 16;
+  static constexpr int kUnits = 2;
+  static constexpr int kChunksPerToken = D / 4;
+  static constexpr int kHalf = kTokens * D / 4;
+  static constexpr int kLoads = kHalf / 64;
+  static constexpr int kDt = D / 16;
+  f32x4 q[2][kDt];  // channels 16j + 4g + i
+  f32x4 o[2][kDt];
+  float m[2], l[2];
+  int hz[2];
+
+  static __device__ __forceinline__ int row(int lane, int u) { return 16 * u + (lane & 15); }
+  static __device__ __forceinline__ int out_row(int lane, int i) { return 16 * (i / kDt) + (lane & 15); }
+  static __device__ __forceinline__ int out_unit(int i) { return i / kDt; }
+  static __device__ __forceinline__ int out_channel(int lane, int i) { return 16 * (i % kDt) + 4 * (lane >> 4); }
+  __device__ __forceinline__ f32x4 get(int i) const { return o[i / kDt][i % kDt]; }
+  __device__ __forceinline__ void set(int i, f32x4 x) { o[i / kDt][i % kDt] = x; }
+  __device__ __forceinline__ float row_sum(int u) const {
+    const float x = l[u] + __shfl_xor(l[u], 16);
+    return x + __shfl_xor(x, 32);
+  }
+  static __device__ __forceinline__ int kswz(int t) { return t & (kChunksPerToken - 1) & 15; }
+  static __device__ __forceinline__ int vswz(int d) { return (d >> 2) & 3; }
+
+  __device__ __forceinline__ void load_q(const float* p, int lane, int u) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < kDt; ++j) q[u][j] = *reinterpret_cast<const f32x4*>(p + 16 * j + 4 * g);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      m[u] = kNegInf;
+      l[u] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kDt; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  static __device__ __forceinline__ void issue(const ChunkArgs& a, const Pages& pg, int head, int tb, int lane, uint4* slot) {
+    constexpr uint32_t kBytes = BS * D * 4;
+    const size_t e = static_cast<size_t>(uniform(pg.entry(tb / BS))), hkv = static_cast<size_t>(a.hkv);
+    const char* kb = static_cast<const char*>(a.k_cache) + (e * hkv + head) * kBytes;
+    const char* vb = static_cast<const char*>(a.v_cache) + (e * hkv + head) * kBytes;
+    const int off = tb % BS;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int chunk = 64 * k + lane, t = chunk / kChunksPerToken, c = chunk % kChunksPerToken;
+      load_lds(kb, kBytes, 4u * ((off + t) * D + 4 * (c ^ kswz(t))), slot + 64 * k);
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int chunk = 64 * k + lane, d = chunk >> 2, c = (chunk & 3) ^ vswz(d);
+      load_lds(vb, kBytes, 4u * (d * BS + off + 4 * c), slot + kHalf + 64 * k);
+    }
+  }
+
+  struct Ops {
+    f32x4 k[kDt], v[kDt];
+  };
+  static __device__ __forceinline__ void read(const uint4* slot, int lane, Ops& x) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < kDt; ++j) x.k[j] = __builtin_bit_cast(f32x4, slot[r * kChunksPerToken + ((4 * j + g) ^ kswz(r))]);
+#pragma unroll
+    for (int j = 0; j < kDt; ++j) {
+      const int d = 16 * j + r;
+      x.v[j] = __builtin_bit_cast(f32x4, slot[kHalf + 4 * d + (g ^ vswz(d))]);
+    }
+  }
+
+  __device__ __forceinline__ void compute(Ops& x, int tb, int end, bool masked, float c, int lane, bool second) {
+    const int g = lane >> 4;
+    if (tb + kTokens > end) {
+#pragma unroll
+      for (int j = 0; j < kDt; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (tb + 4 * g + i >= end) x.v[j][i] = 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (u == 1 && !second) break;
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kDt; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[j][i], q[u][j][i], sc, 0, 0, 0);
+      float sv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sv[i] = sc[i] * c;
+        if (masked && tb + 4 * g + i > min(end - 1, hz[u])) sv[i] = kNegInf;
+      }
+      float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
+      if (__ballot(mx > m[u] + kSlack) != 0) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (mx > m[u]) {
+          const float alpha = exp2_fast(m[u] - mx);
+          l[u] *= alpha;
+#pragma unroll
+          for (int j = 0; j < kDt; ++j) o[u][j] *= alpha;
+          m[u] = mx;
+        }
+      }
+      const float ref = m[u] == kNegInf ? 0.0f : m[u];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sv[i] = exp2_fast(sv[i] - ref);
+        l[u] += sv[i];
+      }
+#pragma unroll
+      for (int j = 0; j < kDt; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[j][i], sv[i], o[u][j], 0, 0, 0);
+    }
+  }
+};
+
+// Two channel runs of a row, normalised, in the output type.
+__device__ __forceinline__ void store_out(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
+__device__ __forceinline__ void store_out(__bf16* p, f32x4 x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+}
+
+// Index of a slice's piece: 0 of a tile that began before it, 1 of one that goes on behind it.
+__device__ __forceinline__ size_t piece_row(int slice, int which) {
+  return (static_cast<size_t>(slice) * 2 + which) * kChunkTileRows;
+}
+
+template <typename T, int D, int BS>
+__global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
+  using E = Engine<T, D, BS>;
+  constexpr int NT = 64 * kWaves, kFloat4s = D / 8;
+  __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];
+  __shared__ float ml[kWaves][2][64 * E::kUnits];
+  __shared__ int64_t wave_sum[kWaves];
+  __shared__ int64_t start[2];
+  static_assert(2 * E::kHalf >= kFloat4s * 64, "a wave's slot holds its accumulator");
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int group = a.hq / a.hkv;
+
+  // ---- the slice: its place on the line ----
+  const int per_die = kChunkSlices / kDies;
+  const int slice = static_cast<int>(blockIdx.x) % kDies * per_die + static_cast<int>(blockIdx.x) / kDies;
+  if (tid == 0) {
+    a.splits[slice].n_rows = 0;
+    a.continues[slice] = 0;
+  }
+  const int per_thread = (a.n_seqs + NT - 1) / NT;
+  const int i0 = min(tid * per_thread, a.n_seqs), i1 = min(i0 + per_thread, a.n_seqs);
+  int64_t sum = 0;
+  for (int i = i0; i < i1; ++i) sum += seq_of(a, i).head_cost;
+  int64_t upto = sum;
+#pragma unroll
+  for (int by = 1; by < 64; by *= 2) {
+    const int64_t y = __shfl_up(upto, by);
+    if (lane >= by) upto += y;
+  }
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += wave_sum[w];
+    total += wave_sum[w];
+  }
+  // (a sequence's KV heads lie side by side: the line is hkv times the sum)
+  total = uniform(total) * a.hkv;
+  const int64_t want = total / kMinSlice;
+  const int n_slices = static_cast<int>(want < 1 ? 1 : want < kChunkSlices ? want : kChunkSlices);
+  if (slice >= n_slices || total == 0) return;
+  int64_t pos = total * slice / n_slices;
+  const int64_t stop = total * (slice + 1) / n_slices;
+  {
+    int64_t at = (upto - sum) * a.hkv;
+    if (pos >= at && pos < upto * a.hkv) {
+      for (int i = i0; i < i1; ++i) {
+        const int64_t c = seq_of(a, i).head_cost * a.hkv;
+        if (pos < at + c) {
+          start[0] = i;
+          start[1] = pos - at;
+          break;
+        }
+        at += c;
+      }
+    }
+  }
+  __syncthreads();
+  int seq = uniform(static_cast<int>(start[0]));
+  const int64_t in_seq = uniform(start[1]);
+  Seq sq = seq_of(a, seq);
+  int head = static_cast<int>(in_seq / sq.head_cost);
+  int64_t y0 = in_seq % sq.head_cost;
+  int tile = 0;
+  for (int hi = sq.tiles; hi - tile > 1;) {  // the last tile that begins at or before y0
+    const int mid = (tile + hi) >> 1;
+    if (sq.before(mid) <= y0) tile = mid;
+    else hi = mid;
+  }
+  y0 -= sq.before(tile);
+
+  for (;;) {
+    // ---- one tile, or the slice's piece of it ----
+    const int end = sq.end(tile);
+    const int64_t tile_cost = kTileCost + static_cast<int64_t>(end) * sq.cost;
+    const int64_t y1 = min(tile_cost, y0 + stop - pos);
+    const int tok_lo = cut(y0, tile_cost, sq.cost, end), tok_hi = cut(y1, tile_cost, sq.cost, end);
+    if (tok_hi > tok_lo || (end == 0 && y0 == 0)) {
+      const int r0 = tile * sq.per;  // first query row of the tile, in the sequence
+      const int n_packed = min(sq.per, sq.rows - r0) * group;
+      const int row_tiles = (n_packed + 31) / 32, ways = max(1, kWaves / row_tiles);
+      const int rt = wave % row_tiles, way = wave / row_tiles;
+      const bool works = way < ways;
+      E e;
+      e.clear();
+      const Pages pg{a.table + static_cast<size_t>(seq) * a.max_blocks, max(0, (sq.kv + BS - 1) / BS - 1), a.num_blocks};
+      const int first = tok_lo + way * E::kTokens, stride = ways * E::kTokens;
+      if (works && first < tok_hi) E::issue(a, pg, head, first, lane, smem[wave]);
+      int least = INT_MAX;
+      const bool second = E::kUnits == 1 || n_packed - 32 * rt > 16;
+#pragma unroll
+      for (int u = 0; u < E::kUnits; ++u) {
+        const int p = 32 * rt + E::row(lane, u), pp = p < n_packed ? p : 0;
+        const int row = r0 + pp / group;
+        // rows that are none see everything: they never hold up a stage
+        e.hz[u] = p < n_packed ? sq.kv - sq.rows + row : INT_MAX;
+        least = min(least, e.hz[u]);
+        e.load_q(static_cast<const T*>(a.q) + static_cast<int64_t>(sq.row0 + row) * a.q_stride +
+                     (head * group + pp % group) * D, lane, u);
+      }
+      least = uniform(wave_min_int(least));
+      const float c = a.scale_log2;
+      if (works) {
+        for (int tb = first; tb < tok_hi; tb += stride) {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          typename E::Ops x;
+          E::read(smem[wave], lane, x);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the slot is written again
+          if (tb + stride < tok_hi) E::issue(a, pg, head, tb + stride, lane, smem[wave]);
+          e.compute(x, tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second);
+        }
+      }
+      if (ways > 1) {  // join the ways: the first takes the others' results
+        if (works && way > 0) {
+#pragma unroll
+          for (int u = 0; u < E::kUnits; ++u) {
+            ml[wave][0][64 * u + lane] = e.m[u];
+            ml[wave][1][64 * u + lane] = e.l[u];
+          }
+#pragma unroll
+          for (int i = 0; i < kFloat4s; ++i) reinterpret_cast<f32x4*>(smem[wave])[64 * i + lane] = e.get(i);
+        }
+        __syncthreads();
+        if (works && way == 0) {
+          for (int v = 1; v < ways; ++v) {
+            const int other = v * row_tiles + rt;
+            float mine[E::kUnits], theirs[E::kUnits];
+#pragma unroll
+            for (int u = 0; u < E::kUnits; ++u) {
+              const float om = ml[other][0][64 * u + lane], top = fmaxf(e.m[u], om), ref = top == kNegInf ? 0.0f : top;
+              mine[u] = exp2_fast(e.m[u] - ref);
+              theirs[u] = exp2_fast(om - ref);
+              e.l[u] = e.l[u] * mine[u] + ml[other][1][64 * u + lane] * theirs[u];
+              e.m[u] = top;
+            }
+#pragma unroll
+            for (int i = 0; i < kFloat4s; ++i) {
+              const int u = E::out_unit(i);
+              e.set(i, e.get(i) * mine[u] + reinterpret_cast<const f32x4*>(smem[other])[64 * i + lane] * theirs[u]);
+            }
+          }
+        }
+        __syncthreads();  // the slots are read
+      }
+      // ---- its outputs, or its piece for the merge ----
+      const bool whole = tok_lo == 0 && tok_hi == end;
+      const int which = tok_lo == 0 ? 1 : 0;
+      if (works && way == 0) {
+        float sum_u[E::kUnits];
+#pragma unroll
+        for (int u = 0; u < E::kUnits; ++u) sum_u[u] = e.row_sum(u);
+        if (whole) {
+#pragma unroll
+          for (int u = 0; u < E::kUnits; ++u) {
+            const int p = 32 * rt + E::row(lane, u);
+            if (a.lse != nullptr && p < n_packed && lane < 32 / E::kUnits) {
+              a.lse[static_cast<size_t>(sq.row0 + r0 + p / group) * a.hq + head * group + p % group] =
+                  sum_u[u] > 0.0f ? (e.m[u] + __builtin_amdgcn_logf(sum_u[u])) * kLn2 : kNegInf;
+            }
+            sum_u[u] = sum_u[u] > 0.0f ? 1.0f / sum_u[u] : 0.0f;
+          }
+#pragma unroll
+          for (int i = 0; i < kFloat4s; ++i) {
+            const int p = 32 * rt + E::out_row(lane, i);
+            if (p < n_packed)
+              store_out(static_cast<T*>(a.out) +
+                            (static_cast<size_t>(sq.row0 + r0 + p / group) * a.hq + head * group + p % group) * D +
+                            E::out_channel(lane, i),
+                        e.get(i) * sum_u[E::out_unit(i)]);
+          }
+        } else {
+          const size_t base = piece_row(slice, which) + 32 * rt;
+#pragma unroll
+          for (int u = 0; u < E::kUnits; ++u) {
+            if (lane < 32 / E::kUnits) {
+              a.part_ml[2 * (base + E::row(lane, u))] = e.m[u];
+              a.part_ml[2 * (base + E::row(lane, u)) + 1] = sum_u[u];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kFloat4s; ++i)
+            *reinterpret_cast<f32x4*>(a.part_o + (base + E::out_row(lane, i)) * D + E::out_channel(lane, i)) = e.get(i);
+        }
+      }
+      if (!whole && tid == 0) {
+        if (tok_lo > 0) {
+          a.continues[slice] = 1;
+        } else {
+          // the slice that holds the tile's last token: of the line's cuts, the
+          // first at or behind which the tile's cut is its end
+          const int64_t tile_pos = pos - y0;
+          int last = slice + 1;
+          while (last + 1 < n_slices &&
+                 cut(total * (last + 1) / n_slices - tile_pos, tile_cost, sq.cost, end) < end)
+            ++last;
+          a.splits[slice] = ChunkSplit{sq.row0 + r0, head, n_packed, last};
+        }
+      }
+    }
+    // ---- the next tile of the line ----
+    pos += y1 - y0;
+    y0 = 0;
+    if (pos >= stop) break;
+    if (++tile == sq.tiles) {
+      tile = 0;
+      if (++head == a.hkv) {
+        head = 0;
+        // the next sequence with rows, 64 at a time
+        int found = -1;
+        for (int i = seq + 1; found < 0; i += 64) {
+          const bool has = i + lane < a.n_seqs && seq_of(a, i + lane).tiles > 0;
+          const uint64_t bal = __ballot(has);
+          if (bal != 0) found = i + __builtin_ctzll(bal);
+          else if (i + 64 >= a.n_seqs) break;  // not reached: the line ends with the last tile
+        }
+        if (found < 0) break;
+        seq = uniform(found);
+        sq = seq_of(a, seq);
+      }
+    }
+  }
+}
+
+// Log-sum-exp merge of a split tile: a workgroup per (slice that begins one, 32
+// packed rows), a wave per row and 8 rows in turn, D / 64 channels a lane.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {
+  constexpr int PER = D / 64;
+  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.hq / a.hkv;
+  const ChunkSplit s = a.splits[slice];
+  const int row_end = min(s.n_rows, 32 * (static_cast<int>(blockIdx.y) + 1));
+  for (int p = 32 * blockIdx.y + (threadIdx.x >> 6); p < row_end; p += 4) {
+    float m = kNegInf, l = 0.0f, o[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) o[k] = 0.0f;
+    for (int v = slice; v <= s.last; ++v) {
+      if (v > slice && a.continues[v] == 0) continue;
+      const size_t row = piece_row(v, v == slice ? 1 : 0) + p;
+      const float pm = a.part_ml[2 * row], pl = a.part_ml[2 * row + 1], top = fmaxf(m, pm), ref = top == kNegInf ? 0.0f : top;
+      const float mine = exp2_fast(m - ref), theirs = exp2_fast(pm - ref);
+#pragma unroll
+      for (int k = 0; k < PER; ++k) o[k] = o[k] * mine + a.part_o[row * D + PER * lane + k] * theirs;
+      l = l * mine + pl * theirs;
+      m = top;
+    }
+    const size_t out = static_cast<size_t>(s.row0 + p / group) * a.hq + s.head * group + p % group;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) static_cast<T*>(a.out)[out * D + PER * lane + k] = static_cast<T>(o[k] * inv);
+    if (a.lse != nullptr && lane == 0) a.lse[out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+  }
+}
+
+using ChunkKernel = void (*)(ChunkArgs);
+
+template <typename T>
+ChunkKernel pick_attn(int d, int bs) {
+  if (bs != 16 && bs != 32) return nullptr;
+  if (d == 64) return bs == 16 ? chunk_attn_kernel<T, 64, 16> : chunk_attn_kernel<T, 64, 32>;
+  if (d == 128) return bs == 16 ? chunk_attn_kernel<T, 128, 16> : chunk_attn_kernel<T, 128, 32>;
+  return nullptr;
+}
+
+template <typename T>
+ChunkKernel pick_merge(int d) {
+  return d == 64 ? chunk_merge_kernel<T, 64> : d == 128 ? chunk_merge_kernel<T, 128> : nullptr;
+}
+
+}  // namespace
+
+bool chunk_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
+  return (dtype == 0 || dtype == 1) && (head_dim == 64 || head_dim == 128) && (block_size == 16 || block_size == 32);
+}
+
+static constexpr size_t kNotes = kChunkSlices * (sizeof(ChunkSplit) + sizeof(int32_t));
+static constexpr size_t kPieceRows = static_cast<size_t>(kChunkSlices) * 2 * kChunkTileRows;
+
+size_t chunk_workspace_bytes(int32_t head_dim) {
+  return kNotes + kPieceRows * (2 + static_cast<size_t>(head_dim)) * sizeof(float);
+}
+
+void chunk_workspace(ChunkArgs* a, void* workspace) {
+  a->splits = static_cast<ChunkSplit*>(workspace);
+  a->continues = reinterpret_cast<int32_t*>(a->splits + kChunkSlices);
+  a->part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + kNotes);
+  a->part_o = a->part_ml + 2 * kPieceRows;
+}
+
+hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t stream) {
+  const ChunkKernel k = a.dtype == 1 ? pick_attn<__bf16>(a.head_dim, a.block_size) : pick_attn<float>(a.head_dim, a.block_size);
+  if (k == nullptr) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k, dim3(kChunkSlices), dim3(64 * kWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
+  const ChunkKernel k = a.dtype == 1 ? pick_merge<__bf16>(a.head_dim) : pick_merge<float>(a.head_dim);
+  if (k == nullptr) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k, dim3(kChunkSlices, kChunkTileRows / 32), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace spork

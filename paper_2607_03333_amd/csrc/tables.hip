@@ -1,0 +1,455 @@
+// gfx950 kernels that keep block tables on the GPU: one step takes every row
+// from the tokens it had to the tokens it now has (rollback, fork, append) and
+// gives each new token its slot, from lengths that only the device knows.
+//
+// The rules are the host block manager's (block_manager.h), run over a batch:
+// with b(x) = ceil(x / block_size),
+//   forks     row s of parent p becomes the first b(len s) entries of row p;
+//   releases  in row and table order, the entries of a row behind its first
+//             b(len s), and all old entries of a forked row; a block without
+//             references goes to the back of the free queue;
+//   appends   in row order: a row that appends inside a block which others hold
+//             takes a copy target from the queue's front, then every block that
+//             it opens takes the next front.
+// Done in that order by one thread this is a chain of queue operations; what
+// makes it parallel is that only three things depend on the order, and each has
+// a closed form: a freed block is put into the queue by the last place that
+// releases it, its rank there is a prefix sum; of k rows that append inside a
+// block of r references all copy it, except that the last one writes in place
+// where k = r; and the fronts that a row takes start at a prefix sum. Counts
+// and last places go through atomics whose order does not matter (sums, maxima),
+// so the same step gives the same tables every time.
+//
+// Four launches: count (references and last places), decide (what each row frees
+// and takes, their sums, and whether the step fits), release (frees into the
+// queue, forked rows, copies), assign (fronts into the tables, slots). The
+// references are changed while they are counted, and changed back where decide
+// refuses the step.
+#include "device_common.h"
+#include "spork.h"
+#include "tables_kernels.h"
+
+namespace spork {
+namespace {
+
+constexpr int kRowThreads = 256;      // of a row's workgroup in count, release and assign
+constexpr int kDecideThreads = 1024;  // a wave per row
+constexpr int kDecideRows = kDecideThreads / 64;
+
+struct Row {
+  int len, grow, parent, held;
+  int keep;        // blocks of the tokens that stay
+  int from;        // row that those blocks stand in
+  int release_lo;  // first entry of the old row that is released
+};
+
+__device__ __forceinline__ int blocks_of(int64_t tokens, int bs) { return static_cast<int>((tokens + bs - 1) / bs); }
+
+// Row s as the step asks for it, and the status of that: its fields are used
+// only where it is SPORK_OK, and then every index that follows from them is in
+// range, entries of the tables apart.
+__device__ __forceinline__ int read_row(const TablesArgs& a, int s, Row* r) {
+  r->len = a.lens[s];
+  r->grow = a.n_new[s];
+  r->held = a.held[s];
+  r->parent = a.parents != nullptr ? a.parents[s] : -1;
+  if (r->len < 0 || r->grow < 0 || r->held < 0 || r->held > a.max_blocks || r->parent >= a.n_seqs) return SPORK_E_INVAL;
+  if (r->parent < 0) r->parent = -1;
+  int have = r->held;
+  if (r->parent >= 0) {
+    if (r->parent == s || a.parents[r->parent] >= 0) return SPORK_E_INVAL;
+    have = a.held[r->parent];
+    if (have < 0 || have > a.max_blocks) return SPORK_E_INVAL;
+  }
+  const int64_t end = static_cast<int64_t>(r->len) + r->grow;
+  if (blocks_of(r->len, a.block_size) > have) return SPORK_E_INVAL;
+  if (end > static_cast<int64_t>(a.max_blocks) * a.block_size) return SPORK_E_CAPACITY;
+  r->keep = blocks_of(r->len, a.block_size);
+  r->from = r->parent >= 0 ? r->parent : s;
+  r->release_lo = r->parent >= 0 ? 0 : r->keep;
+  return SPORK_OK;
+}
+
+__device__ __forceinline__ bool in_pool(const TablesArgs& a, int block) { return block >= 0 && block < a.num_blocks; }
+
+__device__ __forceinline__ size_t place(const TablesArgs& a, int s, int col) {
+  return static_cast<size_t>(s) * a.max_blocks + col;
+}
+
+// Block that row s appends into behind tokens that stay, or -1.
+__device__ __forceinline__ int shared_tail(const TablesArgs& a, const Row& r) {
+  if (r.grow == 0 || r.len % a.block_size == 0) return -1;
+  return a.table[place(a, r.from, r.len / a.block_size)];
+}
+
+__global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
+  const int s = blockIdx.x, tid = threadIdx.x;
+  Row r;
+  int err = read_row(a, s, &r);
+  if (err == SPORK_OK) {
+    if (r.parent >= 0) {
+      for (int j = tid; j < r.keep; j += kRowThreads) {
+        const int b = a.table[place(a, r.parent, j)];
+        if (in_pool(a, b)) atomicAdd(a.refcount + b, 1);
+        else err = SPORK_E_INVAL;
+      }
+    }
+    for (int j = r.release_lo + tid; j < r.held; j += kRowThreads) {
+      const int b = a.table[place(a, s, j)];
+      if (in_pool(a, b)) {
+        atomicAdd(a.refcount + b, -1);
+        atomicMax(a.last_release + b, static_cast<int>(place(a, s, j)) + 1);
+      } else {
+        err = SPORK_E_INVAL;
+      }
+    }
+    if (tid == 0) {
+      const int b = shared_tail(a, r);
+      if (b != -1 || (r.grow != 0 && r.len % a.block_size != 0)) {
+        if (in_pool(a, b)) {
+          atomicAdd(a.sharers + b, 1);
+          atomicMax(a.last_sharer + b, s + 1);
+        } else {
+          err = SPORK_E_INVAL;
+        }
+      }
+    }
+  }
+  if (err != SPORK_OK) atomicMin(&a.totals->error, err);
+}
+
+__device__ __forceinline__ int agent_load(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void agent_store(int32_t* p, int x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Inclusive sum over the workgroup's threads of four numbers at once.
+struct Sums {
+  int64_t tokens;
+  int frees, takes, copies;
+};
+__device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) {
+  return {x.tokens + y.tokens, x.frees + y.frees, x.takes + y.takes, x.copies + y.copies};
+}
+__device__ __forceinline__ Sums shifted(const Sums& x, int by) {
+  return {__shfl_up(x.tokens, by), __shfl_up(x.frees, by), __shfl_up(x.takes, by), __shfl_up(x.copies, by)};
+}
+__device__ __forceinline__ Sums block_scan(Sums x, Sums* wave_sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int by = 1; by < 64; by *= 2) {
+    const Sums y = shifted(x, by);
+    if (lane >= by) x = x + y;
+  }
+  __syncthreads();
+  if (lane == 63) wave_sums[wave] = x;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) x = x + wave_sums[w];
+  return x;
+}
+
+__global__ void __launch_bounds__(kDecideThreads) tables_decide(TablesArgs a) {
+  __shared__ Sums wave_sums[kDecideRows];
+  __shared__ Sums done;
+  __shared__ int last;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int s = blockIdx.x * kDecideRows + (tid >> 6);
+  if (s < a.n_seqs) {
+    Row r;
+    int frees = 0, takes = 0, copies = 0;
+    if (read_row(a, s, &r) == SPORK_OK) {
+      for (int j0 = r.release_lo; j0 < r.held; j0 += 64) {
+        const int j = j0 + lane;
+        bool free_here = false;
+        if (j < r.held) {
+          const int b = a.table[place(a, s, j)];
+          free_here = in_pool(a, b) && a.last_release[b] == static_cast<int>(place(a, s, j)) + 1 && a.refcount[b] == 0;
+        }
+        frees += __popcll(__ballot(free_here));
+      }
+      const int b = shared_tail(a, r);
+      if (b >= 0 && b < a.num_blocks) {
+        const int refs = a.refcount[b];
+        copies = refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
+      }
+      takes = copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
+    }
+    if (lane == 0) {
+      agent_store(a.frees + s, frees);
+      agent_store(a.takes + s, takes);
+      agent_store(a.copy_off + s, copies);
+    }
+  }
+  // The last workgroup to get here has every row's numbers to sum.
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) last = atomicAdd(&a.totals->arrived, 1) == static_cast<int>(gridDim.x) - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  if (tid == 0) done = Sums{0, 0, 0, 0};
+  __syncthreads();
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kDecideThreads) {
+    const int i = s0 + tid;
+    Sums x{0, 0, 0, 0};
+    if (i < a.n_seqs) x = {max(a.n_new[i], 0), agent_load(a.frees + i), agent_load(a.takes + i), agent_load(a.copy_off + i)};
+    const Sums base = done, upto = base + block_scan(x, wave_sums);
+    if (i < a.n_seqs) {
+      a.frees[i] = upto.frees - x.frees;
+      a.takes[i] = upto.takes - x.takes;
+      a.copy_off[i] = x.copies ? upto.copies - 1 : -1 - upto.copies;
+      a.row_off[i + 1] = static_cast<int>(min(upto.tokens, static_cast<int64_t>(INT_MAX)));
+    }
+    __syncthreads();
+    if (tid == kDecideThreads - 1) done = upto;
+    __syncthreads();
+  }
+  if (tid != 0) return;
+  const int front = a.queue[0], count = a.queue[1];
+  int status = agent_load(&a.totals->error);
+  if (front < 0 || front >= a.num_blocks || count < 0 || count > a.num_blocks - done.frees) status = min(status, SPORK_E_INVAL);
+  if (done.tokens > a.max_tokens) status = min(status, SPORK_E_CAPACITY);
+  if (status == SPORK_OK && done.takes > count + done.frees) status = SPORK_E_NOBLOCKS;
+  TablesTotals* t = a.totals;
+  t->status = status;
+  t->front = front;
+  t->count = count;
+  t->error = 0;
+  t->arrived = 0;
+  *a.status = status;
+  *a.n_copies = status == SPORK_OK ? done.copies : 0;
+  a.row_off[0] = 0;
+  if (status == SPORK_OK) {
+    a.queue[0] = static_cast<int>((static_cast<int64_t>(front) + done.takes) % a.num_blocks);
+    a.queue[1] = count + done.frees - done.takes;
+  }
+}
+
+__device__ __forceinline__ int ring(const TablesArgs& a, int front, int64_t nth) {
+  return static_cast<int>((front + nth) % a.num_blocks);
+}
+
+__global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
+  __shared__ int freed[kRowThreads / 64];
+  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const TablesTotals t = *a.totals;
+  Row r;
+  if (read_row(a, s, &r) != SPORK_OK) return;
+  if (t.status != SPORK_OK) {  // as it was: references back, words clear
+    if (r.parent >= 0) {
+      for (int j = tid; j < r.keep; j += kRowThreads) {
+        const int b = a.table[place(a, r.parent, j)];
+        if (in_pool(a, b)) atomicAdd(a.refcount + b, -1);
+      }
+    }
+    for (int j = r.release_lo + tid; j < r.held; j += kRowThreads) {
+      const int b = a.table[place(a, s, j)];
+      if (!in_pool(a, b)) continue;
+      atomicAdd(a.refcount + b, 1);
+      a.last_release[b] = 0;
+    }
+    if (tid == 0) {
+      const int b = shared_tail(a, r);
+      if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
+    }
+    return;
+  }
+  int at = a.frees[s];  // of the row's freed blocks among all
+  for (int j0 = r.release_lo; j0 < r.held; j0 += kRowThreads) {
+    const int j = j0 + tid;
+    int b = 0;
+    bool free_here = false;
+    if (j < r.held) {
+      b = a.table[place(a, s, j)];
+      // The last place alone clears the word: any other compares unequal before and after.
+      if (a.last_release[b] == static_cast<int>(place(a, s, j)) + 1) {
+        free_here = a.refcount[b] == 0;
+        a.last_release[b] = 0;
+      }
+    }
+    const uint64_t bal = __ballot(free_here);
+    __syncthreads();
+    if (lane == 0) freed[wave] = __popcll(bal);
+    __syncthreads();
+    int rank = at + __popcll(bal & ((uint64_t{1} << lane) - 1));
+    for (int w = 0; w < kRowThreads / 64; ++w) {
+      if (w < wave) rank += freed[w];
+      at += freed[w];
+    }
+    if (free_here) a.free_queue[ring(a, t.front, static_cast<int64_t>(t.count) + rank)] = b;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    const int b = shared_tail(a, r), c = a.copy_off[s];
+    if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
+    if (c >= 0) {
+      a.copies[3 * c] = b;
+      a.copies[3 * c + 2] = r.len % a.block_size;
+    }
+  }
+  if (r.parent >= 0)
+    for (int j = tid; j < r.keep; j += kRowThreads) a.table[place(a, s, j)] = a.table[place(a, r.parent, j)];
+}
+
+__global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
+  const int tid = threadIdx.x, bs = a.block_size;
+  const TablesTotals t = *a.totals;
+  if (static_cast<int>(blockIdx.x) < a.n_seqs) {  // a row: its table and references
+    const int s = blockIdx.x;
+    if (t.status != SPORK_OK) {
+      if (tid == 0) {
+        a.row_off[s + 1] = 0;
+        a.kv_len[s] = 0;
+      }
+      return;
+    }
+    const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
+    const int c = a.copy_off[s];
+    int64_t first = a.takes[s];
+    if (c >= 0) {
+      if (tid == 0) {
+        const int dst = a.free_queue[ring(a, t.front, first)];
+        atomicAdd(a.refcount + a.copies[3 * c], -1);
+        a.copies[3 * c + 1] = dst;
+        a.refcount[dst] = 1;
+        a.table[place(a, s, len / bs)] = dst;
+      }
+      ++first;
+    }
+    for (int j = keep + tid; j < to; j += kRowThreads) {
+      const int b = a.free_queue[ring(a, t.front, first + j - keep)];
+      a.table[place(a, s, j)] = b;
+      a.refcount[b] = 1;
+    }
+    if (tid == 0) {
+      a.held[s] = to;
+      a.kv_len[s] = end;
+    }
+    return;
+  }
+  // a token: its row by search in the offsets, its block from the queue or, in
+  // front of the row's first new block, from the tail or its copy
+  const int i = (static_cast<int>(blockIdx.x) - a.n_seqs) * kRowThreads + tid;
+  if (i >= a.max_tokens) return;
+  int64_t slot = -1;
+  int pos = -1;
+  if (t.status == SPORK_OK && i < a.row_off[a.n_seqs]) {
+    int lo = 0, hi = a.n_seqs - 1;  // the last row that starts at or before token i
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.row_off[mid] <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    const int s = lo, len = a.lens[s], keep = blocks_of(len, bs), c = a.copy_off[s];
+    pos = len + i - a.row_off[s];
+    const int col = pos / bs;
+    const int64_t first = a.takes[s] + (c >= 0 ? 1 : 0);
+    int b;
+    if (col >= keep) b = a.free_queue[ring(a, t.front, first + col - keep)];
+    else if (c >= 0) b = a.free_queue[ring(a, t.front, first - 1)];
+    else b = a.table[place(a, s, col)];
+    slot = static_cast<int64_t>(b) * bs + pos % bs;
+  }
+  a.slots[i] = slot;
+  if (a.positions != nullptr) a.positions[i] = pos;
+}
+
+__global__ void __launch_bounds__(256) tables_init_kernel(TablesArgs a, const int32_t* free_order) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < a.num_blocks) {
+    a.free_queue[i] = free_order != nullptr ? free_order[i] : i;
+    a.refcount[i] = 0;
+  }
+  if (i < a.n_seqs) a.held[i] = 0;
+  if (i == 0) {
+    a.queue[0] = 0;
+    a.queue[1] = a.num_blocks;
+  }
+}
+
+__global__ void __launch_bounds__(256) words_clear_kernel(int32_t* words, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256)
+    words[i] = 0;
+}
+
+// The copies of copy-on-write, from the list that a step wrote: a workgroup per
+// (copy, KV head), 16 bytes a thread. K: the first n_valid tokens are one run of
+// bytes. V: by element, the first n_valid of each channel's run of block_size.
+__global__ void __launch_bounds__(256) kv_copy_batch_kernel(int elem, int hkv, int D, int BS, int num_blocks, char* kc,
+                                                            char* vc, const int32_t* copies, const int32_t* n_copies,
+                                                            int max_copies) {
+  const int c = blockIdx.x / hkv, h = blockIdx.x % hkv;
+  if (c >= min(*n_copies, max_copies)) return;
+  const int src = copies[3 * c], dst = copies[3 * c + 1], nv = copies[3 * c + 2];
+  if (src < 0 || src >= num_blocks || dst < 0 || dst >= num_blocks || src == dst || nv <= 0 || nv > BS) return;
+  const size_t bytes = static_cast<size_t>(D) * BS * elem;
+  const size_t from = (static_cast<size_t>(src) * hkv + h) * bytes, to = (static_cast<size_t>(dst) * hkv + h) * bytes;
+  const uint4* ks = reinterpret_cast<const uint4*>(kc + from);
+  uint4* kd = reinterpret_cast<uint4*>(kc + to);
+  for (int i = threadIdx.x; i < nv * D * elem / 16; i += 256) kd[i] = ks[i];
+  const int run = BS * elem;
+  for (int i = threadIdx.x; i < D * run / elem; i += 256) {
+    const int t = i % BS;
+    if (t >= nv) continue;
+    if (elem == 2) reinterpret_cast<uint16_t*>(vc + to)[i] = reinterpret_cast<const uint16_t*>(vc + from)[i];
+    else reinterpret_cast<uint32_t*>(vc + to)[i] = reinterpret_cast<const uint32_t*>(vc + from)[i];
+  }
+}
+
+}  // namespace
+
+size_t tables_control_bytes(int32_t num_blocks) {
+  return sizeof(TablesTotals) + (3 * sizeof(int32_t) * static_cast<size_t>(num_blocks) + 255) / 256 * 256;
+}
+
+size_t tables_workspace_bytes(int32_t num_blocks, int32_t n_seqs) {
+  return tables_control_bytes(num_blocks) + 3 * sizeof(int32_t) * static_cast<size_t>(n_seqs);
+}
+
+void tables_workspace(TablesArgs* a, void* workspace) {
+  a->totals = static_cast<TablesTotals*>(workspace);
+  a->last_release = reinterpret_cast<int32_t*>(a->totals + 1);
+  a->sharers = a->last_release + a->num_blocks;
+  a->last_sharer = a->sharers + a->num_blocks;
+  a->frees = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + tables_control_bytes(a->num_blocks));
+  a->takes = a->frees + a->n_seqs;
+  a->copy_off = a->takes + a->n_seqs;
+}
+
+hipError_t launch_tables_init(const TablesArgs& a, const int32_t* free_order, hipStream_t stream) {
+  const int n = a.num_blocks > a.n_seqs ? a.num_blocks : a.n_seqs;
+  hipLaunchKernelGGL(tables_init_kernel, dim3((static_cast<unsigned>(n) + 255) / 256), dim3(256), 0, stream, a, free_order);
+  return hipGetLastError();
+}
+
+hipError_t launch_words_clear(int32_t* words, int64_t n, hipStream_t stream) {
+  if (n <= 0) return hipSuccess;
+  const int64_t blocks = (n + 255) / 256;
+  hipLaunchKernelGGL(words_clear_kernel, dim3(static_cast<unsigned>(blocks < 1024 ? blocks : 1024)), dim3(256), 0, stream, words,
+                     n);
+  return hipGetLastError();
+}
+
+hipError_t launch_tables_step(const TablesArgs& a, hipStream_t stream) {
+  const unsigned rows = static_cast<unsigned>(a.n_seqs);
+  hipLaunchKernelGGL(tables_count, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  hipLaunchKernelGGL(tables_decide, dim3((rows + kDecideRows - 1) / kDecideRows), dim3(kDecideThreads), 0, stream, a);
+  hipLaunchKernelGGL(tables_release, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  const unsigned tokens = (static_cast<unsigned>(a.max_tokens) + kRowThreads - 1) / kRowThreads;
+  hipLaunchKernelGGL(tables_assign, dim3(rows + tokens), dim3(kRowThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_copy_batch(int32_t elem_bytes, int32_t hkv, int32_t head_dim, int32_t block_size, int32_t num_blocks,
+                                void* k_cache, void* v_cache, const int32_t* copies, const int32_t* n_copies,
+                                int32_t max_copies, hipStream_t stream) {
+  if (max_copies <= 0) return hipSuccess;
+  hipLaunchKernelGGL(kv_copy_batch_kernel, dim3(static_cast<unsigned>(max_copies) * static_cast<unsigned>(hkv)), dim3(256), 0,
+                     stream, elem_bytes, hkv, head_dim, block_size, num_blocks, static_cast<char*>(k_cache),
+                     static_cast<char*>(v_cache), copies, n_copies, max_copies);
+  return hipGetLastError();
+}
+
+}  // namespace spork

@@ -67,6 +67,11 @@ class spork_plan_info(ctypes.Structure):
                 ("attn_wide", _c_i32), ("control_bytes", ctypes.c_size_t)]
 
 
+class spork_tables(ctypes.Structure):
+    _fields_ = [("num_blocks", _c_i32), ("block_size", _c_i32), ("n_seqs", _c_i32), ("max_blocks", _c_i32),
+                ("table", _p), ("held", _p), ("refcount", _p), ("free_queue", _p), ("queue", _p)]
+
+
 # name -> (restype, argtypes); every name is declared in include/spork.h
 _SIGNATURES = {
     "spork_last_error": (ctypes.c_char_p, []),
@@ -107,6 +112,16 @@ _SIGNATURES = {
     "spork_ngram_workspace_bytes": (ctypes.c_int, [_c_i32, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
     "spork_ngram_propose": (ctypes.c_int, [_p, _p, _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _p, _p, _p,
                                            ctypes.c_size_t, _p]),
+    "spork_tables_init": (ctypes.c_int, [ctypes.POINTER(spork_tables), _p, _p]),
+    "spork_tables_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(spork_tables), ctypes.POINTER(ctypes.c_size_t)]),
+    "spork_tables_workspace_clear": (ctypes.c_int, [ctypes.POINTER(spork_tables), _p, ctypes.c_size_t, _p]),
+    "spork_tables_step": (ctypes.c_int, [ctypes.POINTER(spork_tables), _p, _p, _p, _c_i32, _p, _p, _p, _p, _p, _p,
+                                         _p, _p, ctypes.c_size_t, _p]),
+    "spork_kv_copy_batch": (ctypes.c_int, [ctypes.POINTER(spork_shape), _p, _p, _c_i32, _p, _p, _c_i32, _p]),
+    "spork_chunk_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(spork_shape), _c_i32, _c_i32,
+                                                   ctypes.POINTER(ctypes.c_size_t)]),
+    "spork_chunk_attn": (ctypes.c_int, [ctypes.POINTER(spork_shape), _p, _c_i64, _p, _p, _c_i32, _p, _c_i32, _p, _p,
+                                        _c_i32, _c_i32, _p, _p, _p, ctypes.c_size_t, _p]),
     "spork_read_ceiling": (ctypes.c_int, [_p, _c_i64, _c_i32, _c_i32, _p, _p]),
     "spork_timing_enable": (ctypes.c_int, [_c_i32]),
     "spork_timing_read": (ctypes.c_int, [_p, _p]),
@@ -125,6 +140,9 @@ def lib():
                                "`python -m paper_2607_03333_amd.build` (there is no fallback)")
         handle = ctypes.CDLL(path)
         for name, (res, args) in _SIGNATURES.items():
+            # the sanitizer build holds only the host sources that it was given
+            if _HOST_SANITIZER_LIB and not hasattr(handle, name):
+                continue
             fn = getattr(handle, name)
             fn.restype = res
             fn.argtypes = args
@@ -361,6 +379,104 @@ def spork_ngram_propose(tokens, seq_off, n_seqs, max_len, n_min, n_max, k, draft
     _check(lib().spork_ngram_propose(_ptr(tokens), _ptr(seq_off), n_seqs, max_len, n_min, n_max, k,
                                      _ptr(drafts), _ptr(n_drafts), _ptr(workspace), ws_bytes,
                                      _stream(stream)))
+
+
+# ---- steps whose lengths live on the GPU --------------------------------------
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _want(name, x, size, *shape):
+    """Device pointer of an integer tensor that the library reads or writes whole, `size` bytes an element (None
+    passes: the library says what may be NULL)."""
+    if x is None:
+        return None
+    if x.shape != shape or x.element_size() != size or x.is_floating_point() or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {8 * size}-bit integers of shape {list(shape)}, "
+                         f"not {x.dtype} {list(x.shape)}")
+    return x.data_ptr()
+
+
+def _on_gpu(*tensors):
+    for x in tensors:
+        if x is not None and not x.is_cuda:
+            raise ValueError("tensor arguments must be in GPU memory")
+
+
+def make_tables(block_size, table, held, refcount, free_queue, queue):
+    """A spork_tables over the given int32 tensors, which it keeps alive: table [n_seqs, max_blocks], held [n_seqs],
+    refcount [num_blocks], free_queue [num_blocks], queue [2]."""
+    n_seqs, max_blocks = table.shape
+    num_blocks = refcount.shape[0]
+    t = spork_tables(num_blocks, block_size, n_seqs, max_blocks, _want("table", table, 4, n_seqs, max_blocks),
+                     _want("held", held, 4, n_seqs), _want("refcount", refcount, 4, num_blocks),
+                     _want("free_queue", free_queue, 4, num_blocks), _want("queue", queue, 4, 2))
+    t.tensors = (table, held, refcount, free_queue, queue)
+    return t
+
+
+def spork_tables_init(tables, free_order=None, stream=None):
+    _check(lib().spork_tables_init(ctypes.byref(tables), _want("free_order", free_order, 4, tables.num_blocks),
+                                   _stream(stream)))
+
+
+def spork_tables_workspace_bytes(tables):
+    b = ctypes.c_size_t()
+    _check(lib().spork_tables_workspace_bytes(ctypes.byref(tables), ctypes.byref(b)))
+    return b.value
+
+
+def spork_tables_workspace_clear(tables, workspace, stream=None):
+    _check(lib().spork_tables_workspace_clear(ctypes.byref(tables), _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def spork_tables_step(tables, lens, n_new, parents, slots, positions, row_off, kv_len, copies, n_copies, status,
+                      workspace, stream=None):
+    """max_tokens is the length of slots."""
+    n, most = tables.n_seqs, 0 if slots is None else slots.shape[0]
+    args = (_want("lens", lens, 4, n), _want("n_new", n_new, 4, n), _want("parents", parents, 4, n), most,
+            _want("slots", slots, 8, most), _want("positions", positions, 4, most), _want("row_off", row_off, 4, n + 1),
+            _want("kv_len", kv_len, 4, n), _want("copies", copies, 4, n, 3), _want("n_copies", n_copies, 4, 1),
+            _want("status", status, 4, 1), _ptr(workspace), _bytes(workspace))
+    _on_gpu(tables.tensors[0], lens, n_new, parents, slots, positions, row_off, kv_len, copies, n_copies, status, workspace)
+    _check(lib().spork_tables_step(ctypes.byref(tables), *args, _stream(stream)))
+
+
+def spork_kv_copy_batch(shape, k_cache, v_cache, num_blocks, copies, n_copies, stream=None):
+    most = copies.shape[0]
+    _on_gpu(k_cache, v_cache, copies, n_copies)
+    _check(lib().spork_kv_copy_batch(ctypes.byref(shape), _ptr(k_cache), _ptr(v_cache), num_blocks,
+                                     _want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1),
+                                     most, _stream(stream)))
+
+
+def spork_chunk_workspace_bytes(shape, n_seqs, n_rows):
+    b = ctypes.c_size_t()
+    _check(lib().spork_chunk_workspace_bytes(ctypes.byref(shape), n_seqs, n_rows, ctypes.byref(b)))
+    return b.value
+
+
+def spork_chunk_attn(shape, q, k_cache, v_cache, table, row_off, kv_len, out, lse, workspace, stream=None):
+    """q [rows, hq, head_dim] may have any stride between its rows; num_blocks is the pools' first size."""
+    (n_rows, hq, d), (n_seqs, max_blocks), blocks = q.shape, table.shape, k_cache.shape[0]
+    if (hq, d) != (shape.hq, shape.head_dim):
+        raise ValueError("q must be [rows, hq, head_dim] of the shape")
+    if n_rows > 0 and (q.stride(2) != 1 or q.stride(1) != d):
+        raise ValueError("the rows of q must be contiguous")
+    if tuple(out.shape) != (n_rows, hq, d) or (lse is not None and tuple(lse.shape) != (n_rows, hq)):
+        raise ValueError("out must be [rows, hq, head_dim] and lse [rows, hq]")
+    elem = {SPORK_DTYPE_F32: 4, SPORK_DTYPE_BF16: 2}.get(shape.dtype)  # bf16 may come as 16-bit integers
+    if any(x.element_size() != elem for x in (q, k_cache, v_cache, out)) or (lse is not None and lse.element_size() != 4):
+        raise ValueError("q, the pools and out must be of the shape's dtype and lse float32")
+    bs = shape.block_size
+    if tuple(k_cache.shape) != (blocks, shape.hkv, bs, d) or tuple(v_cache.shape) != (blocks, shape.hkv, d, bs):
+        raise ValueError("the pools must be [blocks, hkv, block_size, head_dim] and [blocks, hkv, head_dim, block_size]")
+    stride = q.stride(0) if n_rows > 1 else max(hq * d, q.stride(0))
+    args = (q.data_ptr(), stride, _ptr(k_cache), _ptr(v_cache), blocks, _want("table", table, 4, n_seqs, max_blocks),
+            max_blocks, _want("row_off", row_off, 4, n_seqs + 1), _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows,
+            _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace))
+    _on_gpu(q, k_cache, v_cache, table, row_off, kv_len, out, lse, workspace)
+    _check(lib().spork_chunk_attn(ctypes.byref(shape), *args, _stream(stream)))
 
 
 # ---- measurement aid --------------------------------------------------------

@@ -1,0 +1,253 @@
+"""Attention of the new tokens of a ragged batch over the paged cache
+(spork_chunk_attn) against the definition in float64: prompt chunks and single
+tokens, head groupings, block sizes, lengths around every tile and stage edge,
+empty rows, what lies in unwritten slots, strides, streams, graphs."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_cases import say
+from paged_cases import attention, bounds, paged_pools
+from paper_2607_03333_amd import spork
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+SPORK = {BF16: spork.SPORK_DTYPE_BF16, F32: spork.SPORK_DTYPE_F32}
+
+
+class Case:
+    def __init__(self, dtype, hq, hkv, d, bs, new, kv, seed=0, gain=1.0, scale=None, spare_rows=3, gap=0, junk=float("nan")):
+        rng = np.random.default_rng(seed * 977 + hq + d + bs + sum(kv) % 1009)
+        self.dtype, self.new, self.kv = dtype, list(new), list(kv)
+        self.scale = float(np.float32(1.0 / math.sqrt(d) if scale is None else scale))
+        self.shape = spork.make_shape(hq, hkv, d, bs, SPORK[dtype], self.scale)
+        self.k, self.v, self.table, self.contexts = paged_pools(rng, dtype, hkv, d, bs, kv, junk=junk)
+        rows = sum(new)
+        wide = torch.from_numpy(rng.standard_normal((rows + spare_rows, hq * d + gap)).astype(np.float32) * gain).to(dtype).cuda()
+        self.q = wide[:, :hq * d].unflatten(1, (hq, d))
+        self.rows = rows
+        self.row_off = torch.tensor(np.cumsum([0] + list(new)), dtype=torch.int32, device="cuda")
+        self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device="cuda")
+        self.out = torch.full((rows + spare_rows, hq, d), 7.5, dtype=dtype, device="cuda")
+        self.lse = torch.full((rows + spare_rows, hq), 7.5, dtype=F32, device="cuda")
+        self.ws = torch.full((spork.spork_chunk_workspace_bytes(self.shape, len(new), rows + spare_rows) // 4,), float("nan"),
+                             dtype=F32, device="cuda")
+
+    def run(self, lse=True):
+        spork.spork_chunk_attn(self.shape, self.q, self.k, self.v, self.table, self.row_off, self.kv_len, self.out,
+                               self.lse if lse else None, self.ws)
+
+    def run_and_check(self, tag):
+        self.run()
+        self.check(tag)
+
+    def reference(self):
+        return attention(self.q[:self.rows].cpu(), self.contexts, self.new, self.scale)
+
+    def check(self, tag="", ref=None):
+        torch.cuda.synchronize()
+        out, lse, size, mass = ref or self.reference()
+        o_tol, l_tol = bounds(self.dtype, out, lse, size, mass, self.scale, max(self.kv + [1]), out.shape[2])
+        got, got_lse = self.out[:self.rows].double().cpu(), self.lse[:self.rows].double().cpu()
+        assert torch.isfinite(got).all(), f"{tag}: not finite"
+        off = (got - out).abs()
+        assert (off <= o_tol).all(), f"{tag}: out off by {(off / o_tol).max().item():.2f} of its bound"
+        empty = lse.isinf()
+        assert torch.equal(got_lse.isinf(), empty) and (got_lse[empty] < 0).all(), f"{tag}: empty rows"
+        assert (got[empty] == 0).all()
+        l_off = torch.where(empty, torch.zeros_like(lse), got_lse - lse).abs()
+        assert (l_off <= l_tol).all(), f"{tag}: lse off by {(l_off / l_tol).max().item():.2f} of its bound"
+        assert (self.out[self.rows:] == 7.5).all() and (self.lse[self.rows:] == 7.5).all(), f"{tag}: rows of no sequence"
+        share = (off / o_tol).max().item() if off.numel() else 0.0
+        say(f"  chunk {tag}: out at {share:.2f}, lse at {(l_off / l_tol).max().item() if off.numel() else 0:.2f} of the bound")
+
+
+EDGES = [1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 63, 64, 65, 95, 96, 97, 127, 128, 129, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("bs", (16, 32))
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF16, 4, 1, 128), (BF16, 2, 2, 64), (F32, 2, 1, 64), (F32, 3, 3, 128)])
+def test_single_tokens_around_every_edge(dtype, hq, hkv, d, bs):
+    Case(dtype, hq, hkv, d, bs, [1] * len(EDGES), EDGES).run_and_check("single tokens")
+
+
+@pytest.mark.parametrize("bs", (16, 32))
+@pytest.mark.parametrize("dtype,hq,hkv,d", [(BF16, 8, 1, 128), (BF16, 3, 3, 64), (F32, 4, 2, 64), (F32, 2, 2, 128)])
+def test_whole_prompts_around_every_edge(dtype, hq, hkv, d, bs):
+    Case(dtype, hq, hkv, d, bs, EDGES, EDGES, gap=8 * hkv).run_and_check("whole prompts")
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,bs,new,kv", [
+    (BF16, 8, 2, 128, 16, [5, 0, 64, 1, 0, 33, 2], [900, 77, 64, 1, 0, 500, 31]),
+    (BF16, 7, 1, 128, 32, [40, 1, 300], [41, 1000, 700]),
+    (BF16, 28, 4, 128, 16, [37, 73], [500, 73]),
+    (BF16, 16, 1, 64, 16, [16, 17, 100], [300, 17, 101]),
+    (BF16, 5, 5, 64, 32, [260, 513], [1000, 513]),
+    (BF16, 256, 1, 64, 16, [3, 1], [50, 400]),
+    (BF16, 200, 2, 128, 32, [4], [200]),
+    (F32, 8, 2, 128, 16, [5, 0, 64, 1, 33], [300, 77, 64, 1, 200]),
+    (F32, 7, 1, 64, 32, [40, 1, 90], [41, 700, 300]),
+    (F32, 256, 1, 64, 16, [2, 1], [40, 100]),
+])
+def test_mixed_batches(dtype, hq, hkv, d, bs, new, kv):
+    Case(dtype, hq, hkv, d, bs, new, kv, gap=16).run_and_check("mixed")
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("new,kv", [([20, 3], [5, 0]), ([300], [40]), ([1], [0]), ([64, 64], [63, 0]), ([700], [1])])
+def test_rows_with_nothing_to_see(dtype, new, kv):
+    """More rows than positions: the first rows lie before the sequence's start."""
+    c = Case(dtype, 4, 2, 64, 16, new, kv)
+    c.run()
+    torch.cuda.synchronize()
+    o, l = [], []
+    row = 0
+    for (k, v), n in zip(c.contexts, new):
+        hidden = max(0, n - k.shape[0])
+        part = attention(c.q[row + hidden:row + n].cpu(), [(k, v)], [n - hidden], c.scale)
+        o.append([torch.cat([torch.zeros(hidden, *x.shape[1:], dtype=x.dtype), x]) for x in part])
+        o[-1][1][:hidden] = -math.inf
+        row += n
+    c.check("empty rows", ref=[torch.cat(x) for x in zip(*o)])
+
+
+@pytest.mark.parametrize("new,kv,hq,hkv", [
+    ([1, 1], [30011, 70000], 8, 1),          # few rows, a long axis: every slice has a piece
+    ([1], [66001], 4, 4),
+    ([700], [9000], 8, 1),                   # tiles that a cut goes through
+    ([1] * 40 + [257], [40 * i + 1 for i in range(40)] + [3001], 4, 1),
+])
+def test_tiles_split_over_slices(new, kv, hq, hkv):
+    c = Case(BF16, hq, hkv, 128, 16, new, kv, gain=3.0)
+    c.run_and_check("split")
+    first = (c.out.clone(), c.lse.clone())
+    c.ws.fill_(float("inf"))
+    c.out.fill_(7.5)
+    c.lse.fill_(7.5)
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(first[0], c.out) and torch.equal(first[1], c.lse)
+
+
+def test_many_sequences():
+    """More sequences than threads of a workgroup, most without rows."""
+    n = 1500
+    new = [1 if i % 7 == 0 else 3 if i % 211 == 5 else 0 for i in range(n)]
+    new[:300] = [0] * 300
+    new[-64:] = [0] * 64
+    kv = [(i * 13) % 90 + x for i, x in enumerate(new)]
+    Case(BF16, 4, 2, 64, 16, new, kv).run_and_check("many")
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("scale,gain", [(0.0, 1.0), (-0.2, 1.0), (0.125, 30.0), (3.0, 4.0), (1e-30, 1.0)])
+def test_softmax_scales(dtype, scale, gain):
+    Case(dtype, 4, 2, 64, 16, [70, 1], [200, 90], scale=scale, gain=gain).run_and_check(f"scale {scale}")
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf"), torch.finfo(torch.bfloat16).min])
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_unwritten_slots_may_hold_anything(dtype, junk):
+    Case(dtype, 4, 1, 128, 32, [33, 1, 7], [70, 45, 7], junk=junk).run_and_check(f"junk {junk}")
+
+
+def test_entries_out_of_range_are_clamped():
+    """Bad tables, offsets and lengths: no access out of bounds, and the sound sequences' rows are right."""
+    c = Case(BF16, 4, 1, 128, 16, [5, 5, 5], [100, 100, 100])
+    ref = c.reference()
+    c.table[1] = torch.tensor([1 << 30, -5, 2 ** 31 - 1, -2 ** 31, 1 << 20, 9999, -1], dtype=torch.int32)
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    c.out.fill_(7.5)
+    c.kv_len[1] = 1 << 30
+    c.row_off[3] = 1 << 30  # the last sequence takes the spare rows too
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.out[:5], want[:5])
+    o_tol, _ = bounds(BF16, *ref, c.scale, 100, 128)
+    assert ((want[:5].double().cpu() - ref[0][:5]).abs() <= o_tol[:5]).all()
+    c.kv_len[:] = -3
+    c.row_off[:] = torch.tensor([9, -4, 1 << 30, -1 << 31], dtype=torch.int32)
+    c.run()
+    torch.cuda.synchronize()
+
+
+def test_no_lse_no_rows_no_sequences():
+    c = Case(BF16, 4, 1, 128, 16, [9, 40], [50, 40])
+    c.run()
+    torch.cuda.synchronize()
+    want = c.out.clone()
+    c.out.fill_(7.5)
+    c.lse.fill_(7.5)
+    c.run(lse=False)
+    torch.cuda.synchronize()
+    assert torch.equal(c.out, want) and (c.lse == 7.5).all()
+    c.out.fill_(7.5)
+    c.row_off.zero_()
+    c.run()
+    torch.cuda.synchronize()
+    assert (c.out == 7.5).all()
+    spork.spork_chunk_attn(c.shape, c.q[:0], c.k, c.v, c.table, c.row_off, c.kv_len, c.out[:0], c.lse[:0], None)
+    spork.spork_chunk_attn(c.shape, c.q, c.k, c.v, c.table[:0], c.row_off[:1], c.kv_len[:0], c.out, c.lse, None)
+    torch.cuda.synchronize()
+    assert (c.out == 7.5).all()
+
+
+def test_another_stream():
+    c = Case(BF16, 4, 1, 128, 16, [90, 1], [300, 500])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        c.run()
+    s.synchronize()
+    c.check("stream")
+
+
+def test_captured_calls_follow_the_lengths():
+    """One graph; lengths, offsets and tables change between replays, and eager calls run in between."""
+    cases = [Case(BF16, 8, 2, 128, 16, new, kv, seed=i, spare_rows=128 - sum(new)) for i, (new, kv) in enumerate(
+        [([1, 1, 1], [400, 90, 3]), ([100, 1, 0], [130, 500, 64]), ([0, 60, 17], [5, 60, 480]), ([0, 0, 0], [1, 2, 3])])]
+    most = max(c.table.shape[1] for c in cases)
+    blocks = max(c.k.shape[0] for c in cases)
+    live = cases[0]
+    hold = dict(q=torch.empty_like(live.q), k=live.k.new_zeros(blocks, *live.k.shape[1:]), v=live.v.new_zeros(blocks, *live.v.shape[1:]),
+                table=torch.zeros(3, most, dtype=torch.int32, device="cuda"), row_off=live.row_off.clone(), kv_len=live.kv_len.clone())
+    out, lse, ws = live.out.clone(), live.lse.clone(), live.ws.clone()
+
+    def fill(c):
+        for name in ("q", "row_off", "kv_len"):
+            hold[name].copy_(getattr(c, name))
+        hold["k"][:c.k.shape[0]] = c.k
+        hold["v"][:c.v.shape[0]] = c.v
+        hold["table"][:, :c.table.shape[1]] = c.table
+        out.fill_(7.5)
+        lse.fill_(7.5)
+
+    def run():
+        spork.spork_chunk_attn(live.shape, hold["q"], hold["k"], hold["v"], hold["table"], hold["row_off"], hold["kv_len"], out, lse,
+                               ws)
+
+    fill(cases[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for r, c in enumerate(cases + cases[:2]):
+        fill(c)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        c.out.copy_(out)
+        c.lse.copy_(lse)
+        c.check(f"replay {r}")
+        c.run()  # eager, on its own buffers
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
