@@ -427,6 +427,403 @@ struct Engine<float, D, BS> {
   }
 };
 
+// --------------------------------------------------------------------------
+// The wide path: bf16 tiles of more than 128 packed rows, head_dim 128. Each
+// wave owns one row tile of 32 and all of them share every 32-token stage (16
+// KB), which goes through a ring of eight in LDS; a barrier publishes two
+// stages at a time and frees the two that were read. The matrix cores bound a
+// stage (16 32x32x16 products per wave, 512 cycles, two waves to a SIMD), so
+// beside the softmax of stage s run the P.V products of stage s - 1 and the
+// scores of stage s + 1, one product and a few vector instructions at a time;
+// operand reads are spread over the slots likewise. The reads and barriers are
+// outside the compiler's view (it would wait for the loads of later stages at
+// every read), with waits that name the registers; no read is in flight where a
+// loop goes round.
+// --------------------------------------------------------------------------
+constexpr int kStageChunks = 1024;   // 32 tokens x (K + V) x 128 channels x 2 bytes / 16
+constexpr int kRing = 8, kPer = 2;   // stages; stages that a barrier publishes
+constexpr int kAhead = kRing - kPer;
+constexpr int kTabEntries = 6912;    // of a segment: what LDS has left beside the ring
+constexpr int kStageLoads = 2;       // of a wave: the lower four load K, the upper four V
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)(const_cast<void*>(p))));
+}
+template <int OFF = 0>
+__device__ __forceinline__ u32x4 lds_read_b128(uint32_t addr) {
+  static_assert(OFF >= 0 && OFF < 65536, "ds offset field");
+  u32x4 r;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(OFF) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ds_read_b32 %0, %1" : "=v"(r) : "v"(addr) : "memory");
+  return r;
+}
+__device__ __forceinline__ void lds_wait(uint32_t& r) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(r) : : "memory"); }
+__device__ __forceinline__ void lds_wait(u32x4& r, int keep) {
+  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(r) : "i"(keep) : "memory");
+}
+__device__ __forceinline__ void lds_wait(u32x4 (&r)[8]) {
+  asm volatile("s_waitcnt lgkmcnt(0)"
+               : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]), "+v"(r[4]), "+v"(r[5]), "+v"(r[6]), "+v"(r[7])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+// Until at most `after` (0..5) stages of this wave's loads are in flight.
+__device__ __forceinline__ void wait_stage(int after) {
+  switch (after) {
+    case 5: wait_vmcnt<5 * kStageLoads>(); break;
+    case 4: wait_vmcnt<4 * kStageLoads>(); break;
+    case 3: wait_vmcnt<3 * kStageLoads>(); break;
+    case 2: wait_vmcnt<2 * kStageLoads>(); break;
+    case 1: wait_vmcnt<kStageLoads>(); break;
+    default: wait_vmcnt<0>(); break;
+  }
+}
+
+// A tile, or the piece of it that a slice works on.
+struct Tile {
+  int row0, hz0;        // query row of the first packed row, and its last visible position
+  int n_packed, head;
+  int tok_lo, tok_hi;
+};
+
+// A wave's loads of the shared stages: instruction k of wave w fills chunks
+// (2w + k) * 64 + lane of a stage, from one block, at a scalar base plus the
+// lane's fixed offset.
+template <int BS>
+struct RingLoader {
+  using E = Engine<__bf16, 128, BS>;
+  const char* pool;
+  size_t head, hkv;
+  uint32_t off[kStageLoads];
+  uint32_t tab_base;  // LDS address of stage 0's table entry
+  int wave, last;
+  __device__ __forceinline__ void init(const ChunkArgs& a, int kv_head, int nstage, int wave_, int lane, const int* tab) {
+    wave = wave_;
+    last = nstage - 1;
+    head = static_cast<size_t>(kv_head);
+    hkv = static_cast<size_t>(a.hkv);
+    pool = static_cast<const char*>(wave < 4 ? a.k_cache : a.v_cache);
+    tab_base = lds_addr(tab) + (BS == 16 && (wave & 2) != 0 ? 4u : 0u);
+#pragma unroll
+    for (int k = 0; k < kStageLoads; ++k) {
+      const int chunk = (kStageLoads * wave + k) * 64 + lane;
+      if (wave < 4) {
+        const int t = chunk >> 4;
+        off[k] = 2u * ((t % BS) * 128 + 8 * ((chunk & 15) ^ E::kswz(t)));
+      } else if (BS == 16) {
+        const int d = (chunk & 255) >> 1;
+        off[k] = 2u * (d * BS + 8 * ((chunk & 1) ^ E::vswz(d)));
+      } else {
+        const int d = (chunk - 512) >> 2;
+        off[k] = 2u * (d * BS + 8 * ((chunk & 3) ^ E::vswz(d)));
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t entry(int st) const {  // without a wait
+    return lds_read_b32(tab_base + (128u / BS) * static_cast<uint32_t>(min(st, last)));
+  }
+  __device__ __forceinline__ const char* base(uint32_t ent) const {
+    return pool + (static_cast<size_t>(uniform(static_cast<int>(ent))) * hkv + head) * (static_cast<size_t>(BS) * 256);
+  }
+  __device__ __forceinline__ void load(const char* src, uint4* slot, int k) const {
+    load_lds(src, BS * 256, off[k], slot + (kStageLoads * wave + k) * 64);
+  }
+};
+
+// Every wave of the workgroup runs this for the same tile; on return e holds the
+// wave's row tile (nothing where wave * 32 >= n_packed), and its rows' loads are
+// done.
+template <int BS>
+__device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[kStageChunks],
+                                          int* tab, int tid, int wave, Engine<__bf16, 128, BS>& e) {
+  constexpr int kSegment = kTabEntries * BS - 4 * 32;  // tokens
+  const int lane = tid & 63, r32 = lane & 31, g = lane >> 5;
+  const bool owns = wave * 32 < w.n_packed;
+  const int hmin = uniform(wave_min_int(e.hz[0]));
+  const float c = a.scale_log2, masked = c < 0.0f ? -kNegInf : kNegInf;
+  float& m = e.m[0];
+  float& l = e.l[0];
+  auto& o = e.o;
+  // Per-lane LDS addresses of the operands in ring slot 0 (see Engine).
+  const uint32_t smem_base = lds_addr(&smem[0][0]);
+  uint32_t kaddr[4], vaddr[2];
+  {
+    const int t = 16 * (r32 >> 4) + 8 * ((r32 >> 2) & 1) + 4 * ((r32 >> 3) & 1) + (r32 & 3);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      kaddr[s] = smem_base + 16u * (t * 16 + ((2 * s + g) ^ Engine<__bf16, 128, BS>::kswz(t)));
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      vaddr[h] = smem_base + 16u * (BS == 16 ? 512 + 256 * h + 2 * r32 + (g ^ Engine<__bf16, 128, BS>::vswz(r32))
+                                             : 512 + 4 * r32 + ((2 * h + g) ^ Engine<__bf16, 128, BS>::vswz(r32)));
+  }
+  auto slot_off = [&](int st) __attribute__((always_inline)) {
+    return static_cast<uint32_t>(st % kRing) * (kStageChunks * 16);
+  };
+  auto read_k = [&](u32x4 (&kr)[8], int s, uint32_t soff) __attribute__((always_inline)) {
+    kr[s] = lds_read_b128(s < 4 ? kaddr[s] + soff : (kaddr[s - 4] + soff) ^ 128u);
+  };
+  auto read_v = [&](u32x4 (&vr)[8], int i, uint32_t soff) __attribute__((always_inline)) {  // vr[4h + ct]
+    constexpr int kCt = BS == 16 ? 1024 : 2048;  // bytes between channel tiles; 16-token blocks: h 4 KB apart
+    const uint32_t va = vaddr[BS == 16 ? 0 : i >> 2] + soff;
+    const int step = BS == 16 ? i : i & 3;
+    vr[i] = step == 0   ? lds_read_b128<0 * kCt>(va)
+            : step == 1 ? lds_read_b128<1 * kCt>(va)
+            : step == 2 ? lds_read_b128<2 * kCt>(va)
+            : step == 3 ? lds_read_b128<3 * kCt>(va)
+            : step == 4 ? lds_read_b128<4 * kCt>(va)
+            : step == 5 ? lds_read_b128<5 * kCt>(va)
+            : step == 6 ? lds_read_b128<6 * kCt>(va)
+                        : lds_read_b128<7 * kCt>(va);
+  };
+
+  for (int tb0 = w.tok_lo; tb0 < w.tok_hi; tb0 += kSegment) {
+    const int tok_hi = min(w.tok_hi, tb0 + kSegment);
+    const int nstage = (tok_hi - tb0 + 31) / 32;
+    barrier_lds();  // the last tile's, or segment's, reads of the ring and the table are done
+    const int ntab = (nstage * 32 + BS - 1) / BS;
+    for (int i = tid; i < ntab; i += 64 * kWaves) tab[i] = pg.entry(tb0 / BS + i);
+    RingLoader<BS> ld;
+    ld.init(a, w.head, nstage, wave, lane, tab);
+    barrier_lds();
+    // Stages from here on hold positions outside the range or past a row's last.
+    const int inner = max(0, (min(tok_hi, hmin < INT_MAX ? hmin + 1 : INT_MAX) - tb0) / 32);
+
+    struct State {
+      f32x16 sc;       // scores of the stage
+      uint32_t pw[8];  // probabilities of the stage before, as bf16 pairs
+      u32x4 vr[8];     // V of the stage before
+    };
+    auto score_product = [&](f32x16& sc, int s, const u32x4 (&kr)[8]) __attribute__((always_inline)) {
+      f32x16 acc;
+      if (s == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+      } else {
+        acc = sc;
+      }
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[s]), e.q[s], acc, 0, 0, 0);
+    };
+    auto pv_product = [&](int i, const State& x) __attribute__((always_inline)) {
+      const int h = 4 * (i >> 2);
+      o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8, x.vr[i]),
+          __builtin_bit_cast(bf16x8, u32x4{x.pw[h], x.pw[h + 1], x.pw[h + 2], x.pw[h + 3]}), o[i & 3], 0, 0, 0);
+    };
+    // The pair of stages a publish makes room for, loaded until the next one;
+    // the table entries of the pair after it are read one publish ahead.
+    const char* src[kPer] = {nullptr, nullptr};
+    int st_load = 0;
+    uint32_t ent[kPer];
+    auto load = [&](auto fast_c, int i) __attribute__((always_inline)) {
+      if (decltype(fast_c)::value || st_load + i / kStageLoads < nstage)
+        ld.load(src[i / kStageLoads], smem[(st_load + i / kStageLoads) % kRing], i % kStageLoads);
+    };
+    // One stage. FAST: nothing to mask, every load inside the segment, the steady
+    // number of loads in flight. FIRST: no stage before it; LAST: none after it;
+    // PUBLISH: stages st + 1 and st + 2 become readable (this wave's loads of them
+    // have landed, and the barrier says so of every wave's), stages up to st - 1
+    // are no longer read. LOAD: first of the two loads issued here.
+    auto stage = [&](auto owns_c, auto fast_c, auto first_c, auto last_c, auto publish_c, auto load_c, int st, State& x,
+                     u32x4 (&kr)[8]) __attribute__((always_inline)) {
+      constexpr bool OWNS = decltype(owns_c)::value, FAST = decltype(fast_c)::value, FIRST = decltype(first_c)::value;
+      constexpr bool LAST = decltype(last_c)::value, PUBLISH = decltype(publish_c)::value;
+      constexpr int LOAD = decltype(load_c)::value;
+      if constexpr (PUBLISH) {
+        if constexpr (FAST) wait_vmcnt<3 * kStageLoads>();
+        else wait_stage(max(0, min(3, nstage - 3 - st)));
+        barrier_only();
+        st_load = st + kAhead;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          lds_wait(ent[i]);
+          src[i] = ld.base(ent[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) ent[i] = ld.entry(st_load + kPer + i);
+        // Near the ends registers are short: no read may be in flight where the
+        // compiler could spill its register.
+        if constexpr (!FAST) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);
+        }
+      }
+      if constexpr (!OWNS) {
+        if constexpr (LOAD >= 0) {
+          load(fast_c, LOAD);
+          load(fast_c, LOAD + 1);
+        }
+      } else {
+        // 16 slots of one product each: 0-7 the P.V of the stage before, 8-15 the
+        // scores of the stage after. The steps of an element (scale, exponential,
+        // sum, conversion) lie one or more slots apart so that none waits.
+        float sv[16], ex[16], pv[16], ps = 0.0f;
+        uint32_t pw[8];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sv[i] = x.sc[i];
+        if (!FAST && st >= inner) {
+          const int hi = min(tok_hi - 1, e.hz[0]) - (tb0 + st * 32 + 8 * g);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sv[i] = 16 * (i >> 3) + (i & 7) > hi ? masked : sv[i];
+        }
+        const float nm = -m;
+        const uint32_t k_off = slot_off(st + 1), v_off = slot_off(st);
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          if (!FIRST && t < 8) pv_product(t, x);
+          if (!LAST && t >= 8) {
+            // K operand t - 8, read in slot t - 8: all LDS reads but those issued
+            // after it, K t - 7 .. 7 and V max(0, t - 12) .. min(7, t - 5).
+            constexpr int kAfter[8] = {11, 11, 11, 11, 11, 9, 7, 5};
+            lds_wait(kr[t - 8], kAfter[t - 8]);
+            score_product(x.sc, t - 8, kr);
+          }
+          if (!LAST && t < 8) read_k(kr, t, k_off);
+          if (t >= 4 && t < 12) read_v(x.vr, t - 4, v_off);
+          if (LOAD >= 0 && t % 8 == 4) load(fast_c, LOAD + t / 8);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (t == 3 * i / 4) ex[i] = __builtin_fmaf(sv[i], c, nm);
+            if (t == 3 * i / 4 + 1) pv[i] = exp2_fast(ex[i]);
+            if (t == 3 * i / 4 + 3) ps += pv[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (t == 3 * (2 * i + 1) / 4 + 3) {
+              pw[i] = pack2(pv[2 * i], pv[2 * i + 1]);
+              asm volatile("" : "+v"(pw[i]));  // here, not behind the branch below
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (__builtin_expect(__ballot(!(ps <= kSlackSum)) != 0, 0)) {
+          float mx = sv[0] * c;
+#pragma unroll
+          for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sv[i] * c);
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          if (mx > m + kSlack) {  // both lanes of the row agree
+            const float alpha = exp2_fast(m - mx);
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] *= alpha;
+            m = mx;
+          }
+          const float ref = m == kNegInf ? 0.0f : m;
+          ps = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float p0 = exp2_fast(__builtin_fmaf(sv[i], c, -ref)), p1 = exp2_fast(__builtin_fmaf(sv[i + 1], c, -ref));
+            ps += p0 + p1;
+            pw[i / 2] = pack2(p0, p1);
+          }
+        }
+        l += ps;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.pw[i] = pw[i];
+        lds_wait(x.vr);
+        if constexpr (LAST) {
+          const int tb = tb0 + st * 32;
+          if (tb + 32 > tok_hi) {  // what lies behind the end may be anything: 0 * NaN
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint4 z = Engine<__bf16, 128, BS>::zero_past(make_uint4(x.vr[i][0], x.vr[i][1], x.vr[i][2], x.vr[i][3]),
+                                                                tb + 16 * (i >> 2) + 8 * g, tok_hi);
+              x.vr[i] = u32x4{z.x, z.y, z.z, z.w};
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pv_product(i, x);
+        }
+      }
+    };
+
+    // The ring's first stages in flight. (The compiler waits for every load in
+    // flight where the queries are first used: four stages are issued before that
+    // point and two behind it.)
+    auto prologue = [&](auto lo_c, auto hi_c) __attribute__((always_inline)) {
+      constexpr int LO = decltype(lo_c)::value, N = decltype(hi_c)::value - LO;
+      uint32_t e0[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) e0[i] = ld.entry(LO + i);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        lds_wait(e0[i]);
+        if (LO + i < nstage) {
+          const char* from = ld.base(e0[i]);
+#pragma unroll
+          for (int k = 0; k < kStageLoads; ++k) ld.load(from, smem[LO + i], k);
+        }
+      }
+    };
+    prologue(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(e.q[s]));
+    prologue(std::integral_constant<int, 4>{}, std::integral_constant<int, kAhead>{});
+
+    // Every wave runs the same barriers, whether it owns a row tile or not.
+    auto run = [&](auto owns_c) __attribute__((always_inline)) {
+      constexpr bool OWNS = decltype(owns_c)::value;
+      constexpr std::true_type yes{};
+      constexpr std::false_type no{};
+      constexpr std::integral_constant<int, -1> none{};
+      constexpr std::integral_constant<int, 0> load0{};
+      constexpr std::integral_constant<int, 2> load2{};
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) ent[i] = ld.entry(kAhead + i);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);
+      State x;
+      u32x4 kr[8];
+      wait_stage(min(kAhead, nstage) - 1);
+      barrier_only();  // stage 0 is readable
+      if constexpr (OWNS) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) read_k(kr, s, 0);
+        lds_wait(kr);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) score_product(x.sc, s, kr);
+      }
+      if (nstage == 1) {
+        stage(owns_c, no, yes, yes, no, none, 0, x, kr);
+      } else {
+        stage(owns_c, no, yes, no, yes, load0, 0, x, kr);
+        int st = 0;  // the last stage done
+        auto pair = [&](auto fast_c) __attribute__((always_inline)) {
+          stage(owns_c, fast_c, no, no, no, load2, st + 1, x, kr);
+          stage(owns_c, fast_c, no, no, yes, load0, st + 2, x, kr);
+          st += 2;
+        };
+        const int fast_end = min(inner - 2, nstage - kRing);
+        while (st < fast_end) pair(yes);
+        while (st + 3 < nstage) pair(no);
+        // One or two stages are left, all loaded: the last publish, in stage st,
+        // made room for stages st + 6 and st + 7.
+        if (st + 2 < nstage) {
+          stage(owns_c, no, no, no, no, none, st + 1, x, kr);
+          ++st;
+        }
+        stage(owns_c, no, no, yes, no, none, st + 1, x, kr);
+      }
+      wait_vmcnt<0>();
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);  // read ahead, maybe still in flight
+    };
+    if (owns) run(std::true_type{});
+    else run(std::false_type{});
+  }
+}
+
 // Two channel runs of a row, normalised, in the output type.
 __device__ __forceinline__ void store_out(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 __device__ __forceinline__ void store_out(__bf16* p, f32x4 x) {
@@ -442,7 +839,9 @@ template <typename T, int D, int BS>
 __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
   using E = Engine<T, D, BS>;
   constexpr int NT = 64 * kWaves, kFloat4s = D / 8;
-  __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];
+  constexpr bool kWide = std::is_same_v<T, __bf16> && D == 128;
+  __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];  // wide: the ring
+  __shared__ __align__(16) int tab[kWide ? kTabEntries : 1];
   __shared__ float ml[kWaves][2][64 * E::kUnits];
   __shared__ int64_t wave_sum[kWaves];
   __shared__ int64_t start[2];
@@ -521,12 +920,13 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const int n_packed = min(sq.per, sq.rows - r0) * group;
       const int row_tiles = (n_packed + 31) / 32, ways = max(1, kWaves / row_tiles);
       const int rt = wave % row_tiles, way = wave / row_tiles;
-      const bool works = way < ways;
+      const bool works = way < ways;  // wide: every wave loads, those with a row tile compute
       E e;
       e.clear();
       const Pages pg{a.table + static_cast<size_t>(seq) * a.max_blocks, max(0, (sq.kv + BS - 1) / BS - 1), a.num_blocks};
       const int first = tok_lo + way * E::kTokens, stride = ways * E::kTokens;
-      if (works && first < tok_hi) E::issue(a, pg, head, first, lane, smem[wave]);
+      const bool wide = kWide && row_tiles > kWaves / 2;
+      if (!wide && works && first < tok_hi) E::issue(a, pg, head, first, lane, smem[wave]);
       int least = INT_MAX;
       const bool second = E::kUnits == 1 || n_packed - 32 * rt > 16;
 #pragma unroll
@@ -541,7 +941,11 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       }
       least = uniform(wave_min_int(least));
       const float c = a.scale_log2;
-      if (works) {
+      if (wide) {
+        if constexpr (kWide)
+          wide_tile<BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, tab, tid, wave, e);
+        barrier_lds();  // the ring is read: a wave may load its slot for the next tile
+      } else if (works) {
         for (int tb = first; tb < tok_hi; tb += stride) {
           asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
           typename E::Ops x;

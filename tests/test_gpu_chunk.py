@@ -131,6 +131,30 @@ def test_tiles_split_over_slices(new, kv, hq, hkv):
     assert torch.equal(first[0], c.out) and torch.equal(first[1], c.lse)
 
 
+@pytest.mark.parametrize("bs", (16, 32))
+@pytest.mark.parametrize("group", (8, 7))
+def test_tiles_that_fill_a_workgroup(bs, group):
+    """More than 128 packed rows per tile, contexts of one to ten stages, odd and even, whole and part."""
+    new = [17, 20, 31, 32, 33, 19, 28, 36, 37, 64, 65, 18, 25, 29]
+    kv = [17, 33, 63, 64, 65, 95, 97, 128, 130, 160, 190, 224, 288, 319]
+    Case(BF16, group, 1, 128, bs, new, kv, gain=2.0).run_and_check(f"groups of {group}")
+
+
+def test_a_tile_longer_than_its_table_in_lds():
+    """256 tiles of up to 116,000 positions, so that slices don't cut them: the block table goes through LDS in
+    parts. A few rows of the first, a middle and the last tile are compared."""
+    c = Case(BF16, 64, 8, 128, 16, [1024], [116011], spare_rows=0)
+    c.run()
+    torch.cuda.synchronize()
+    (k, v), = c.contexts
+    for r in (0, 5, 31, 500, 1023):
+        end = 116011 - 1024 + r + 1
+        ref = attention(c.q[r:r + 1].cpu(), [(k[:end], v[:end])], [1], c.scale)
+        o_tol, l_tol = bounds(BF16, *ref, c.scale, end, 128)
+        assert ((c.out[r:r + 1].double().cpu() - ref[0]).abs() <= o_tol).all(), r
+        assert ((c.lse[r:r + 1].double().cpu() - ref[1]).abs() <= l_tol).all(), r
+
+
 def test_many_sequences():
     """More sequences than threads of a workgroup, most without rows."""
     n = 1500
