@@ -49,6 +49,8 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kWaves = 8;
 constexpr int kDies = 8;
+// Cache policy of keys and values that one wave reads: non-temporal.
+constexpr int kStream = 2;
 constexpr float kSlack = 8.0f;    // base-2 headroom before the reference moves
 constexpr float kSlackSum = 256.0f;
 
@@ -88,17 +90,25 @@ struct Seq {
 };
 
 // Offsets and lengths are clamped to what the buffers hold.
-__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
+__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off, int kv) {
   Seq s;
   const int group = a.hq / a.hkv;
-  s.row0 = min(max(a.row_off[i], 0), a.n_rows);
-  s.rows = max(0, min(max(a.row_off[i + 1], 0), a.n_rows) - s.row0);
-  s.kv = min(max(a.kv_len[i], 0), a.max_blocks * a.block_size);
+  s.row0 = min(max(off, 0), a.n_rows);
+  s.rows = max(0, min(max(next_off, 0), a.n_rows) - s.row0);
+  s.kv = min(max(kv, 0), a.max_blocks * a.block_size);
   s.per = kChunkTileRows / group;
   s.tiles = (s.rows + s.per - 1) / s.per;
   s.cost = token_cost((min(s.rows, s.per) * group + 31) / 32);
   s.head_cost = s.tiles > 0 ? s.before(s.tiles) : 0;
   return s;
+}
+
+__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
+  return seq_of(a, a.row_off[i], a.row_off[i + 1], a.kv_len[i]);
+}
+// The same for an i that all lanes share, in scalar registers.
+__device__ __forceinline__ Seq seq_uniform(const ChunkArgs& a, int i) {
+  return seq_of(a, uniform(a.row_off[i]), uniform(a.row_off[i + 1]), uniform(a.kv_len[i]));
 }
 
 // Token at which a cut at `y` of a tile's cost goes through its `end` tokens.
@@ -125,11 +135,61 @@ struct Pages {
   }
 };
 
-// Byte `off` of a block, 16 bytes per lane, to `dst` (+ 16 bytes per lane).
-__device__ __forceinline__ void load_lds(const char* block, uint32_t bytes, uint32_t off, void* dst) {
+// Byte off + more (a constant) of a block, 16 bytes per lane, to `dst` (+ 16
+// bytes per lane). POLICY: see kStream.
+template <int POLICY>
+__device__ __forceinline__ void load_lds(const char* block, uint32_t bytes, uint32_t off, int more, void* dst) {
   const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(block), 0, bytes, 0x00027000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(dst), 16, off, 0, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(dst), 16, off, more, 0, POLICY);
 }
+
+// A value that the compiler takes for new: what is computed from it inside a
+// loop stays there instead of in a register for each stage's every address.
+__device__ __forceinline__ uint32_t anew(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Until at most N of this wave's vector loads and stores are in flight.
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// LDS reads outside the compiler's view, which would wait for the direct loads in
+// flight before each. A read's register counts as written only behind an
+// lds_wait that names it (and waits for all reads but the `keep` issued last:
+// they complete in order).
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)(const_cast<void*>(p))));
+}
+__device__ __forceinline__ u32x4 lds_read_b128(uint32_t addr, int off) {
+  u32x4 r;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(off) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ds_read_b32 %0, %1" : "=v"(r) : "v"(addr) : "memory");
+  return r;
+}
+__device__ __forceinline__ void lds_wait(uint32_t& r) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(r) : : "memory"); }
+__device__ __forceinline__ void lds_wait(u32x4& r, int keep) {
+  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(r) : "i"(keep) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void lds_wait(u32x4 (&r)[N]) {
+  lds_wait(r[0], 0);
+#pragma unroll
+  for (int i = 1; i < N; ++i) asm volatile("" : "+v"(r[i]) : : "memory");
+}
+
+// A lane's share of the addresses of a stage: of its loads inside a block and of
+// its operand reads inside a slot.
+struct Bases {
+  uint32_t kload, vload, kread, vread;
+};
 
 template <typename T, int D, int BS>
 struct Engine;
@@ -176,6 +236,11 @@ struct Engine<__bf16, D, BS> {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) q[s] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 16 * s + 8 * g));
   }
+  // The queries have arrived: no wait for them is left for the loops.
+  __device__ __forceinline__ void settle_q() {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(q[s]));
+  }
   __device__ __forceinline__ void clear() {
     m[0] = kNegInf;
     l[0] = 0.0f;
@@ -185,74 +250,88 @@ struct Engine<__bf16, D, BS> {
       for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
   }
 
-  // Stage at token tb (a multiple of 32) into the wave's slot.
-  static __device__ __forceinline__ void issue(const ChunkArgs& a, const Pages& pg, int head, int tb, int lane, uint4* slot) {
+  static __device__ __forceinline__ Bases bases(int lane) {
+    const int tl = lane / kChunksPerToken, c = lane % kChunksPerToken, r = lane & 31, g = lane >> 5;
+    const int t = 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+    Bases x;
+    x.kload = 2 * tl * D + 16 * (c ^ kswz(tl));
+    x.vload = BS == 16 ? 32 * (lane >> 1) + 16 * ((lane & 1) ^ vswz(lane >> 1)) : 64 * (lane >> 2) + 16 * ((lane & 3) ^ vswz(lane >> 2));
+    x.kread = 2 * t * D + 16 * (g ^ kswz(t));
+    x.vread = 16 * kHalf + (BS == 16 ? 32 : 64) * r + 16 * (g ^ vswz(r));
+    return x;
+  }
+  static constexpr int kBlocks = kTokens / BS;  // of a stage: 2 or 1
+
+  // K, or V, of the stage of the blocks `ent` (from their token `first`) into the
+  // wave's slot.
+  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Bases& x, const int (&ent)[kBlocks], int head, int,
+                                                 uint4* slot) {
     constexpr uint32_t kBytes = BS * D * 2;
-    const size_t per_block = static_cast<size_t>(a.hkv) * kBytes, at = static_cast<size_t>(head) * kBytes;
-    constexpr int kBlocks = kTokens / BS;  // 2 or 1
-    const char *kb[kBlocks], *vb[kBlocks];
+    const char* from[kBlocks];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      const size_t e = static_cast<size_t>(uniform(pg.entry(tb / BS + b)));
-      kb[b] = static_cast<const char*>(a.k_cache) + e * per_block + at;
-      vb[b] = static_cast<const char*>(a.v_cache) + e * per_block + at;
+    for (int b = 0; b < kBlocks; ++b)
+      from[b] = static_cast<const char*>(a.k_cache) + (static_cast<size_t>(uniform(ent[b])) * a.hkv + head) * kBytes;
+    const uint32_t kl = anew(x.kload);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {  // tokens tk .. of the stage
+      const int tk = 64 * k / kChunksPerToken;
+      load_lds<kStream>(from[tk / BS], kBytes, kl ^ (16u * kswz(tk)), 2 * (tk % BS) * D, slot + 64 * k);
     }
+  }
+  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Bases& x, const int (&ent)[kBlocks], int head, int,
+                                                 uint4* slot) {
+    constexpr uint32_t kBytes = BS * D * 2;
+    const char* from[kBlocks];
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      const int chunk = 64 * k + lane, t = chunk / kChunksPerToken, c = chunk % kChunksPerToken;
-      load_lds(kb[64 * k / kChunksPerToken / BS], kBytes, 2u * ((t % BS) * D + 8 * (c ^ kswz(t))), slot + 64 * k);
-    }
+    for (int b = 0; b < kBlocks; ++b)
+      from[b] = static_cast<const char*>(a.v_cache) + (static_cast<size_t>(uniform(ent[b])) * a.hkv + head) * kBytes;
+    const uint32_t vl = anew(x.vload);
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      const int chunk = 64 * k + lane;
-      int d, c;
-      if (BS == 16) {
-        d = (chunk % (kHalf / 2)) >> 1;
-        c = (chunk & 1) ^ vswz(d);
-      } else {
-        d = chunk >> 2;
-        c = (chunk & 3) ^ vswz(d);
-      }
-      load_lds(vb[BS == 16 ? 64 * k / (kHalf / 2) : 0], kBytes, 2u * (d * BS + 8 * c), slot + kHalf + 64 * k);
+    for (int k = 0; k < kLoads; ++k) {  // channels dk .. of a half, or of all 32 tokens
+      const int dk = BS == 16 ? 64 * k % (kHalf / 2) / 2 : 16 * k;
+      load_lds<kStream>(from[BS == 16 ? 64 * k / (kHalf / 2) : 0], kBytes, vl ^ (16u * vswz(dk)), 2 * dk * BS,
+                        slot + kHalf + 64 * k);
     }
   }
 
-  struct Ops {
-    uint4 k[kSteps], v[2 * kCt];
-  };
-  static __device__ __forceinline__ void read(const uint4* slot, int lane, Ops& x) {
-    const int r = lane & 31, g = lane >> 5;
-    const int t = 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+  u32x4 kop[kSteps], vop[2 * kCt];
+  // The slot's halves into registers: issued, and waited for by lds_wait.
+  __device__ __forceinline__ void read_k(uint32_t slot, const Bases& b) {
+    const uint32_t kr = anew(b.kread);
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) x.k[s] = slot[t * kChunksPerToken + ((2 * s + g) ^ kswz(t))];
+    for (int s = 0; s < kSteps; ++s) kop[s] = lds_read_b128(slot + (kr ^ (32u * s)), 0);
+    lds_wait(kop);
+  }
+  __device__ __forceinline__ void read_v(uint32_t slot, const Bases& b) {
+    const uint32_t vr = anew(b.vread);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int ct = 0; ct < kCt; ++ct) {
-        const int d = 32 * ct + r;
-        x.v[h * kCt + ct] = slot[kHalf + (BS == 16 ? h * (kHalf / 2) + 2 * d + (g ^ vswz(d)) : 4 * d + ((2 * h + g) ^ vswz(d)))];
-      }
+      for (int ct = 0; ct < kCt; ++ct)
+        vop[h * kCt + ct] = BS == 16 ? lds_read_b128(slot + vr, 8 * kHalf * h + 1024 * ct) : lds_read_b128(slot + (vr ^ (32u * h)), 2048 * ct);
+    lds_wait(vop);
   }
 
   // Zero the elements of an 8-token chunk from position `first` on that lie at or
   // past `end`.
-  static __device__ __forceinline__ uint4 zero_past(uint4 v, int first, int end) {
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  static __device__ __forceinline__ u32x4 zero_past(u32x4 w, int first, int end) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       w[i] &= (first + 2 * i < end ? 0x0000FFFFu : 0u) | (first + 2 * i + 1 < end ? 0xFFFF0000u : 0u);
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return w;
   }
 
-  // Scores, softmax and P.V of the stage at tb; positions from `end` on are not
-  // there, `masked`: a row of the wave doesn't see all of the stage.
-  __device__ __forceinline__ void compute(Ops& x, int tb, int end, bool masked, float c, int lane, bool) {
+  uint32_t pw[8];  // the stage's probabilities, as bf16 pairs
+
+  // Scores and softmax of the stage at tb; positions from `end` on are not there,
+  // `masked`: a row of the wave doesn't see all of the stage.
+  __device__ __forceinline__ void softmax(int tb, int end, bool masked, float c, int lane, bool) {
     const int g = lane >> 5;
     f32x16 sc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.0f;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x.k[s]), q[s], sc, 0, 0, 0);
+    for (int s = 0; s < kSteps; ++s) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kop[s]), q[s], sc, 0, 0, 0);
     float sv[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) sv[e] = sc[e];
@@ -263,7 +342,6 @@ struct Engine<__bf16, D, BS> {
       for (int e = 0; e < 16; ++e) sv[e] = 16 * (e >> 3) + (e & 7) > hi ? none : sv[e];
     }
     float ps = 0.0f;
-    uint32_t pw[8];
     auto probs = [&](float ref) __attribute__((always_inline)) {
       ps = 0.0f;
 #pragma unroll
@@ -289,19 +367,20 @@ struct Engine<__bf16, D, BS> {
       probs(m[0] == kNegInf ? 0.0f : m[0]);
     }
     l[0] += ps;
+  }
+
+  // P.V of the stage.
+  __device__ __forceinline__ void values(int tb, int end, int lane, bool) {
     if (tb + kTokens > end) {  // what lies behind the end may be anything: 0 * NaN
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) x.v[h * kCt + ct] = zero_past(x.v[h * kCt + ct], tb + 16 * h + 8 * g, end);
+      for (int i = 0; i < 2 * kCt; ++i) vop[i] = zero_past(vop[i], tb + 16 * (i / kCt) + 8 * (lane >> 5), end);
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int ct = 0; ct < kCt; ++ct)
-        o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(x.v[h * kCt + ct]), __builtin_bit_cast(bf16x8, u32x4{pw[4 * h], pw[4 * h + 1], pw[4 * h + 2], pw[4 * h + 3]}),
-            o[ct], 0, 0, 0);
+    for (int i = 0; i < 2 * kCt; ++i) {
+      const int h = 4 * (i / kCt), ct = i % kCt;
+      o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8, vop[i]), __builtin_bit_cast(bf16x8, u32x4{pw[h], pw[h + 1], pw[h + 2], pw[h + 3]}), o[ct], 0, 0, 0);
+    }
   }
 };
 
@@ -336,6 +415,12 @@ struct Engine<float, D, BS> {
 #pragma unroll
     for (int j = 0; j < kDt; ++j) q[u][j] = *reinterpret_cast<const f32x4*>(p + 16 * j + 4 * g);
   }
+  __device__ __forceinline__ void settle_q() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < kDt; ++j) asm volatile("" : "+v"(q[u][j]));
+  }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -346,47 +431,57 @@ struct Engine<float, D, BS> {
     }
   }
 
-  static __device__ __forceinline__ void issue(const ChunkArgs& a, const Pages& pg, int head, int tb, int lane, uint4* slot) {
-    constexpr uint32_t kBytes = BS * D * 4;
-    const size_t e = static_cast<size_t>(uniform(pg.entry(tb / BS))), hkv = static_cast<size_t>(a.hkv);
-    const char* kb = static_cast<const char*>(a.k_cache) + (e * hkv + head) * kBytes;
-    const char* vb = static_cast<const char*>(a.v_cache) + (e * hkv + head) * kBytes;
-    const int off = tb % BS;
+  static __device__ __forceinline__ Bases bases(int lane) {
+    const int tl = lane / kChunksPerToken, c = lane % kChunksPerToken, r = lane & 15, g = lane >> 4;
+    Bases x;
+    x.kload = 4 * tl * D + 16 * (c ^ kswz(tl));
+    x.vload = 4 * (lane >> 2) * BS + 16 * ((lane & 3) ^ vswz(lane >> 2));
+    x.kread = 4 * r * D + 16 * (g ^ kswz(r));
+    x.vread = 16 * kHalf + 64 * r + 16 * (g ^ vswz(r));
+    return x;
+  }
+  static constexpr int kBlocks = 1;
+
+  static __device__ __forceinline__ const char* block(const ChunkArgs& a, const void* pool, int ent, int head) {
+    return static_cast<const char*>(pool) + (static_cast<size_t>(uniform(ent)) * a.hkv + head) * (BS * D * 4);
+  }
+  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Bases& x, const int (&ent)[1], int head, int first,
+                                                 uint4* slot) {
+    const char* from = block(a, a.k_cache, ent[0], head);
+    const uint32_t kl = anew(x.kload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      const int chunk = 64 * k + lane, t = chunk / kChunksPerToken, c = chunk % kChunksPerToken;
-      load_lds(kb, kBytes, 4u * ((off + t) * D + 4 * (c ^ kswz(t))), slot + 64 * k);
-    }
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      const int chunk = 64 * k + lane, d = chunk >> 2, c = (chunk & 3) ^ vswz(d);
-      load_lds(vb, kBytes, 4u * (d * BS + off + 4 * c), slot + kHalf + 64 * k);
+      const int tk = 64 * k / kChunksPerToken;
+      load_lds<kStream>(from, BS * D * 4, kl ^ (16u * kswz(tk)), 4 * (first + tk) * D, slot + 64 * k);
     }
   }
-
-  struct Ops {
-    f32x4 k[kDt], v[kDt];
-  };
-  static __device__ __forceinline__ void read(const uint4* slot, int lane, Ops& x) {
-    const int r = lane & 15, g = lane >> 4;
+  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Bases& x, const int (&ent)[1], int head, int first,
+                                                 uint4* slot) {
+    const char* from = block(a, a.v_cache, ent[0], head);
+    const uint32_t vl = anew(x.vload);
 #pragma unroll
-    for (int j = 0; j < kDt; ++j) x.k[j] = __builtin_bit_cast(f32x4, slot[r * kChunksPerToken + ((4 * j + g) ^ kswz(r))]);
-#pragma unroll
-    for (int j = 0; j < kDt; ++j) {
-      const int d = 16 * j + r;
-      x.v[j] = __builtin_bit_cast(f32x4, slot[kHalf + 4 * d + (g ^ vswz(d))]);
-    }
+    for (int k = 0; k < kLoads; ++k)
+      load_lds<kStream>(from, BS * D * 4, vl, 4 * (16 * k * BS + first), slot + kHalf + 64 * k);
   }
 
-  __device__ __forceinline__ void compute(Ops& x, int tb, int end, bool masked, float c, int lane, bool second) {
+  u32x4 kop[kDt], vop[kDt];
+  float p[2][4];  // the stage's probabilities
+  __device__ __forceinline__ void read_k(uint32_t slot, const Bases& b) {
+    const uint32_t kr = anew(b.kread);
+#pragma unroll
+    for (int j = 0; j < kDt; ++j) kop[j] = lds_read_b128(slot + (kr ^ (64u * j)), 0);
+    lds_wait(kop);
+  }
+  __device__ __forceinline__ void read_v(uint32_t slot, const Bases& b) {
+    const uint32_t vr = anew(b.vread);
+#pragma unroll
+    for (int j = 0; j < kDt; ++j) vop[j] = lds_read_b128(slot + vr, 1024 * j);
+    lds_wait(vop);
+  }
+
+  // second: the wave's rows 16 .. 31 are there.
+  __device__ __forceinline__ void softmax(int tb, int end, bool masked, float c, int lane, bool second) {
     const int g = lane >> 4;
-    if (tb + kTokens > end) {
-#pragma unroll
-      for (int j = 0; j < kDt; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (tb + 4 * g + i >= end) x.v[j][i] = 0.0f;
-    }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if (u == 1 && !second) break;
@@ -394,14 +489,13 @@ struct Engine<float, D, BS> {
 #pragma unroll
       for (int j = 0; j < kDt; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[j][i], q[u][j][i], sc, 0, 0, 0);
-      float sv[4];
+        for (int i = 0; i < 4; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kop[j][i]), q[u][j][i], sc, 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sv[i] = sc[i] * c;
-        if (masked && tb + 4 * g + i > min(end - 1, hz[u])) sv[i] = kNegInf;
+        p[u][i] = sc[i] * c;
+        if (masked && tb + 4 * g + i > min(end - 1, hz[u])) p[u][i] = kNegInf;
       }
-      float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
+      float mx = fmaxf(fmaxf(p[u][0], p[u][1]), fmaxf(p[u][2], p[u][3]));
       if (__ballot(mx > m[u] + kSlack) != 0) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -416,13 +510,27 @@ struct Engine<float, D, BS> {
       const float ref = m[u] == kNegInf ? 0.0f : m[u];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sv[i] = exp2_fast(sv[i] - ref);
-        l[u] += sv[i];
+        p[u][i] = exp2_fast(p[u][i] - ref);
+        l[u] += p[u][i];
       }
+    }
+  }
+
+  __device__ __forceinline__ void values(int tb, int end, int lane, bool second) {
+    if (tb + kTokens > end) {
 #pragma unroll
       for (int j = 0; j < kDt; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[j][i], sv[i], o[u][j], 0, 0, 0);
+        for (int i = 0; i < 4; ++i)
+          if (tb + 4 * (lane >> 4) + i >= end) vop[j][i] = 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (u == 1 && !second) break;
+#pragma unroll
+      for (int j = 0; j < kDt; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vop[j][i]), p[u][i], o[u][j], 0, 0, 0);
     }
   }
 };
@@ -446,38 +554,8 @@ constexpr int kAhead = kRing - kPer;
 constexpr int kTabEntries = 6912;    // of a segment: what LDS has left beside the ring
 constexpr int kStageLoads = 2;       // of a wave: the lower four load K, the upper four V
 
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr)(const_cast<void*>(p))));
-}
-template <int OFF = 0>
-__device__ __forceinline__ u32x4 lds_read_b128(uint32_t addr) {
-  static_assert(OFF >= 0 && OFF < 65536, "ds offset field");
-  u32x4 r;
-  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(OFF) : "memory");
-  return r;
-}
-__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr) {
-  uint32_t r;
-  asm volatile("ds_read_b32 %0, %1" : "=v"(r) : "v"(addr) : "memory");
-  return r;
-}
-__device__ __forceinline__ void lds_wait(uint32_t& r) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(r) : : "memory"); }
-__device__ __forceinline__ void lds_wait(u32x4& r, int keep) {
-  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(r) : "i"(keep) : "memory");
-}
-__device__ __forceinline__ void lds_wait(u32x4 (&r)[8]) {
-  asm volatile("s_waitcnt lgkmcnt(0)"
-               : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]), "+v"(r[4]), "+v"(r[5]), "+v"(r[6]), "+v"(r[7])
-               :
-               : "memory");
-}
 __device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-}
 // Until at most `after` (0..5) stages of this wave's loads are in flight.
 __device__ __forceinline__ void wait_stage(int after) {
   switch (after) {
@@ -537,7 +615,7 @@ struct RingLoader {
     return pool + (static_cast<size_t>(uniform(static_cast<int>(ent))) * hkv + head) * (static_cast<size_t>(BS) * 256);
   }
   __device__ __forceinline__ void load(const char* src, uint4* slot, int k) const {
-    load_lds(src, BS * 256, off[k], slot + (kStageLoads * wave + k) * 64);
+    load_lds<0>(src, BS * 256, off[k], 0, slot + (kStageLoads * wave + k) * 64);
   }
 };
 
@@ -572,20 +650,13 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
     return static_cast<uint32_t>(st % kRing) * (kStageChunks * 16);
   };
   auto read_k = [&](u32x4 (&kr)[8], int s, uint32_t soff) __attribute__((always_inline)) {
-    kr[s] = lds_read_b128(s < 4 ? kaddr[s] + soff : (kaddr[s - 4] + soff) ^ 128u);
+    kr[s] = lds_read_b128(s < 4 ? kaddr[s] + soff : (kaddr[s - 4] + soff) ^ 128u, 0);
   };
   auto read_v = [&](u32x4 (&vr)[8], int i, uint32_t soff) __attribute__((always_inline)) {  // vr[4h + ct]
     constexpr int kCt = BS == 16 ? 1024 : 2048;  // bytes between channel tiles; 16-token blocks: h 4 KB apart
     const uint32_t va = vaddr[BS == 16 ? 0 : i >> 2] + soff;
     const int step = BS == 16 ? i : i & 3;
-    vr[i] = step == 0   ? lds_read_b128<0 * kCt>(va)
-            : step == 1 ? lds_read_b128<1 * kCt>(va)
-            : step == 2 ? lds_read_b128<2 * kCt>(va)
-            : step == 3 ? lds_read_b128<3 * kCt>(va)
-            : step == 4 ? lds_read_b128<4 * kCt>(va)
-            : step == 5 ? lds_read_b128<5 * kCt>(va)
-            : step == 6 ? lds_read_b128<6 * kCt>(va)
-                        : lds_read_b128<7 * kCt>(va);
+    vr[i] = lds_read_b128(va, step * kCt);
   };
 
   for (int tb0 = w.tok_lo; tb0 < w.tok_hi; tb0 += kSegment) {
@@ -736,11 +807,8 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
           const int tb = tb0 + st * 32;
           if (tb + 32 > tok_hi) {  // what lies behind the end may be anything: 0 * NaN
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint4 z = Engine<__bf16, 128, BS>::zero_past(make_uint4(x.vr[i][0], x.vr[i][1], x.vr[i][2], x.vr[i][3]),
-                                                                tb + 16 * (i >> 2) + 8 * g, tok_hi);
-              x.vr[i] = u32x4{z.x, z.y, z.z, z.w};
-            }
+            for (int i = 0; i < 8; ++i)
+              x.vr[i] = Engine<__bf16, 128, BS>::zero_past(x.vr[i], tb + 16 * (i >> 2) + 8 * g, tok_hi);
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) pv_product(i, x);
@@ -767,8 +835,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       }
     };
     prologue(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
-#pragma unroll
-    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(e.q[s]));
+    e.settle_q();
     prologue(std::integral_constant<int, 4>{}, std::integral_constant<int, kAhead>{});
 
     // Every wave runs the same barriers, whether it owns a row tile or not.
@@ -879,8 +946,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   const int64_t want = total / kMinSlice;
   const int n_slices = static_cast<int>(want < 1 ? 1 : want < kChunkSlices ? want : kChunkSlices);
   if (slice >= n_slices || total == 0) return;
-  int64_t pos = total * slice / n_slices;
-  const int64_t stop = total * (slice + 1) / n_slices;
+  int64_t pos = uniform(total * slice / n_slices);
+  const int64_t stop = uniform(total * (slice + 1) / n_slices);
   {
     int64_t at = (upto - sum) * a.hkv;
     if (pos >= at && pos < upto * a.hkv) {
@@ -898,7 +965,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   __syncthreads();
   int seq = uniform(static_cast<int>(start[0]));
   const int64_t in_seq = uniform(start[1]);
-  Seq sq = seq_of(a, seq);
+  Seq sq = seq_uniform(a, seq);
   int head = static_cast<int>(in_seq / sq.head_cost);
   int64_t y0 = in_seq % sq.head_cost;
   int tile = 0;
@@ -911,10 +978,19 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 
   for (;;) {
     // ---- one tile, or the slice's piece of it ----
-    const int end = sq.end(tile);
+    // All of this is the same in every lane; said to the compiler, it stays in
+    // scalar registers (64-bit comparisons would move it to vector ones, and a
+    // load from a block there takes a loop over the lanes' addresses).
+    seq = uniform(seq);
+    head = uniform(head);
+    tile = uniform(tile);
+    y0 = uniform(y0);
+    pos = uniform(pos);
+    sq = seq_of(a, uniform(sq.row0), uniform(sq.row0 + sq.rows), uniform(sq.kv));
+    const int end = uniform(sq.end(tile));
     const int64_t tile_cost = kTileCost + static_cast<int64_t>(end) * sq.cost;
-    const int64_t y1 = min(tile_cost, y0 + stop - pos);
-    const int tok_lo = cut(y0, tile_cost, sq.cost, end), tok_hi = cut(y1, tile_cost, sq.cost, end);
+    const int64_t y1 = uniform(min(tile_cost, y0 + stop - pos));
+    const int tok_lo = uniform(cut(y0, tile_cost, sq.cost, end)), tok_hi = uniform(cut(y1, tile_cost, sq.cost, end));
     if (tok_hi > tok_lo || (end == 0 && y0 == 0)) {
       const int r0 = tile * sq.per;  // first query row of the tile, in the sequence
       const int n_packed = min(sq.per, sq.rows - r0) * group;
@@ -926,7 +1002,18 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const Pages pg{a.table + static_cast<size_t>(seq) * a.max_blocks, max(0, (sq.kv + BS - 1) / BS - 1), a.num_blocks};
       const int first = tok_lo + way * E::kTokens, stride = ways * E::kTokens;
       const bool wide = kWide && row_tiles > kWaves / 2;
-      if (!wide && works && first < tok_hi) E::issue(a, pg, head, first, lane, smem[wave]);
+      const Bases at = E::bases(lane);
+      int ent[E::kBlocks], ahead[E::kBlocks];  // blocks of the stage that is loaded next, and of the one behind it
+      auto look_up = [&](int (&to)[E::kBlocks], int tb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < E::kBlocks; ++b) to[b] = pg.entry(tb / BS + b);
+      };
+      if (!wide && works && first < tok_hi) {
+        look_up(ent, first);
+        look_up(ahead, first + stride);
+        E::issue_k(a, at, ent, head, first % BS, smem[wave]);
+        E::issue_v(a, at, ent, head, first % BS, smem[wave]);
+      }
       int least = INT_MAX;
       const bool second = E::kUnits == 1 || n_packed - 32 * rt > 16;
 #pragma unroll
@@ -946,13 +1033,27 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           wide_tile<BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, tab, tid, wave, e);
         barrier_lds();  // the ring is read: a wave may load its slot for the next tile
       } else if (works) {
+        // K and V of a stage are loaded as soon as the slot's halves have been read:
+        // at every wait the loads behind the awaited half are the other half's, kLoads
+        // of them. (Lookups are issued in front of the loads of a half: they can only
+        // make a wait longer.)
+        const uint32_t slot = lds_addr(smem[wave]);
+        e.settle_q();
         for (int tb = first; tb < tok_hi; tb += stride) {
-          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-          typename E::Ops x;
-          E::read(smem[wave], lane, x);
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the slot is written again
-          if (tb + stride < tok_hi) E::issue(a, pg, head, tb + stride, lane, smem[wave]);
-          e.compute(x, tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second);
+          const bool more = tb + stride < tok_hi;
+          wait_vmcnt<E::kLoads>();
+          e.read_k(slot, at);  // (waited for: the half may be written again)
+#pragma unroll
+          for (int b = 0; b < E::kBlocks; ++b) ent[b] = ahead[b];
+          look_up(ahead, tb + 2 * stride);
+          asm volatile("" ::: "memory");
+          if (more) E::issue_k(a, at, ent, head, (tb + stride) % BS, smem[wave]);
+          e.softmax(tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second);
+          if (more) wait_vmcnt<E::kLoads>();
+          else wait_vmcnt<0>();
+          e.read_v(slot, at);
+          if (more) E::issue_v(a, at, ent, head, (tb + stride) % BS, smem[wave]);
+          e.values(tb, tok_hi, lane, second);
         }
       }
       if (ways > 1) {  // join the ways: the first takes the others' results
@@ -1043,7 +1144,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       }
     }
     // ---- the next tile of the line ----
-    pos += y1 - y0;
+    pos = uniform(pos + y1 - y0);
     y0 = 0;
     if (pos >= stop) break;
     if (++tile == sq.tiles) {
@@ -1060,7 +1161,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
         }
         if (found < 0) break;
         seq = uniform(found);
-        sq = seq_of(a, seq);
+        sq = seq_uniform(a, seq);
       }
     }
   }
