@@ -55,7 +55,7 @@ constexpr float kSlack = 8.0f;    // base-2 headroom before the reference moves
 constexpr float kSlackSum = 256.0f;
 
 // The line's unit is half the time that a token takes where HBM bounds it.
-constexpr int kTileCost = 256;      // a tile's start-up
+constexpr int kTileCost = 512;      // a tile's start-up
 constexpr int kMinSlice = 512;      // least length of a slice
 constexpr int kMinPiece = 64;       // tokens: a cut closer to a tile's end moves to it
 __device__ __forceinline__ int token_cost(int row_tiles) { return row_tiles <= 2 ? 2 : row_tiles <= 4 ? 3 : 4; }
@@ -66,7 +66,11 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
          static_cast<uint32_t>(uniform(static_cast<int>(x)));
 }
 
-// A sequence's tiles and their cost on the line.
+// A sequence's tiles and their cost on the line. On the line a sequence's tiles
+// of a KV head go first, last, second, last but one, ...: the later a tile, the
+// more it sees, and so every two neighbours cost the same and slices end where
+// tiles do (in the order of the tiles a 4,096-token prompt's first slices held
+// eleven start-ups each).
 struct Seq {
   int row0, rows, kv;
   int per;    // query rows of a tile
@@ -75,40 +79,51 @@ struct Seq {
   int64_t head_cost;
   // positions that tile j sees
   __device__ __forceinline__ int end(int j) const { return max(0, kv - rows + min(rows, (j + 1) * per)); }
-  // cost of the tiles before tile j
-  __device__ __forceinline__ int64_t before(int j) const {
+  __device__ __forceinline__ int64_t tile_cost(int j) const { return kTileCost + static_cast<int64_t>(end(j)) * cost; }
+  // cost of the tiles 0 .. j - 1
+  __device__ __forceinline__ int64_t first(int j) const {
     const int64_t base = kv - rows;
     const int whole = min(j, tiles - 1);  // tiles that end at a multiple of `per`
-    const int first = base >= 0 ? 0 : static_cast<int>(-base / per);  // the first of them that sees something
+    const int blind = base >= 0 ? 0 : static_cast<int>(-base / per);  // of these, that see nothing
     int64_t tokens = 0;
-    if (whole > first)
-      tokens = (whole - first) * base +
-               per * (static_cast<int64_t>(whole) * (whole + 1) / 2 - static_cast<int64_t>(first) * (first + 1) / 2);
+    if (whole > blind)
+      tokens = (whole - blind) * base +
+               per * (static_cast<int64_t>(whole) * (whole + 1) / 2 - static_cast<int64_t>(blind) * (blind + 1) / 2);
     if (j == tiles) tokens += max(0, kv);
     return static_cast<int64_t>(j) * kTileCost + tokens * cost;
+  }
+  // the k-th tile on the line, and the cost of those before it
+  __device__ __forceinline__ int at(int k) const { return k & 1 ? tiles - 1 - (k >> 1) : k >> 1; }
+  __device__ __forceinline__ int64_t before(int k) const {
+    return first((k + 1) >> 1) + head_cost - first(tiles - (k >> 1));
   }
 };
 
 // Offsets and lengths are clamped to what the buffers hold.
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off, int kv) {
   Seq s;
-  const int group = a.hq / a.hkv;
   s.row0 = min(max(off, 0), a.n_rows);
   s.rows = max(0, min(max(next_off, 0), a.n_rows) - s.row0);
   s.kv = min(max(kv, 0), a.max_blocks * a.block_size);
-  s.per = kChunkTileRows / group;
-  s.tiles = (s.rows + s.per - 1) / s.per;
-  s.cost = token_cost((min(s.rows, s.per) * group + 31) / 32);
-  s.head_cost = s.tiles > 0 ? s.before(s.tiles) : 0;
+  s.per = a.tile_rows;
+  s.tiles = s.rows <= s.per ? s.rows > 0 : (s.rows + s.per - 1) / s.per;
+  s.cost = token_cost((min(s.rows, s.per) * a.group + 31) / 32);
+  s.head_cost = s.tiles <= 1 ? s.tiles * s.tile_cost(0) : s.first(s.tiles);
   return s;
 }
-
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
   return seq_of(a, a.row_off[i], a.row_off[i + 1], a.kv_len[i]);
 }
 // The same for an i that all lanes share, in scalar registers.
 __device__ __forceinline__ Seq seq_uniform(const ChunkArgs& a, int i) {
   return seq_of(a, uniform(a.row_off[i]), uniform(a.row_off[i + 1]), uniform(a.kv_len[i]));
+}
+
+// Where the line of length `total` is cut in front of slice i of n. (Fewer slices
+// than workgroups: the line is short.)
+__device__ __forceinline__ int64_t line_cut(int64_t total, int i, int n) {
+  return n == kChunkSlices ? total / kChunkSlices * i + total % kChunkSlices * i / kChunkSlices
+                           : static_cast<int64_t>(static_cast<uint64_t>(total) * i / n);
 }
 
 // Token at which a cut at `y` of a tile's cost goes through its `end` tokens.
@@ -209,16 +224,11 @@ struct Engine<__bf16, D, BS> {
 
   static __device__ __forceinline__ int row(int lane, int) { return lane & 31; }
   static __device__ __forceinline__ int out_row(int lane, int) { return lane & 31; }
-  static __device__ __forceinline__ int out_unit(int) { return 0; }
   static __device__ __forceinline__ int out_channel(int lane, int i) { return 32 * (i / 4) + 8 * (i % 4) + 4 * (lane >> 5); }
   __device__ __forceinline__ f32x4 get(int i) const {
     const f32x16& v = o[i / 4];
     const int e = 4 * (i % 4);
     return f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-  }
-  __device__ __forceinline__ void set(int i, f32x4 x) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[i / 4][4 * (i % 4) + k] = x[k];
   }
   __device__ __forceinline__ float row_sum(int) const { return l[0] + __shfl_xor(l[0], 32); }
 
@@ -399,10 +409,8 @@ struct Engine<float, D, BS> {
 
   static __device__ __forceinline__ int row(int lane, int u) { return 16 * u + (lane & 15); }
   static __device__ __forceinline__ int out_row(int lane, int i) { return 16 * (i / kDt) + (lane & 15); }
-  static __device__ __forceinline__ int out_unit(int i) { return i / kDt; }
   static __device__ __forceinline__ int out_channel(int lane, int i) { return 16 * (i % kDt) + 4 * (lane >> 4); }
   __device__ __forceinline__ f32x4 get(int i) const { return o[i / kDt][i % kDt]; }
-  __device__ __forceinline__ void set(int i, f32x4 x) { o[i / kDt][i % kDt] = x; }
   __device__ __forceinline__ float row_sum(int u) const {
     const float x = l[u] + __shfl_xor(l[u], 16);
     return x + __shfl_xor(x, 32);
@@ -556,18 +564,6 @@ constexpr int kStageLoads = 2;       // of a wave: the lower four load K, the up
 
 __device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
-// Until at most `after` (0..5) stages of this wave's loads are in flight.
-__device__ __forceinline__ void wait_stage(int after) {
-  switch (after) {
-    case 5: wait_vmcnt<5 * kStageLoads>(); break;
-    case 4: wait_vmcnt<4 * kStageLoads>(); break;
-    case 3: wait_vmcnt<3 * kStageLoads>(); break;
-    case 2: wait_vmcnt<2 * kStageLoads>(); break;
-    case 1: wait_vmcnt<kStageLoads>(); break;
-    default: wait_vmcnt<0>(); break;
-  }
-}
-
 // A tile, or the piece of it that a slice works on.
 struct Tile {
   int row0, hz0;        // query row of the first packed row, and its last visible position
@@ -693,27 +689,26 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
           __builtin_bit_cast(bf16x8, u32x4{x.pw[h], x.pw[h + 1], x.pw[h + 2], x.pw[h + 3]}), o[i & 3], 0, 0, 0);
     };
     // The pair of stages a publish makes room for, loaded until the next one;
-    // the table entries of the pair after it are read one publish ahead.
+    // the table entries of the pair after it are read one publish ahead. Behind
+    // the last stage these are loads of that stage again: so the number of loads
+    // in flight is always the same, and the loop needs no variant for its end.
     const char* src[kPer] = {nullptr, nullptr};
     int st_load = 0;
     uint32_t ent[kPer];
-    auto load = [&](auto fast_c, int i) __attribute__((always_inline)) {
-      if (decltype(fast_c)::value || st_load + i / kStageLoads < nstage)
-        ld.load(src[i / kStageLoads], smem[(st_load + i / kStageLoads) % kRing], i % kStageLoads);
+    auto load = [&](int i) __attribute__((always_inline)) {
+      ld.load(src[i / kStageLoads], smem[(st_load + i / kStageLoads) % kRing], i % kStageLoads);
     };
-    // One stage. FAST: nothing to mask, every load inside the segment, the steady
-    // number of loads in flight. FIRST: no stage before it; LAST: none after it;
-    // PUBLISH: stages st + 1 and st + 2 become readable (this wave's loads of them
-    // have landed, and the barrier says so of every wave's), stages up to st - 1
-    // are no longer read. LOAD: first of the two loads issued here.
-    auto stage = [&](auto owns_c, auto fast_c, auto first_c, auto last_c, auto publish_c, auto load_c, int st, State& x,
+    // One stage. FIRST: no stage before it; LAST: none after it; PUBLISH: stages
+    // st + 1 and st + 2 become readable (this wave's loads of them have landed,
+    // and the barrier says so of every wave's), stages up to st - 1 are no longer
+    // read. LOAD: first of the two loads issued here.
+    auto stage = [&](auto owns_c, auto first_c, auto last_c, auto publish_c, auto load_c, int st, State& x,
                      u32x4 (&kr)[8]) __attribute__((always_inline)) {
-      constexpr bool OWNS = decltype(owns_c)::value, FAST = decltype(fast_c)::value, FIRST = decltype(first_c)::value;
+      constexpr bool OWNS = decltype(owns_c)::value, FIRST = decltype(first_c)::value;
       constexpr bool LAST = decltype(last_c)::value, PUBLISH = decltype(publish_c)::value;
       constexpr int LOAD = decltype(load_c)::value;
       if constexpr (PUBLISH) {
-        if constexpr (FAST) wait_vmcnt<3 * kStageLoads>();
-        else wait_stage(max(0, min(3, nstage - 3 - st)));
+        wait_vmcnt<3 * kStageLoads>();
         barrier_only();
         st_load = st + kAhead;
 #pragma unroll
@@ -723,17 +718,11 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) ent[i] = ld.entry(st_load + kPer + i);
-        // Near the ends registers are short: no read may be in flight where the
-        // compiler could spill its register.
-        if constexpr (!FAST) {
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);
-        }
       }
       if constexpr (!OWNS) {
         if constexpr (LOAD >= 0) {
-          load(fast_c, LOAD);
-          load(fast_c, LOAD + 1);
+          load(LOAD);
+          load(LOAD + 1);
         }
       } else {
         // 16 slots of one product each: 0-7 the P.V of the stage before, 8-15 the
@@ -743,7 +732,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         uint32_t pw[8];
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[i] = x.sc[i];
-        if (!FAST && st >= inner) {
+        if (__builtin_expect(st >= inner, 0)) {
           const int hi = min(tok_hi - 1, e.hz[0]) - (tb0 + st * 32 + 8 * g);
 #pragma unroll
           for (int i = 0; i < 16; ++i) sv[i] = 16 * (i >> 3) + (i & 7) > hi ? masked : sv[i];
@@ -762,7 +751,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
           }
           if (!LAST && t < 8) read_k(kr, t, k_off);
           if (t >= 4 && t < 12) read_v(x.vr, t - 4, v_off);
-          if (LOAD >= 0 && t % 8 == 4) load(fast_c, LOAD + t / 8);
+          if (LOAD >= 0 && t % 8 == 4) load(LOAD + t / 8);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             if (t == 3 * i / 4) ex[i] = __builtin_fmaf(sv[i], c, nm);
@@ -827,11 +816,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         lds_wait(e0[i]);
-        if (LO + i < nstage) {
-          const char* from = ld.base(e0[i]);
+        const char* from = ld.base(e0[i]);
 #pragma unroll
-          for (int k = 0; k < kStageLoads; ++k) ld.load(from, smem[LO + i], k);
-        }
+        for (int k = 0; k < kStageLoads; ++k) ld.load(from, smem[LO + i], k);
       }
     };
     prologue(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
@@ -852,7 +839,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);
       State x;
       u32x4 kr[8];
-      wait_stage(min(kAhead, nstage) - 1);
+      wait_vmcnt<(kAhead - 1) * kStageLoads>();
       barrier_only();  // stage 0 is readable
       if constexpr (OWNS) {
 #pragma unroll
@@ -862,25 +849,21 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         for (int s = 0; s < 8; ++s) score_product(x.sc, s, kr);
       }
       if (nstage == 1) {
-        stage(owns_c, no, yes, yes, no, none, 0, x, kr);
+        stage(owns_c, yes, yes, no, none, 0, x, kr);
       } else {
-        stage(owns_c, no, yes, no, yes, load0, 0, x, kr);
+        stage(owns_c, yes, no, yes, load0, 0, x, kr);
         int st = 0;  // the last stage done
-        auto pair = [&](auto fast_c) __attribute__((always_inline)) {
-          stage(owns_c, fast_c, no, no, no, load2, st + 1, x, kr);
-          stage(owns_c, fast_c, no, no, yes, load0, st + 2, x, kr);
+        while (st + 3 < nstage) {
+          stage(owns_c, no, no, no, load2, st + 1, x, kr);
+          stage(owns_c, no, no, yes, load0, st + 2, x, kr);
           st += 2;
-        };
-        const int fast_end = min(inner - 2, nstage - kRing);
-        while (st < fast_end) pair(yes);
-        while (st + 3 < nstage) pair(no);
-        // One or two stages are left, all loaded: the last publish, in stage st,
-        // made room for stages st + 6 and st + 7.
+        }
+        // One or two stages are left, all loaded.
         if (st + 2 < nstage) {
-          stage(owns_c, no, no, no, no, none, st + 1, x, kr);
+          stage(owns_c, no, no, no, none, st + 1, x, kr);
           ++st;
         }
-        stage(owns_c, no, no, yes, no, none, st + 1, x, kr);
+        stage(owns_c, no, yes, no, none, st + 1, x, kr);
       }
       wait_vmcnt<0>();
 #pragma unroll
@@ -891,10 +874,13 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
   }
 }
 
-// Two channel runs of a row, normalised, in the output type.
-__device__ __forceinline__ void store_out(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
-__device__ __forceinline__ void store_out(__bf16* p, f32x4 x) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+// Eight channels of a row, in the output type.
+__device__ __forceinline__ void store_out(float* p, f32x4 x, f32x4 y) {
+  reinterpret_cast<f32x4*>(p)[0] = x;
+  reinterpret_cast<f32x4*>(p)[1] = y;
+}
+__device__ __forceinline__ void store_out(__bf16* p, f32x4 x, f32x4 y) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(y[0], y[1]), pack2(y[2], y[3]));
 }
 
 // Index of a slice's piece: 0 of a tile that began before it, 1 of one that goes on behind it.
@@ -902,31 +888,24 @@ __device__ __forceinline__ size_t piece_row(int slice, int which) {
   return (static_cast<size_t>(slice) * 2 + which) * kChunkTileRows;
 }
 
-template <typename T, int D, int BS>
-__global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
-  using E = Engine<T, D, BS>;
-  constexpr int NT = 64 * kWaves, kFloat4s = D / 8;
-  constexpr bool kWide = std::is_same_v<T, __bf16> && D == 128;
-  __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];  // wide: the ring
-  __shared__ __align__(16) int tab[kWide ? kTabEntries : 1];
-  __shared__ float ml[kWaves][2][64 * E::kUnits];
-  __shared__ int64_t wave_sum[kWaves];
-  __shared__ int64_t start[2];
-  static_assert(2 * E::kHalf >= kFloat4s * 64, "a wave's slot holds its accumulator");
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int group = a.hq / a.hkv;
+// Where a slice begins.
+struct Start {
+  int seq, row0, rows, kv, head, nth;
+  int64_t y0;
+};
 
-  // ---- the slice: its place on the line ----
-  const int per_die = kChunkSlices / kDies;
-  const int slice = static_cast<int>(blockIdx.x) % kDies * per_die + static_cast<int>(blockIdx.x) / kDies;
-  if (tid == 0) {
-    a.splits[slice].n_rows = 0;
-    a.continues[slice] = 0;
-  }
-  const int per_thread = (a.n_seqs + NT - 1) / NT;
+// The line's length and this slice's part of it, in [pos, stop); false: none.
+__device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int tid, int64_t* wave_sum, Start* start, int* n_slices,
+                                           int64_t* total_out, int64_t* pos_out, int64_t* stop_out) {
+  const int lane = tid & 63, wave = tid >> 6;
+  const int per_thread = (a.n_seqs + 64 * kWaves - 1) / (64 * kWaves);
   const int i0 = min(tid * per_thread, a.n_seqs), i1 = min(i0 + per_thread, a.n_seqs);
   int64_t sum = 0;
-  for (int i = i0; i < i1; ++i) sum += seq_of(a, i).head_cost;
+  Seq s;
+  for (int i = i0; i < i1; ++i) {
+    s = seq_of(a, i);
+    sum += s.head_cost;
+  }
   int64_t upto = sum;
 #pragma unroll
   for (int by = 1; by < 64; by *= 2) {
@@ -943,38 +922,67 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   }
   // (a sequence's KV heads lie side by side: the line is hkv times the sum)
   total = uniform(total) * a.hkv;
-  const int64_t want = total / kMinSlice;
-  const int n_slices = static_cast<int>(want < 1 ? 1 : want < kChunkSlices ? want : kChunkSlices);
-  if (slice >= n_slices || total == 0) return;
-  int64_t pos = uniform(total * slice / n_slices);
-  const int64_t stop = uniform(total * (slice + 1) / n_slices);
-  {
-    int64_t at = (upto - sum) * a.hkv;
-    if (pos >= at && pos < upto * a.hkv) {
-      for (int i = i0; i < i1; ++i) {
-        const int64_t c = seq_of(a, i).head_cost * a.hkv;
-        if (pos < at + c) {
-          start[0] = i;
-          start[1] = pos - at;
-          break;
-        }
-        at += c;
-      }
+  const int n = static_cast<int>(min(max(total / kMinSlice, static_cast<int64_t>(1)), static_cast<int64_t>(kChunkSlices)));
+  *n_slices = n;
+  *total_out = total;
+  if (slice >= n || total == 0) return false;
+  const int64_t pos = line_cut(total, slice, n);
+  *pos_out = pos;
+  *stop_out = line_cut(total, slice + 1, n);
+  int64_t at = (upto - sum) * a.hkv;
+  if (pos >= at && pos < upto * a.hkv) {
+    int i = i0;
+    for (; i1 - i0 > 1; ++i) {
+      s = seq_of(a, i);
+      if (pos < at + s.head_cost * a.hkv) break;
+      at += s.head_cost * a.hkv;
     }
+    int64_t y0 = pos - at;
+    int head = static_cast<int>(static_cast<double>(y0) / static_cast<double>(s.head_cost));
+    if (head * s.head_cost > y0) --head;
+    else if ((head + 1) * s.head_cost <= y0) ++head;
+    y0 -= head * s.head_cost;
+    int nth = 0;
+    for (int hi = s.tiles; hi - nth > 1;) {  // the last tile that begins at or before y0
+      const int mid = (nth + hi) >> 1;
+      if (s.before(mid) <= y0) nth = mid;
+      else hi = mid;
+    }
+    if (nth > 0) y0 -= s.before(nth);
+    *start = Start{i, s.row0, s.rows, s.kv, head, nth, y0};
   }
   __syncthreads();
-  int seq = uniform(static_cast<int>(start[0]));
-  const int64_t in_seq = uniform(start[1]);
-  Seq sq = seq_uniform(a, seq);
-  int head = static_cast<int>(in_seq / sq.head_cost);
-  int64_t y0 = in_seq % sq.head_cost;
-  int tile = 0;
-  for (int hi = sq.tiles; hi - tile > 1;) {  // the last tile that begins at or before y0
-    const int mid = (tile + hi) >> 1;
-    if (sq.before(mid) <= y0) tile = mid;
-    else hi = mid;
+  return true;
+}
+
+template <typename T, int D, int BS>
+__global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
+  using E = Engine<T, D, BS>;
+  constexpr int kFloat4s = D / 8;  // of a lane's accumulator
+  constexpr bool kWide = std::is_same_v<T, __bf16> && D == 128;
+  __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];  // a slot for each wave; wide: the ring
+  __shared__ __align__(16) int tab[kWide ? kTabEntries : 1];
+  __shared__ float2 ml[kWaves][32];
+  __shared__ int64_t wave_sum[kWaves];
+  __shared__ Start start;
+  static_assert(2 * E::kHalf >= kFloat4s * 64, "a wave's slot holds its accumulator");
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int group = a.group;
+  const int per_die = kChunkSlices / kDies;
+  const int slice = static_cast<int>(blockIdx.x) % kDies * per_die + static_cast<int>(blockIdx.x) / kDies;
+  if (tid == 0) {
+    a.splits[slice].n_rows = 0;
+    a.continues[slice] = 0;
   }
-  y0 -= sq.before(tile);
+  int n_slices;
+  int64_t total, pos, stop;
+  if (!find_slice(a, slice, tid, wave_sum, &start, &n_slices, &total, &pos, &stop)) return;
+  int seq = start.seq, head = start.head, nth = start.nth;
+  int64_t y0 = start.y0;
+  Seq sq;
+  sq.row0 = start.row0;
+  sq.rows = start.rows;
+  sq.kv = start.kv;
 
   for (;;) {
     // ---- one tile, or the slice's piece of it ----
@@ -983,12 +991,13 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     // load from a block there takes a loop over the lanes' addresses).
     seq = uniform(seq);
     head = uniform(head);
-    tile = uniform(tile);
+    nth = uniform(nth);
     y0 = uniform(y0);
     pos = uniform(pos);
+    stop = uniform(stop);
     sq = seq_of(a, uniform(sq.row0), uniform(sq.row0 + sq.rows), uniform(sq.kv));
-    const int end = uniform(sq.end(tile));
-    const int64_t tile_cost = kTileCost + static_cast<int64_t>(end) * sq.cost;
+    const int tile = sq.at(nth), end = uniform(sq.end(tile));
+    const int64_t tile_cost = uniform(sq.tile_cost(tile));
     const int64_t y1 = uniform(min(tile_cost, y0 + stop - pos));
     const int tok_lo = uniform(cut(y0, tile_cost, sq.cost, end)), tok_hi = uniform(cut(y1, tile_cost, sq.cost, end));
     if (tok_hi > tok_lo || (end == 0 && y0 == 0)) {
@@ -1056,78 +1065,53 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           e.values(tb, tok_hi, lane, second);
         }
       }
-      if (ways > 1) {  // join the ways: the first takes the others' results
-        if (works && way > 0) {
+      // ---- join the ways, and write the outputs or the piece for the merge ----
+      // Every wave puts its sums into LDS by rows, then takes rows of the tile:
+      // kRows at a time, eight channels a lane, so that stores fill lines.
+      constexpr int kLanesPerRow = D / 8, kRows = 64 / kLanesPerRow, kPasses = 32 / kRows;
+      auto chunk_at = [&](int w, int r, int c) __attribute__((always_inline)) {
+        return reinterpret_cast<f32x4*>(smem[w]) + r * (D / 4) + (c ^ (r & (D / 4 - 1)));
+      };
+      if (works) {
 #pragma unroll
-          for (int u = 0; u < E::kUnits; ++u) {
-            ml[wave][0][64 * u + lane] = e.m[u];
-            ml[wave][1][64 * u + lane] = e.l[u];
-          }
-#pragma unroll
-          for (int i = 0; i < kFloat4s; ++i) reinterpret_cast<f32x4*>(smem[wave])[64 * i + lane] = e.get(i);
+        for (int u = 0; u < E::kUnits; ++u) {
+          const float sum = e.row_sum(u);
+          if (lane < 32 / E::kUnits) ml[wave][E::row(lane, u)] = make_float2(e.m[u], sum);
         }
-        __syncthreads();
-        if (works && way == 0) {
-          for (int v = 1; v < ways; ++v) {
-            const int other = v * row_tiles + rt;
-            float mine[E::kUnits], theirs[E::kUnits];
 #pragma unroll
-            for (int u = 0; u < E::kUnits; ++u) {
-              const float om = ml[other][0][64 * u + lane], top = fmaxf(e.m[u], om), ref = top == kNegInf ? 0.0f : top;
-              mine[u] = exp2_fast(e.m[u] - ref);
-              theirs[u] = exp2_fast(om - ref);
-              e.l[u] = e.l[u] * mine[u] + ml[other][1][64 * u + lane] * theirs[u];
-              e.m[u] = top;
-            }
-#pragma unroll
-            for (int i = 0; i < kFloat4s; ++i) {
-              const int u = E::out_unit(i);
-              e.set(i, e.get(i) * mine[u] + reinterpret_cast<const f32x4*>(smem[other])[64 * i + lane] * theirs[u]);
-            }
-          }
-        }
-        __syncthreads();  // the slots are read
+        for (int i = 0; i < kFloat4s; ++i) *chunk_at(wave, E::out_row(lane, i), E::out_channel(lane, i) / 4) = e.get(i);
       }
-      // ---- its outputs, or its piece for the merge ----
+      if (ways > 1) __syncthreads();
       const bool whole = tok_lo == 0 && tok_hi == end;
-      const int which = tok_lo == 0 ? 1 : 0;
-      if (works && way == 0) {
-        float sum_u[E::kUnits];
-#pragma unroll
-        for (int u = 0; u < E::kUnits; ++u) sum_u[u] = e.row_sum(u);
+      const int passes = ways > 1 ? row_tiles * kPasses / kWaves + (row_tiles * kPasses % kWaves != 0) : works ? kPasses : 0;
+      for (int k = 0; k < passes; ++k) {
+        const int id = (ways > 1 ? wave : rt) * passes + k, tr = id / kPasses, r = id % kPasses * kRows + lane / kLanesPerRow;
+        const int p = 32 * tr + r, c = 2 * (lane % kLanesPerRow);
+        if (p >= n_packed) continue;
+        float m = kNegInf, l = 0.0f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+        for (int v = 0; v < ways; ++v) m = fmaxf(m, ml[v * row_tiles + tr][r].x);
+        const float ref = m == kNegInf ? 0.0f : m;
+        for (int v = 0; v < ways; ++v) {
+          const int w = v * row_tiles + tr;
+          const float f = exp2_fast(ml[w][r].x - ref);
+          l += ml[w][r].y * f;
+          x += *chunk_at(w, r, c) * f;
+          y += *chunk_at(w, r, c + 1) * f;
+        }
         if (whole) {
-#pragma unroll
-          for (int u = 0; u < E::kUnits; ++u) {
-            const int p = 32 * rt + E::row(lane, u);
-            if (a.lse != nullptr && p < n_packed && lane < 32 / E::kUnits) {
-              a.lse[static_cast<size_t>(sq.row0 + r0 + p / group) * a.hq + head * group + p % group] =
-                  sum_u[u] > 0.0f ? (e.m[u] + __builtin_amdgcn_logf(sum_u[u])) * kLn2 : kNegInf;
-            }
-            sum_u[u] = sum_u[u] > 0.0f ? 1.0f / sum_u[u] : 0.0f;
-          }
-#pragma unroll
-          for (int i = 0; i < kFloat4s; ++i) {
-            const int p = 32 * rt + E::out_row(lane, i);
-            if (p < n_packed)
-              store_out(static_cast<T*>(a.out) +
-                            (static_cast<size_t>(sq.row0 + r0 + p / group) * a.hq + head * group + p % group) * D +
-                            E::out_channel(lane, i),
-                        e.get(i) * sum_u[E::out_unit(i)]);
-          }
+          const int row = p / group;
+          const size_t at_row = static_cast<size_t>(sq.row0 + r0 + row) * a.hq + head * group + (p - row * group);
+          const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+          store_out(static_cast<T*>(a.out) + at_row * D + 4 * c, x * inv, y * inv);
+          if (a.lse != nullptr && c == 0) a.lse[at_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         } else {
-          const size_t base = piece_row(slice, which) + 32 * rt;
-#pragma unroll
-          for (int u = 0; u < E::kUnits; ++u) {
-            if (lane < 32 / E::kUnits) {
-              a.part_ml[2 * (base + E::row(lane, u))] = e.m[u];
-              a.part_ml[2 * (base + E::row(lane, u)) + 1] = sum_u[u];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < kFloat4s; ++i)
-            *reinterpret_cast<f32x4*>(a.part_o + (base + E::out_row(lane, i)) * D + E::out_channel(lane, i)) = e.get(i);
+          const size_t at_row = piece_row(slice, tok_lo == 0 ? 1 : 0) + p;
+          store_out(a.part_o + at_row * D + 4 * c, x, y);
+          if (c == 0) reinterpret_cast<float2*>(a.part_ml)[at_row] = make_float2(m, l);
         }
       }
+      if (ways > 1) __syncthreads();  // the slots are read
       if (!whole && tid == 0) {
         if (tok_lo > 0) {
           a.continues[slice] = 1;
@@ -1137,7 +1121,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           const int64_t tile_pos = pos - y0;
           int last = slice + 1;
           while (last + 1 < n_slices &&
-                 cut(total * (last + 1) / n_slices - tile_pos, tile_cost, sq.cost, end) < end)
+                 cut(line_cut(total, last + 1, n_slices) - tile_pos, tile_cost, sq.cost, end) < end)
             ++last;
           a.splits[slice] = ChunkSplit{sq.row0 + r0, head, n_packed, last};
         }
@@ -1147,19 +1131,18 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     pos = uniform(pos + y1 - y0);
     y0 = 0;
     if (pos >= stop) break;
-    if (++tile == sq.tiles) {
-      tile = 0;
+    if (++nth == sq.tiles) {
+      nth = 0;
       if (++head == a.hkv) {
         head = 0;
         // the next sequence with rows, 64 at a time
         int found = -1;
-        for (int i = seq + 1; found < 0; i += 64) {
+        for (int i = seq + 1; found < 0 && i < a.n_seqs; i += 64) {
           const bool has = i + lane < a.n_seqs && seq_of(a, i + lane).tiles > 0;
           const uint64_t bal = __ballot(has);
           if (bal != 0) found = i + __builtin_ctzll(bal);
-          else if (i + 64 >= a.n_seqs) break;  // not reached: the line ends with the last tile
         }
-        if (found < 0) break;
+        if (found < 0) break;  // not reached: the line ends with the last tile
         seq = uniform(found);
         sq = seq_uniform(a, seq);
       }
@@ -1172,7 +1155,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 template <typename T, int D>
 __global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {
   constexpr int PER = D / 64;
-  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.hq / a.hkv;
+  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.group;
   const ChunkSplit s = a.splits[slice];
   const int row_end = min(s.n_rows, 32 * (static_cast<int>(blockIdx.y) + 1));
   for (int p = 32 * blockIdx.y + (threadIdx.x >> 6); p < row_end; p += 4) {

@@ -33,7 +33,8 @@ struct ChunkArgs {
   float* lse;  // nullptr: not wanted
   int32_t num_blocks, max_blocks, n_seqs, n_rows;
   int32_t hq, hkv, head_dim, block_size, dtype;
-  float scale_log2;  // sm_scale * log2(e)
+  int32_t group, tile_rows;  // query heads per KV head, query rows of a tile (kChunkTileRows / group)
+  float scale_log2;          // sm_scale * log2(e)
   // workspace
   ChunkSplit* splits;   // [kChunkSlices]
   int32_t* continues;   // [kChunkSlices] 1: the slice holds a piece of a tile that began before it

@@ -204,6 +204,8 @@ int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, 
     a.n_rows = n_rows;
     a.hq = shape->hq;
     a.hkv = shape->hkv;
+    a.group = shape->hq / shape->hkv;
+    a.tile_rows = spork::kChunkTileRows / a.group;
     a.head_dim = shape->head_dim;
     a.block_size = shape->block_size;
     a.dtype = shape->dtype;
