@@ -145,8 +145,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 struct Pages {
   const int32_t* table;
   int last, num_blocks;
-  __device__ __forceinline__ int entry(int i) const {
-    return min(static_cast<uint32_t>(table[min(i, last)]), static_cast<uint32_t>(num_blocks - 1));
+  __device__ __forceinline__ int entry(int i) const { return table[min(i, last)]; }
+  // an entry as a block of the pools
+  __device__ __forceinline__ int block(int entry) const {
+    return static_cast<int>(min(static_cast<uint32_t>(entry), static_cast<uint32_t>(num_blocks - 1)));
   }
 };
 
@@ -184,12 +186,6 @@ __device__ __forceinline__ u32x4 lds_read_b128(uint32_t addr, int off) {
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(off) : "memory");
   return r;
 }
-__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr) {
-  uint32_t r;
-  asm volatile("ds_read_b32 %0, %1" : "=v"(r) : "v"(addr) : "memory");
-  return r;
-}
-__device__ __forceinline__ void lds_wait(uint32_t& r) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(r) : : "memory"); }
 __device__ __forceinline__ void lds_wait(u32x4& r, int keep) {
   asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(r) : "i"(keep) : "memory");
 }
@@ -274,13 +270,13 @@ struct Engine<__bf16, D, BS> {
 
   // K, or V, of the stage of the blocks `ent` (from their token `first`) into the
   // wave's slot.
-  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Bases& x, const int (&ent)[kBlocks], int head, int,
+  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[kBlocks], int head, int,
                                                  uint4* slot) {
     constexpr uint32_t kBytes = BS * D * 2;
     const char* from[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
-      from[b] = static_cast<const char*>(a.k_cache) + (static_cast<size_t>(uniform(ent[b])) * a.hkv + head) * kBytes;
+      from[b] = static_cast<const char*>(a.k_cache) + (static_cast<size_t>(pg.block(uniform(ent[b]))) * a.hkv + head) * kBytes;
     const uint32_t kl = anew(x.kload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {  // tokens tk .. of the stage
@@ -288,13 +284,13 @@ struct Engine<__bf16, D, BS> {
       load_lds<kStream>(from[tk / BS], kBytes, kl ^ (16u * kswz(tk)), 2 * (tk % BS) * D, slot + 64 * k);
     }
   }
-  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Bases& x, const int (&ent)[kBlocks], int head, int,
+  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[kBlocks], int head, int,
                                                  uint4* slot) {
     constexpr uint32_t kBytes = BS * D * 2;
     const char* from[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
-      from[b] = static_cast<const char*>(a.v_cache) + (static_cast<size_t>(uniform(ent[b])) * a.hkv + head) * kBytes;
+      from[b] = static_cast<const char*>(a.v_cache) + (static_cast<size_t>(pg.block(uniform(ent[b]))) * a.hkv + head) * kBytes;
     const uint32_t vl = anew(x.vload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {  // channels dk .. of a half, or of all 32 tokens
@@ -450,12 +446,12 @@ struct Engine<float, D, BS> {
   }
   static constexpr int kBlocks = 1;
 
-  static __device__ __forceinline__ const char* block(const ChunkArgs& a, const void* pool, int ent, int head) {
-    return static_cast<const char*>(pool) + (static_cast<size_t>(uniform(ent)) * a.hkv + head) * (BS * D * 4);
+  static __device__ __forceinline__ const char* block(const ChunkArgs& a, const Pages& pg, const void* pool, int ent, int head) {
+    return static_cast<const char*>(pool) + (static_cast<size_t>(pg.block(uniform(ent))) * a.hkv + head) * (BS * D * 4);
   }
-  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Bases& x, const int (&ent)[1], int head, int first,
+  static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[1], int head, int first,
                                                  uint4* slot) {
-    const char* from = block(a, a.k_cache, ent[0], head);
+    const char* from = block(a, pg, a.k_cache, ent[0], head);
     const uint32_t kl = anew(x.kload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
@@ -463,9 +459,9 @@ struct Engine<float, D, BS> {
       load_lds<kStream>(from, BS * D * 4, kl ^ (16u * kswz(tk)), 4 * (first + tk) * D, slot + 64 * k);
     }
   }
-  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Bases& x, const int (&ent)[1], int head, int first,
+  static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[1], int head, int first,
                                                  uint4* slot) {
-    const char* from = block(a, a.v_cache, ent[0], head);
+    const char* from = block(a, pg, a.v_cache, ent[0], head);
     const uint32_t vl = anew(x.vload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
@@ -559,7 +555,6 @@ struct Engine<float, D, BS> {
 constexpr int kStageChunks = 1024;   // 32 tokens x (K + V) x 128 channels x 2 bytes / 16
 constexpr int kRing = 8, kPer = 2;   // stages; stages that a barrier publishes
 constexpr int kAhead = kRing - kPer;
-constexpr int kTabEntries = 6912;    // of a segment: what LDS has left beside the ring
 constexpr int kStageLoads = 2;       // of a wave: the lower four load K, the upper four V
 
 __device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -573,22 +568,31 @@ struct Tile {
 
 // A wave's loads of the shared stages: instruction k of wave w fills chunks
 // (2w + k) * 64 + lane of a stage, from one block, at a scalar base plus the
-// lane's fixed offset.
+// lane's fixed offset. The table goes through registers: lane i holds entry i of
+// the window of 64 that the loads are in, and of the next one.
 template <int BS>
 struct RingLoader {
   using E = Engine<__bf16, 128, BS>;
+  static constexpr int kPerStage = 32 / BS;  // entries of a stage
+  static constexpr int kWindow = 64 / kPerStage;  // stages of a window
   const char* pool;
-  size_t head, hkv;
+  Pages pages;
+  int first;  // the tile's first entry
+  int64_t head, hkv;
   uint32_t off[kStageLoads];
-  uint32_t tab_base;  // LDS address of stage 0's table entry
-  int wave, last;
-  __device__ __forceinline__ void init(const ChunkArgs& a, int kv_head, int nstage, int wave_, int lane, const int* tab) {
+  int wave, lane, half;
+  int now, next;
+  __device__ __forceinline__ void init(const ChunkArgs& a, const Pages& pg, int kv_head, int tb0, int wave_, int lane_) {
     wave = wave_;
-    last = nstage - 1;
-    head = static_cast<size_t>(kv_head);
-    hkv = static_cast<size_t>(a.hkv);
+    lane = lane_;
+    pages = pg;
+    first = tb0 / BS;
+    head = kv_head;
+    hkv = a.hkv;
     pool = static_cast<const char*>(wave < 4 ? a.k_cache : a.v_cache);
-    tab_base = lds_addr(tab) + (BS == 16 && (wave & 2) != 0 ? 4u : 0u);
+    half = BS == 16 ? (wave >> 1) & 1 : 0;  // which block of a stage the wave loads
+    now = pages.entry(first + lane);
+    next = pages.entry(first + 64 + lane);
 #pragma unroll
     for (int k = 0; k < kStageLoads; ++k) {
       const int chunk = (kStageLoads * wave + k) * 64 + lane;
@@ -604,11 +608,14 @@ struct RingLoader {
       }
     }
   }
-  __device__ __forceinline__ uint32_t entry(int st) const {  // without a wait
-    return lds_read_b32(tab_base + (128u / BS) * static_cast<uint32_t>(min(st, last)));
+  // The window of stage st, which begins with it; windows are entered in order.
+  __device__ __forceinline__ void enter(int st) {
+    now = next;
+    next = pages.entry(first + (st + kWindow) * kPerStage + lane);
   }
-  __device__ __forceinline__ const char* base(uint32_t ent) const {
-    return pool + (static_cast<size_t>(uniform(static_cast<int>(ent))) * hkv + head) * (static_cast<size_t>(BS) * 256);
+  __device__ __forceinline__ const char* block(int st) const {
+    const int64_t e = pages.block(__builtin_amdgcn_readlane(now, st % kWindow * kPerStage + half));
+    return pool + (e * hkv + head) * (BS * 256);
   }
   __device__ __forceinline__ void load(const char* src, uint4* slot, int k) const {
     load_lds<0>(src, BS * 256, off[k], 0, slot + (kStageLoads * wave + k) * 64);
@@ -620,9 +627,8 @@ struct RingLoader {
 // done.
 template <int BS>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[kStageChunks],
-                                          int* tab, int tid, int wave, Engine<__bf16, 128, BS>& e) {
-  constexpr int kSegment = kTabEntries * BS - 4 * 32;  // tokens
-  const int lane = tid & 63, r32 = lane & 31, g = lane >> 5;
+                                          int lane, int wave, Engine<__bf16, 128, BS>& e) {
+  const int r32 = lane & 31, g = lane >> 5;
   const bool owns = wave * 32 < w.n_packed;
   const int hmin = uniform(wave_min_int(e.hz[0]));
   const float c = a.scale_log2, masked = c < 0.0f ? -kNegInf : kNegInf;
@@ -655,15 +661,12 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
     vr[i] = lds_read_b128(va, step * kCt);
   };
 
-  for (int tb0 = w.tok_lo; tb0 < w.tok_hi; tb0 += kSegment) {
-    const int tok_hi = min(w.tok_hi, tb0 + kSegment);
+  {
+    const int tb0 = w.tok_lo, tok_hi = w.tok_hi;
     const int nstage = (tok_hi - tb0 + 31) / 32;
-    barrier_lds();  // the last tile's, or segment's, reads of the ring and the table are done
-    const int ntab = (nstage * 32 + BS - 1) / BS;
-    for (int i = tid; i < ntab; i += 64 * kWaves) tab[i] = pg.entry(tb0 / BS + i);
     RingLoader<BS> ld;
-    ld.init(a, w.head, nstage, wave, lane, tab);
-    barrier_lds();
+    ld.init(a, pg, w.head, tb0, wave, lane);
+    barrier_lds();  // the last tile's reads of the ring are done
     // Stages from here on hold positions outside the range or past a row's last.
     const int inner = max(0, (min(tok_hi, hmin < INT_MAX ? hmin + 1 : INT_MAX) - tb0) / 32);
 
@@ -688,13 +691,13 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
           __builtin_bit_cast(bf16x8, x.vr[i]),
           __builtin_bit_cast(bf16x8, u32x4{x.pw[h], x.pw[h + 1], x.pw[h + 2], x.pw[h + 3]}), o[i & 3], 0, 0, 0);
     };
-    // The pair of stages a publish makes room for, loaded until the next one;
-    // the table entries of the pair after it are read one publish ahead. Behind
-    // the last stage these are loads of that stage again: so the number of loads
-    // in flight is always the same, and the loop needs no variant for its end.
+    // The pair of stages a publish makes room for, loaded until the next one.
+    // Behind the last stage these are loads of blocks that nothing reads: so the
+    // number of loads in flight is always the same (but for those of the table,
+    // which can only make a wait longer), and the loop needs no variant for its
+    // end.
     const char* src[kPer] = {nullptr, nullptr};
     int st_load = 0;
-    uint32_t ent[kPer];
     auto load = [&](int i) __attribute__((always_inline)) {
       ld.load(src[i / kStageLoads], smem[(st_load + i / kStageLoads) % kRing], i % kStageLoads);
     };
@@ -711,13 +714,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         wait_vmcnt<3 * kStageLoads>();
         barrier_only();
         st_load = st + kAhead;
+        if (st_load % RingLoader<BS>::kWindow == 0) ld.enter(st_load);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          lds_wait(ent[i]);
-          src[i] = ld.base(ent[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) ent[i] = ld.entry(st_load + kPer + i);
+        for (int i = 0; i < kPer; ++i) src[i] = ld.block(st_load + i);
       }
       if constexpr (!OWNS) {
         if constexpr (LOAD >= 0) {
@@ -743,14 +742,15 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         for (int t = 0; t < 16; ++t) {
           if (!FIRST && t < 8) pv_product(t, x);
           if (!LAST && t >= 8) {
-            // K operand t - 8, read in slot t - 8: all LDS reads but those issued
-            // after it, K t - 7 .. 7 and V max(0, t - 12) .. min(7, t - 5).
-            constexpr int kAfter[8] = {11, 11, 11, 11, 11, 9, 7, 5};
-            lds_wait(kr[t - 8], kAfter[t - 8]);
+            // K operand t - 8, read three slots ago: all LDS reads but those issued
+            // since. (Read as late as this, the operands of K and V fit the registers
+            // together.)
+            constexpr int kSince[8] = {4, 5, 5, 5, 5, 5, 4, 2};
+            lds_wait(kr[t - 8], kSince[t - 8]);
             score_product(x.sc, t - 8, kr);
           }
-          if (!LAST && t < 8) read_k(kr, t, k_off);
-          if (t >= 4 && t < 12) read_v(x.vr, t - 4, v_off);
+          if (!LAST && t >= 5 && t < 13) read_k(kr, t - 5, k_off);
+          if (t >= 6 && t < 14) read_v(x.vr, t - 6, v_off);
           if (LOAD >= 0 && t % 8 == 4) load(LOAD + t / 8);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -810,13 +810,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
     // point and two behind it.)
     auto prologue = [&](auto lo_c, auto hi_c) __attribute__((always_inline)) {
       constexpr int LO = decltype(lo_c)::value, N = decltype(hi_c)::value - LO;
-      uint32_t e0[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) e0[i] = ld.entry(LO + i);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        lds_wait(e0[i]);
-        const char* from = ld.base(e0[i]);
+        const char* from = ld.block(LO + i);
 #pragma unroll
         for (int k = 0; k < kStageLoads; ++k) ld.load(from, smem[LO + i], k);
       }
@@ -833,10 +829,6 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       constexpr std::integral_constant<int, -1> none{};
       constexpr std::integral_constant<int, 0> load0{};
       constexpr std::integral_constant<int, 2> load2{};
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) ent[i] = ld.entry(kAhead + i);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);
       State x;
       u32x4 kr[8];
       wait_vmcnt<(kAhead - 1) * kStageLoads>();
@@ -866,8 +858,6 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         stage(owns_c, no, yes, no, none, st + 1, x, kr);
       }
       wait_vmcnt<0>();
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) lds_wait(ent[i]);  // read ahead, maybe still in flight
     };
     if (owns) run(std::true_type{});
     else run(std::false_type{});
@@ -961,12 +951,11 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   constexpr int kFloat4s = D / 8;  // of a lane's accumulator
   constexpr bool kWide = std::is_same_v<T, __bf16> && D == 128;
   __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];  // a slot for each wave; wide: the ring
-  __shared__ __align__(16) int tab[kWide ? kTabEntries : 1];
   __shared__ float2 ml[kWaves][32];
   __shared__ int64_t wave_sum[kWaves];
   __shared__ Start start;
   static_assert(2 * E::kHalf >= kFloat4s * 64, "a wave's slot holds its accumulator");
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int tid = threadIdx.x, wave = uniform(tid >> 6);
   const int group = a.group;
   const int per_die = kChunkSlices / kDies;
   const int slice = static_cast<int>(blockIdx.x) % kDies * per_die + static_cast<int>(blockIdx.x) / kDies;
@@ -988,7 +977,10 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     // ---- one tile, or the slice's piece of it ----
     // All of this is the same in every lane; said to the compiler, it stays in
     // scalar registers (64-bit comparisons would move it to vector ones, and a
-    // load from a block there takes a loop over the lanes' addresses).
+    // load from a block there takes a loop over the lanes' addresses). A lane's
+    // addresses are computed anew for each tile: kept over tiles, those of both
+    // paths would fill the registers and spill.
+    const int lane = static_cast<int>(anew(tid & 63));
     seq = uniform(seq);
     head = uniform(head);
     nth = uniform(nth);
@@ -1020,8 +1012,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       if (!wide && works && first < tok_hi) {
         look_up(ent, first);
         look_up(ahead, first + stride);
-        E::issue_k(a, at, ent, head, first % BS, smem[wave]);
-        E::issue_v(a, at, ent, head, first % BS, smem[wave]);
+        E::issue_k(a, pg, at, ent, head, first % BS, smem[wave]);
+        E::issue_v(a, pg, at, ent, head, first % BS, smem[wave]);
       }
       int least = INT_MAX;
       const bool second = E::kUnits == 1 || n_packed - 32 * rt > 16;
@@ -1039,7 +1031,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const float c = a.scale_log2;
       if (wide) {
         if constexpr (kWide)
-          wide_tile<BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, tab, tid, wave, e);
+          wide_tile<BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, lane, wave, e);
         barrier_lds();  // the ring is read: a wave may load its slot for the next tile
       } else if (works) {
         // K and V of a stage are loaded as soon as the slot's halves have been read:
@@ -1056,12 +1048,12 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           for (int b = 0; b < E::kBlocks; ++b) ent[b] = ahead[b];
           look_up(ahead, tb + 2 * stride);
           asm volatile("" ::: "memory");
-          if (more) E::issue_k(a, at, ent, head, (tb + stride) % BS, smem[wave]);
+          if (more) E::issue_k(a, pg, at, ent, head, (tb + stride) % BS, smem[wave]);
           e.softmax(tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second);
           if (more) wait_vmcnt<E::kLoads>();
           else wait_vmcnt<0>();
           e.read_v(slot, at);
-          if (more) E::issue_v(a, at, ent, head, (tb + stride) % BS, smem[wave]);
+          if (more) E::issue_v(a, pg, at, ent, head, (tb + stride) % BS, smem[wave]);
           e.values(tb, tok_hi, lane, second);
         }
       }
