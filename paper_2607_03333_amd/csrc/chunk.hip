@@ -54,11 +54,17 @@ constexpr int kStream = 2;
 constexpr float kSlack = 8.0f;    // base-2 headroom before the reference moves
 constexpr float kSlackSum = 256.0f;
 
-// The line's unit is half the time that a token takes where HBM bounds it.
-constexpr int kTileCost = 512;      // a tile's start-up
+// The line's unit is half the time that a token of 128 bf16 channels takes where
+// HBM bounds it, about 9 ns on one compute unit.
+constexpr int kTileCost = 640;      // a tile's start-up and end
 constexpr int kMinSlice = 512;      // least length of a slice
 constexpr int kMinPiece = 64;       // tokens: a cut closer to a tile's end moves to it
-__device__ __forceinline__ int token_cost(int row_tiles) { return row_tiles <= 2 ? 2 : row_tiles <= 4 ? 3 : 4; }
+// A token, for tiles of so many row tiles: bf16 by bytes until the products weigh
+// more; fp32 products (64 flop per cycle and SIMD) weigh more from the first row tile.
+__device__ __forceinline__ int token_cost(const ChunkArgs& a, int row_tiles) {
+  if (a.dtype == 0) return (a.head_dim == 128 ? 4 : 2) * row_tiles;
+  return a.head_dim == 128 ? (row_tiles <= 2 ? 2 : row_tiles <= 4 ? 3 : 4) : row_tiles <= 2 ? 1 : 2;
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -107,7 +113,7 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off,
   s.kv = min(max(kv, 0), a.max_blocks * a.block_size);
   s.per = a.tile_rows;
   s.tiles = s.rows <= s.per ? s.rows > 0 : (s.rows + s.per - 1) / s.per;
-  s.cost = token_cost((min(s.rows, s.per) * a.group + 31) / 32);
+  s.cost = token_cost(a, (min(s.rows, s.per) * a.group + 31) / 32);
   s.head_cost = s.tiles <= 1 ? s.tiles * s.tile_cost(0) : s.first(s.tiles);
   return s;
 }
@@ -932,11 +938,14 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     if (head * s.head_cost > y0) --head;
     else if ((head + 1) * s.head_cost <= y0) ++head;
     y0 -= head * s.head_cost;
+    // The last tile that begins at or before y0: neighbours cost the same, so a
+    // division finds it, but where the last tile is part of one or tiles are blind.
     int nth = 0;
-    for (int hi = s.tiles; hi - nth > 1;) {  // the last tile that begins at or before y0
-      const int mid = (nth + hi) >> 1;
-      if (s.before(mid) <= y0) nth = mid;
-      else hi = mid;
+    if (s.tiles > 1) {
+      const double pair = static_cast<double>(s.tile_cost(0) + s.tile_cost(s.tiles - 1));
+      nth = min(2 * static_cast<int>(static_cast<double>(y0) / pair), s.tiles - 1);
+      while (s.before(nth) > y0) --nth;
+      while (nth + 1 < s.tiles && s.before(nth + 1) <= y0) ++nth;
     }
     if (nth > 0) y0 -= s.before(nth);
     *start = Start{i, s.row0, s.rows, s.kv, head, nth, y0};
@@ -1142,29 +1151,60 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   }
 }
 
-// Log-sum-exp merge of a split tile: a workgroup per (slice that begins one, 32
-// packed rows), a wave per row and 8 rows in turn, D / 64 channels a lane.
+// Log-sum-exp merge of a split tile: a wave per packed row, D / 64 channels a
+// lane. Lane i takes piece i's maximum and sum, so that all weights are there in
+// one round trip; the pieces' rows then come in eight at a time.
+constexpr int kMergeWaves = 4, kMergeRows = 8;  // of a workgroup; workgroups of a slice
+
 template <typename T, int D>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(ChunkArgs a) {
-  constexpr int PER = D / 64;
+__global__ void __launch_bounds__(64 * kMergeWaves) chunk_merge_kernel(ChunkArgs a) {
+  constexpr int PER = D / 64, kBatch = 8;
   const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.group;
   const ChunkSplit s = a.splits[slice];
-  const int row_end = min(s.n_rows, 32 * (static_cast<int>(blockIdx.y) + 1));
-  for (int p = 32 * blockIdx.y + (threadIdx.x >> 6); p < row_end; p += 4) {
+  const int pieces = s.last - slice + 1;
+  for (int p = blockIdx.y * kMergeWaves + (threadIdx.x >> 6); p < s.n_rows; p += kMergeRows * kMergeWaves) {
     float m = kNegInf, l = 0.0f, o[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) o[k] = 0.0f;
-    for (int v = slice; v <= s.last; ++v) {
-      if (v > slice && a.continues[v] == 0) continue;
-      const size_t row = piece_row(v, v == slice ? 1 : 0) + p;
-      const float pm = a.part_ml[2 * row], pl = a.part_ml[2 * row + 1], top = fmaxf(m, pm), ref = top == kNegInf ? 0.0f : top;
-      const float mine = exp2_fast(m - ref), theirs = exp2_fast(pm - ref);
+    for (int base = 0; base < pieces; base += 64) {
+      const int i = base + lane;
+      float2 x = make_float2(kNegInf, 0.0f);
+      if (i < pieces && (i == 0 || a.continues[slice + i] != 0))
+        x = reinterpret_cast<const float2*>(a.part_ml)[piece_row(slice + i, i == 0) + p];
+      float top = x.x;
 #pragma unroll
-      for (int k = 0; k < PER; ++k) o[k] = o[k] * mine + a.part_o[row * D + PER * lane + k] * theirs;
-      l = l * mine + pl * theirs;
+      for (int by = 32; by >= 1; by /= 2) top = fmaxf(top, __shfl_xor(top, by));
+      top = fmaxf(top, m);
+      const float ref = top == kNegInf ? 0.0f : top, mine = exp2_fast(m - ref), f = exp2_fast(x.x - ref);
+      float sum = x.y * f;
+#pragma unroll
+      for (int by = 32; by >= 1; by /= 2) sum += __shfl_xor(sum, by);
+      l = l * mine + sum;
       m = top;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) o[k] *= mine;
+      const int n = min(64, pieces - base);
+      for (int j = 0; j < n; j += kBatch) {
+        float w[kBatch], v[kBatch][PER];
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+          // a piece that is none, or whose rows see nothing, weighs nothing: any
+          // row that was written stands in for it
+          const int at = min(j + q, n - 1);
+          w[q] = j + q < n ? __shfl(f, at) : 0.0f;
+          const bool there = w[q] != 0.0f;
+          const float* row = a.part_o + (piece_row(there ? slice + base + at : slice, !there || base + at == 0) + p) * D + PER * lane;
+#pragma unroll
+          for (int k = 0; k < PER; ++k) v[q][k] = row[k];
+        }
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q)
+#pragma unroll
+          for (int k = 0; k < PER; ++k) o[k] += v[q][k] * w[q];
+      }
     }
-    const size_t out = static_cast<size_t>(s.row0 + p / group) * a.hq + s.head * group + p % group;
+    const int row = p / group;
+    const size_t out = static_cast<size_t>(s.row0 + row) * a.hq + s.head * group + (p - row * group);
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
     for (int k = 0; k < PER; ++k) static_cast<T*>(a.out)[out * D + PER * lane + k] = static_cast<T>(o[k] * inv);
@@ -1217,7 +1257,7 @@ hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t stream) {
 hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
   const ChunkKernel k = a.dtype == 1 ? pick_merge<__bf16>(a.head_dim) : pick_merge<float>(a.head_dim);
   if (k == nullptr) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k, dim3(kChunkSlices, kChunkTileRows / 32), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(k, dim3(kChunkSlices, kMergeRows), dim3(64 * kMergeWaves), 0, stream, a);
   return hipGetLastError();
 }
 
