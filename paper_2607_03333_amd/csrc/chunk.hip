@@ -59,11 +59,13 @@ constexpr float kSlackSum = 256.0f;
 constexpr int kTileCost = 640;      // a tile's start-up and end
 constexpr int kMinSlice = 512;      // least length of a slice
 constexpr int kMinPiece = 64;       // tokens: a cut closer to a tile's end moves to it
-// A token, for tiles of so many row tiles: bf16 by bytes until the products weigh
-// more; fp32 products (64 flop per cycle and SIMD) weigh more from the first row tile.
-__device__ __forceinline__ int token_cost(const ChunkArgs& a, int row_tiles) {
-  if (a.dtype == 0) return (a.head_dim == 128 ? 4 : 2) * row_tiles;
-  return a.head_dim == 128 ? (row_tiles <= 2 ? 2 : row_tiles <= 4 ? 3 : 4) : row_tiles <= 2 ? 1 : 2;
+// A token of a tile of `heads` KV heads with so many row tiles each: bf16 by
+// bytes until the products weigh more; fp32 products (64 flop per cycle and SIMD)
+// weigh more from the first row tile.
+__device__ __forceinline__ int token_cost(const ChunkArgs& a, int row_tiles, int heads) {
+  const int wide = a.head_dim == 128 ? 2 : 1;
+  if (a.dtype == 0) return 2 * wide * row_tiles * heads;
+  return wide * max(heads, row_tiles <= 2 ? 1 : 2);
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -80,9 +82,10 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 struct Seq {
   int row0, rows, kv;
   int per;    // query rows of a tile
-  int tiles;  // per KV head
+  int tiles;  // per group of KV heads
+  int heads, groups;  // KV heads of a tile, and how many such groups there are
   int cost;   // of a token
-  int64_t head_cost;
+  int64_t group_cost;
   // positions that tile j sees
   __device__ __forceinline__ int end(int j) const { return max(0, kv - rows + min(rows, (j + 1) * per)); }
   __device__ __forceinline__ int64_t tile_cost(int j) const { return kTileCost + static_cast<int64_t>(end(j)) * cost; }
@@ -101,7 +104,7 @@ struct Seq {
   // the k-th tile on the line, and the cost of those before it
   __device__ __forceinline__ int at(int k) const { return k & 1 ? tiles - 1 - (k >> 1) : k >> 1; }
   __device__ __forceinline__ int64_t before(int k) const {
-    return first((k + 1) >> 1) + head_cost - first(tiles - (k >> 1));
+    return first((k + 1) >> 1) + group_cost - first(tiles - (k >> 1));
   }
 };
 
@@ -113,8 +116,11 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off,
   s.kv = min(max(kv, 0), a.max_blocks * a.block_size);
   s.per = a.tile_rows;
   s.tiles = s.rows <= s.per ? s.rows > 0 : (s.rows + s.per - 1) / s.per;
-  s.cost = token_cost(a, (min(s.rows, s.per) * a.group + 31) / 32);
-  s.head_cost = s.tiles <= 1 ? s.tiles * s.tile_cost(0) : s.first(s.tiles);
+  const int row_tiles = (min(s.rows, s.per) * a.group + 31) / 32;
+  s.heads = s.tiles == 1 ? min(a.most_heads, kWaves / row_tiles) : 1;
+  s.groups = (a.hkv + s.heads - 1) / s.heads;
+  s.cost = token_cost(a, row_tiles, s.heads);
+  s.group_cost = s.tiles <= 1 ? s.tiles * s.tile_cost(0) : s.first(s.tiles);
   return s;
 }
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
@@ -886,7 +892,7 @@ __device__ __forceinline__ size_t piece_row(int slice, int which) {
 
 // Where a slice begins.
 struct Start {
-  int seq, row0, rows, kv, head, nth;
+  int seq, row0, rows, kv, group, nth;
   int64_t y0;
 };
 
@@ -900,7 +906,7 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
   Seq s;
   for (int i = i0; i < i1; ++i) {
     s = seq_of(a, i);
-    sum += s.head_cost;
+    sum += s.group_cost * s.groups;
   }
   int64_t upto = sum;
 #pragma unroll
@@ -916,8 +922,7 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     if (w < wave) upto += wave_sum[w];
     total += wave_sum[w];
   }
-  // (a sequence's KV heads lie side by side: the line is hkv times the sum)
-  total = uniform(total) * a.hkv;
+  total = uniform(total);
   const int n = static_cast<int>(min(max(total / kMinSlice, static_cast<int64_t>(1)), static_cast<int64_t>(kChunkSlices)));
   *n_slices = n;
   *total_out = total;
@@ -925,19 +930,22 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
   const int64_t pos = line_cut(total, slice, n);
   *pos_out = pos;
   *stop_out = line_cut(total, slice + 1, n);
-  int64_t at = (upto - sum) * a.hkv;
-  if (pos >= at && pos < upto * a.hkv) {
+  int64_t at = upto - sum;
+  if (pos >= at && pos < upto) {
     int i = i0;
     for (; i1 - i0 > 1; ++i) {
       s = seq_of(a, i);
-      if (pos < at + s.head_cost * a.hkv) break;
-      at += s.head_cost * a.hkv;
+      if (pos < at + s.group_cost * s.groups) break;
+      at += s.group_cost * s.groups;
     }
     int64_t y0 = pos - at;
-    int head = static_cast<int>(static_cast<double>(y0) / static_cast<double>(s.head_cost));
-    if (head * s.head_cost > y0) --head;
-    else if ((head + 1) * s.head_cost <= y0) ++head;
-    y0 -= head * s.head_cost;
+    int group = 0;
+    if (y0 >= s.group_cost) {
+      group = static_cast<int>(static_cast<double>(y0) / static_cast<double>(s.group_cost));
+      if (group * s.group_cost > y0) --group;
+      else if ((group + 1) * s.group_cost <= y0) ++group;
+      y0 -= group * s.group_cost;
+    }
     // The last tile that begins at or before y0: neighbours cost the same, so a
     // division finds it, but where the last tile is part of one or tiles are blind.
     int nth = 0;
@@ -948,7 +956,7 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
       while (nth + 1 < s.tiles && s.before(nth + 1) <= y0) ++nth;
     }
     if (nth > 0) y0 -= s.before(nth);
-    *start = Start{i, s.row0, s.rows, s.kv, head, nth, y0};
+    *start = Start{i, s.row0, s.rows, s.kv, group, nth, y0};
   }
   __syncthreads();
   return true;
@@ -965,7 +973,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   __shared__ Start start;
   static_assert(2 * E::kHalf >= kFloat4s * 64, "a wave's slot holds its accumulator");
   const int tid = threadIdx.x, wave = uniform(tid >> 6);
-  const int group = a.group;
+  const int group = a.group;  // query heads of a KV head
   const int per_die = kChunkSlices / kDies;
   const int slice = static_cast<int>(blockIdx.x) % kDies * per_die + static_cast<int>(blockIdx.x) / kDies;
   if (tid == 0) {
@@ -975,7 +983,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   int n_slices;
   int64_t total, pos, stop;
   if (!find_slice(a, slice, tid, wave_sum, &start, &n_slices, &total, &pos, &stop)) return;
-  int seq = start.seq, head = start.head, nth = start.nth;
+  int seq = start.seq, head_group = start.group, nth = start.nth;
   int64_t y0 = start.y0;
   Seq sq;
   sq.row0 = start.row0;
@@ -991,7 +999,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     // paths would fill the registers and spill.
     const int lane = static_cast<int>(anew(tid & 63));
     seq = uniform(seq);
-    head = uniform(head);
+    head_group = uniform(head_group);
     nth = uniform(nth);
     y0 = uniform(y0);
     pos = uniform(pos);
@@ -1004,8 +1012,12 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     if (tok_hi > tok_lo || (end == 0 && y0 == 0)) {
       const int r0 = tile * sq.per;  // first query row of the tile, in the sequence
       const int n_packed = min(sq.per, sq.rows - r0) * group;
-      const int row_tiles = (n_packed + 31) / 32, ways = max(1, kWaves / row_tiles);
-      const int rt = wave % row_tiles, way = wave / row_tiles;
+      const int row_tiles = (n_packed + 31) / 32;
+      const int head0 = head_group * sq.heads, heads = min(sq.heads, a.hkv - head0);
+      // a wave's unit (KV head and row tile), and its share of the tokens
+      const int units = row_tiles * heads, ways = max(1, kWaves / units);
+      const int unit = wave % units, way = wave / units;
+      const int head = head0 + unit / row_tiles, rt = unit % row_tiles;
       const bool works = way < ways;  // wide: every wave loads, those with a row tile compute
       E e;
       e.clear();
@@ -1084,47 +1096,59 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       }
       if (ways > 1) __syncthreads();
       const bool whole = tok_lo == 0 && tok_hi == end;
-      const int passes = ways > 1 ? row_tiles * kPasses / kWaves + (row_tiles * kPasses % kWaves != 0) : works ? kPasses : 0;
-      for (int k = 0; k < passes; ++k) {
-        const int id = (ways > 1 ? wave : rt) * passes + k, tr = id / kPasses, r = id % kPasses * kRows + lane / kLanesPerRow;
-        const int p = 32 * tr + r, c = 2 * (lane % kLanesPerRow);
-        if (p >= n_packed) continue;
-        float m = kNegInf, l = 0.0f;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-        for (int v = 0; v < ways; ++v) m = fmaxf(m, ml[v * row_tiles + tr][r].x);
-        const float ref = m == kNegInf ? 0.0f : m;
-        for (int v = 0; v < ways; ++v) {
-          const int w = v * row_tiles + tr;
-          const float f = exp2_fast(ml[w][r].x - ref);
-          l += ml[w][r].y * f;
-          x += *chunk_at(w, r, c) * f;
-          y += *chunk_at(w, r, c + 1) * f;
+      // Rows id * kRows .. of the units, of the sums of the waves that had them.
+      auto finish = [&](int id, int ways_) __attribute__((always_inline)) {
+        const int tr = id / kPasses, r = id % kPasses * kRows + lane / kLanesPerRow;
+        const int p = tr % row_tiles * 32 + r, c = 2 * (lane % kLanesPerRow);
+        if (tr >= units || p >= n_packed) return;
+        float2 s = ml[tr][r];
+        float m = s.x, l = s.y;
+        f32x4 x = *chunk_at(tr, r, c), y = *chunk_at(tr, r, c + 1);
+        if (ways_ > 1) {
+          for (int v = 1; v < ways_; ++v) m = fmaxf(m, ml[v * units + tr][r].x);
+          const float ref = m == kNegInf ? 0.0f : m, f = exp2_fast(s.x - ref);
+          l *= f;
+          x *= f;
+          y *= f;
+          for (int v = 1; v < ways_; ++v) {
+            const int w = v * units + tr;
+            s = ml[w][r];
+            const float g = exp2_fast(s.x - ref);
+            l += s.y * g;
+            x += *chunk_at(w, r, c) * g;
+            y += *chunk_at(w, r, c + 1) * g;
+          }
         }
         if (whole) {
           const int row = p / group;
-          const size_t at_row = static_cast<size_t>(sq.row0 + r0 + row) * a.hq + head * group + (p - row * group);
+          const size_t at_row =
+              static_cast<size_t>(sq.row0 + r0 + row) * a.hq + (head0 + tr / row_tiles) * group + (p - row * group);
           const float inv = l > 0.0f ? 1.0f / l : 0.0f;
           store_out(static_cast<T*>(a.out) + at_row * D + 4 * c, x * inv, y * inv);
           if (a.lse != nullptr && c == 0) a.lse[at_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         } else {
-          const size_t at_row = piece_row(slice, tok_lo == 0 ? 1 : 0) + p;
+          const size_t at_row = piece_row(slice, tok_lo == 0 ? 1 : 0) + 32 * tr + r;
           store_out(a.part_o + at_row * D + 4 * c, x, y);
           if (c == 0) reinterpret_cast<float2*>(a.part_ml)[at_row] = make_float2(m, l);
         }
+      };
+      if (ways > 1) {
+        for (int id = wave; id < units * kPasses; id += kWaves) finish(id, ways);
+      } else if (works) {
+#pragma unroll 4
+        for (int k = 0; k < kPasses; ++k) finish(unit * kPasses + k, 1);
       }
       if (ways > 1) __syncthreads();  // the slots are read
       if (!whole && tid == 0) {
         if (tok_lo > 0) {
           a.continues[slice] = 1;
         } else {
-          // the slice that holds the tile's last token: of the line's cuts, the
-          // first at or behind which the tile's cut is its end
-          const int64_t tile_pos = pos - y0;
-          int last = slice + 1;
-          while (last + 1 < n_slices &&
-                 cut(line_cut(total, last + 1, n_slices) - tile_pos, tile_cost, sq.cost, end) < end)
-            ++last;
-          a.splits[slice] = ChunkSplit{sq.row0 + r0, head, n_packed, last};
+          // the last slice that begins inside the tile
+          const int64_t tile_end = pos - y0 + tile_cost;
+          int last = min(static_cast<int>(static_cast<double>(tile_end) / static_cast<double>(total) * n_slices), n_slices - 1);
+          while (line_cut(total, last, n_slices) >= tile_end) --last;
+          while (last + 1 < n_slices && line_cut(total, last + 1, n_slices) < tile_end) ++last;
+          a.splits[slice] = ChunkSplit{sq.row0 + r0, head0, n_packed, row_tiles, heads, last};
         }
       }
     }
@@ -1134,8 +1158,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
     if (pos >= stop) break;
     if (++nth == sq.tiles) {
       nth = 0;
-      if (++head == a.hkv) {
-        head = 0;
+      if (++head_group == sq.groups) {
+        head_group = 0;
         // the next sequence with rows, 64 at a time
         int found = -1;
         for (int i = seq + 1; found < 0 && i < a.n_seqs; i += 64) {
@@ -1151,64 +1175,72 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   }
 }
 
-// Log-sum-exp merge of a split tile: a wave per packed row, D / 64 channels a
-// lane. Lane i takes piece i's maximum and sum, so that all weights are there in
-// one round trip; the pieces' rows then come in eight at a time.
-constexpr int kMergeWaves = 4, kMergeRows = 8;  // of a workgroup; workgroups of a slice
+// Log-sum-exp merge of a split tile: D / 4 lanes per packed row, four channels a
+// lane. Lane i of a row takes the maximum and sum of pieces i, i + D / 4, ..., so
+// that the weights are there in one round trip; the pieces' rows then come in
+// sixteen at a time (four, where there are no more).
+constexpr int kMergeWaves = 4, kMergeGroups = 8;  // of a workgroup; workgroups of a slice
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kMergeWaves) chunk_merge_kernel(ChunkArgs a) {
-  constexpr int PER = D / 64, kBatch = 8;
-  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.group;
+  constexpr int LPR = D / 4, kRows = 64 / LPR;
+  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.group, sub = lane % LPR;
   const ChunkSplit s = a.splits[slice];
-  const int pieces = s.last - slice + 1;
-  for (int p = blockIdx.y * kMergeWaves + (threadIdx.x >> 6); p < s.n_rows; p += kMergeRows * kMergeWaves) {
-    float m = kNegInf, l = 0.0f, o[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) o[k] = 0.0f;
-    for (int base = 0; base < pieces; base += 64) {
-      const int i = base + lane;
+  const int pieces = s.last - slice + 1, rows = s.n_rows * s.heads;
+  // (the lanes of a wave stay together: rows past the last are computed again)
+  for (int i0 = (blockIdx.y * kMergeWaves + (threadIdx.x >> 6)) * kRows; i0 < rows; i0 += kMergeGroups * kMergeWaves * kRows) {
+    const int at = min(i0 + lane / LPR, rows - 1), head = at / s.n_rows, p = at - head * s.n_rows;
+    const int in_tile = head * s.row_tiles * 32 + p;
+    float m = kNegInf, l = 0.0f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int base = 0; base < pieces; base += LPR) {
+      const int i = base + sub;
       float2 x = make_float2(kNegInf, 0.0f);
       if (i < pieces && (i == 0 || a.continues[slice + i] != 0))
-        x = reinterpret_cast<const float2*>(a.part_ml)[piece_row(slice + i, i == 0) + p];
+        x = reinterpret_cast<const float2*>(a.part_ml)[piece_row(slice + i, i == 0) + in_tile];
       float top = x.x;
 #pragma unroll
-      for (int by = 32; by >= 1; by /= 2) top = fmaxf(top, __shfl_xor(top, by));
+      for (int by = LPR / 2; by >= 1; by /= 2) top = fmaxf(top, __shfl_xor(top, by));
       top = fmaxf(top, m);
       const float ref = top == kNegInf ? 0.0f : top, mine = exp2_fast(m - ref), f = exp2_fast(x.x - ref);
       float sum = x.y * f;
 #pragma unroll
-      for (int by = 32; by >= 1; by /= 2) sum += __shfl_xor(sum, by);
+      for (int by = LPR / 2; by >= 1; by /= 2) sum += __shfl_xor(sum, by);
       l = l * mine + sum;
       m = top;
+      o *= mine;
+      const int n = min(LPR, pieces - base);
+      auto rows_of = [&](auto batch_c) __attribute__((always_inline)) {
+        constexpr int kBatch = decltype(batch_c)::value;
+        for (int j = 0; j < n; j += kBatch) {
+          float w[kBatch];
+          f32x4 v[kBatch];
 #pragma unroll
-      for (int k = 0; k < PER; ++k) o[k] *= mine;
-      const int n = min(64, pieces - base);
-      for (int j = 0; j < n; j += kBatch) {
-        float w[kBatch], v[kBatch][PER];
+          for (int q = 0; q < kBatch; ++q) {
+            // a piece that is none, or whose rows see nothing, weighs nothing: the
+            // first one's row stands in for it
+            const int k = min(j + q, n - 1);
+            w[q] = __shfl(f, lane - sub + k);
+            if (j + q >= n) w[q] = 0.0f;
+            const bool there = w[q] != 0.0f;
+            v[q] = *reinterpret_cast<const f32x4*>(
+                a.part_o + (piece_row(there ? slice + base + k : slice, !there || base + k == 0) + in_tile) * D + 4 * sub);
+          }
 #pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-          // a piece that is none, or whose rows see nothing, weighs nothing: any
-          // row that was written stands in for it
-          const int at = min(j + q, n - 1);
-          w[q] = j + q < n ? __shfl(f, at) : 0.0f;
-          const bool there = w[q] != 0.0f;
-          const float* row = a.part_o + (piece_row(there ? slice + base + at : slice, !there || base + at == 0) + p) * D + PER * lane;
-#pragma unroll
-          for (int k = 0; k < PER; ++k) v[q][k] = row[k];
+          for (int q = 0; q < kBatch; ++q) o += v[q] * w[q];
         }
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q)
-#pragma unroll
-          for (int k = 0; k < PER; ++k) o[k] += v[q][k] * w[q];
-      }
+      };
+      if (n <= 4) rows_of(std::integral_constant<int, 4>{});
+      else rows_of(std::integral_constant<int, 16>{});
     }
     const int row = p / group;
-    const size_t out = static_cast<size_t>(s.row0 + row) * a.hq + s.head * group + (p - row * group);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) static_cast<T*>(a.out)[out * D + PER * lane + k] = static_cast<T>(o[k] * inv);
-    if (a.lse != nullptr && lane == 0) a.lse[out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+    const size_t out = static_cast<size_t>(s.row0 + row) * a.hq + (s.head + head) * group + (p - row * group);
+    o *= l > 0.0f ? 1.0f / l : 0.0f;
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + out * D + 4 * sub) = o;
+    else
+      *reinterpret_cast<uint2*>(static_cast<__bf16*>(a.out) + out * D + 4 * sub) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+    if (a.lse != nullptr && sub == 0) a.lse[out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
   }
 }
 
@@ -1228,6 +1260,12 @@ ChunkKernel pick_merge(int d) {
 }
 
 }  // namespace
+
+int32_t chunk_tile_heads(int32_t n_seqs, int32_t hkv) {
+  int32_t n = 1;
+  while (2 * n <= hkv && 2 * n <= kWaves && static_cast<int64_t>(n_seqs) * hkv >= 2ll * n * kChunkSlices) n *= 2;
+  return n;
+}
 
 bool chunk_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
   return (dtype == 0 || dtype == 1) && (head_dim == 64 || head_dim == 128) && (block_size == 16 || block_size == 32);
@@ -1257,7 +1295,7 @@ hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t stream) {
 hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
   const ChunkKernel k = a.dtype == 1 ? pick_merge<__bf16>(a.head_dim) : pick_merge<float>(a.head_dim);
   if (k == nullptr) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k, dim3(kChunkSlices, kMergeRows), dim3(64 * kMergeWaves), 0, stream, a);
+  hipLaunchKernelGGL(k, dim3(kChunkSlices, kMergeGroups), dim3(64 * kMergeWaves), 0, stream, a);
   return hipGetLastError();
 }
 

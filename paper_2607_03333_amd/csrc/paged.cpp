@@ -206,6 +206,7 @@ int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, 
     a.hkv = shape->hkv;
     a.group = shape->hq / shape->hkv;
     a.tile_rows = spork::kChunkTileRows / a.group;
+    a.most_heads = spork::chunk_tile_heads(n_seqs, shape->hkv);
     a.head_dim = shape->head_dim;
     a.block_size = shape->block_size;
     a.dtype = shape->dtype;

@@ -383,7 +383,7 @@ def spork_ngram_propose(tokens, seq_off, n_seqs, max_len, n_min, n_max, k, draft
 
 # ---- steps whose lengths live on the GPU --------------------------------------
 def _bytes(workspace):
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return 0 if workspace is None else workspace.nbytes
 
 
 def _want(name, x, size, *shape):

@@ -15,6 +15,7 @@ hipError_t launch_kv_copy_batch(int32_t, int32_t, int32_t, int32_t, int32_t, voi
                                 hipStream_t) {
   return hipErrorNoDevice;
 }
+int32_t chunk_tile_heads(int32_t, int32_t) { return 1; }
 bool chunk_supported(int32_t dtype, int32_t d, int32_t bs) {
   return (dtype == 0 || dtype == 1) && (d == 64 || d == 128) && (bs == 16 || bs == 32);
 }
