@@ -38,6 +38,7 @@
 // and accumulators are fp32.
 #include "chunk_kernels.h"
 #include "device_common.h"
+#include "wave_scan.h"
 
 namespace spork {
 namespace {
@@ -908,12 +909,7 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     s = seq_of(a, i);
     sum += s.group_cost * s.groups;
   }
-  int64_t upto = sum;
-#pragma unroll
-  for (int by = 1; by < 64; by *= 2) {
-    const int64_t y = __shfl_up(upto, by);
-    if (lane >= by) upto += y;
-  }
+  int64_t upto = wave_scan(sum);
   if (lane == 63) wave_sum[wave] = upto;
   __syncthreads();
   int64_t total = 0;

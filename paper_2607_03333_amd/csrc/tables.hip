@@ -20,21 +20,23 @@
 // and last places go through atomics whose order does not matter (sums, maxima),
 // so the same step gives the same tables every time.
 //
-// Four launches: count (references and last places), decide (what each row frees
-// and takes, their sums, and whether the step fits), release (frees into the
+// Five launches: count (references and last places), rows (what each row frees and
+// takes), sum (over the rows, and whether the step fits), release (frees into the
 // queue, forked rows, copies), assign (fronts into the tables, slots). The
-// references are changed while they are counted, and changed back where decide
-// refuses the step.
+// references are changed while they are counted, and changed back where the step
+// is refused. A workgroup per row but in sum, and four entries of its row in
+// flight per thread: a fork or the end of a long row is thousands of entries.
 #include "device_common.h"
 #include "spork.h"
 #include "tables_kernels.h"
+#include "wave_scan.h"
 
 namespace spork {
 namespace {
 
-constexpr int kRowThreads = 256;      // of a row's workgroup in count, release and assign
-constexpr int kDecideThreads = 1024;  // a wave per row
-constexpr int kDecideRows = kDecideThreads / 64;
+constexpr int kRowThreads = 256;   // of a row's workgroup
+constexpr int kSumThreads = 1024;  // of the one workgroup that sums the rows
+constexpr int kAtOnce = 4;         // entries of a row that a thread loads together
 
 struct Row {
   int len, grow, parent, held;
@@ -82,50 +84,90 @@ __device__ __forceinline__ int shared_tail(const TablesArgs& a, const Row& r) {
   return a.table[place(a, r.from, r.len / a.block_size)];
 }
 
+// f(column, entry) for the columns [lo, hi) of table row s, each by one thread.
+template <typename F>
+__device__ __forceinline__ void each_entry(const TablesArgs& a, int s, int lo, int hi, F f) {
+  for (int j0 = lo + static_cast<int>(threadIdx.x); j0 < hi; j0 += kAtOnce * kRowThreads) {
+    int b[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) b[q] = j0 + q * kRowThreads < hi ? a.table[place(a, s, j0 + q * kRowThreads)] : -1;
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q)
+      if (j0 + q * kRowThreads < hi) f(j0 + q * kRowThreads, b[q]);
+  }
+}
+
 __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
-  const int s = blockIdx.x, tid = threadIdx.x;
+  const int s = blockIdx.x;
   Row r;
   int err = read_row(a, s, &r);
   if (err == SPORK_OK) {
-    if (r.parent >= 0) {
-      for (int j = tid; j < r.keep; j += kRowThreads) {
-        const int b = a.table[place(a, r.parent, j)];
+    if (r.parent >= 0)
+      each_entry(a, r.parent, 0, r.keep, [&](int, int b) {
         if (in_pool(a, b)) atomicAdd(a.refcount + b, 1);
         else err = SPORK_E_INVAL;
-      }
-    }
-    for (int j = r.release_lo + tid; j < r.held; j += kRowThreads) {
-      const int b = a.table[place(a, s, j)];
+      });
+    each_entry(a, s, r.release_lo, r.held, [&](int j, int b) {
       if (in_pool(a, b)) {
         atomicAdd(a.refcount + b, -1);
         atomicMax(a.last_release + b, static_cast<int>(place(a, s, j)) + 1);
       } else {
         err = SPORK_E_INVAL;
       }
-    }
-    if (tid == 0) {
+    });
+    if (threadIdx.x == 0 && r.grow != 0 && r.len % a.block_size != 0) {
       const int b = shared_tail(a, r);
-      if (b != -1 || (r.grow != 0 && r.len % a.block_size != 0)) {
-        if (in_pool(a, b)) {
-          atomicAdd(a.sharers + b, 1);
-          atomicMax(a.last_sharer + b, s + 1);
-        } else {
-          err = SPORK_E_INVAL;
-        }
+      if (in_pool(a, b)) {
+        atomicAdd(a.sharers + b, 1);
+        atomicMax(a.last_sharer + b, s + 1);
+      } else {
+        err = SPORK_E_INVAL;
       }
     }
   }
   if (err != SPORK_OK) atomicMin(&a.totals->error, err);
 }
 
-__device__ __forceinline__ int agent_load(const int32_t* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void agent_store(int32_t* p, int x) {
-  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Whether place (s, j) is the one that frees block b.
+__device__ __forceinline__ bool frees_block(const TablesArgs& a, int s, int j, int b) {
+  return in_pool(a, b) && a.last_release[b] == static_cast<int>(place(a, s, j)) + 1 && a.refcount[b] == 0;
 }
 
-// Inclusive sum over the workgroup's threads of four numbers at once.
+__global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
+  __shared__ int freed[kRowThreads / 64];
+  const int s = blockIdx.x, tid = threadIdx.x;
+  Row r;
+  if (read_row(a, s, &r) != SPORK_OK) {  // the step is refused
+    if (tid == 0) a.frees[s] = a.takes[s] = a.copy_off[s] = 0;
+    return;
+  }
+  int copies = 0;
+  if (tid == 0) {
+    const int b = shared_tail(a, r);
+    if (in_pool(a, b)) {
+      const int refs = a.refcount[b];
+      copies = refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
+    }
+  }
+  int frees = 0;
+  if (r.release_lo < r.held) {
+    each_entry(a, s, r.release_lo, r.held, [&](int j, int b) { frees += frees_block(a, s, j, b); });
+#pragma unroll
+    for (int o = 32; o >= 1; o /= 2) frees += __shfl_xor(frees, o);
+    if ((tid & 63) == 0) freed[tid >> 6] = frees;
+    __syncthreads();
+    frees = 0;
+#pragma unroll
+    for (int w = 0; w < kRowThreads / 64; ++w) frees += freed[w];
+  }
+  if (tid == 0) {
+    a.frees[s] = frees;
+    a.takes[s] = copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
+    a.copy_off[s] = copies;
+  }
+}
+
+// What a row adds to the sums.
 struct Sums {
   int64_t tokens;
   int frees, takes, copies;
@@ -133,82 +175,36 @@ struct Sums {
 __device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) {
   return {x.tokens + y.tokens, x.frees + y.frees, x.takes + y.takes, x.copies + y.copies};
 }
-__device__ __forceinline__ Sums shifted(const Sums& x, int by) {
-  return {__shfl_up(x.tokens, by), __shfl_up(x.frees, by), __shfl_up(x.takes, by), __shfl_up(x.copies, by)};
-}
-__device__ __forceinline__ Sums block_scan(Sums x, Sums* wave_sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int by = 1; by < 64; by *= 2) {
-    const Sums y = shifted(x, by);
-    if (lane >= by) x = x + y;
-  }
-  __syncthreads();
-  if (lane == 63) wave_sums[wave] = x;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) x = x + wave_sums[w];
-  return x;
-}
 
-__global__ void __launch_bounds__(kDecideThreads) tables_decide(TablesArgs a) {
-  __shared__ Sums wave_sums[kDecideRows];
-  __shared__ Sums done;
-  __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int s = blockIdx.x * kDecideRows + (tid >> 6);
-  if (s < a.n_seqs) {
-    Row r;
-    int frees = 0, takes = 0, copies = 0;
-    if (read_row(a, s, &r) == SPORK_OK) {
-      for (int j0 = r.release_lo; j0 < r.held; j0 += 64) {
-        const int j = j0 + lane;
-        bool free_here = false;
-        if (j < r.held) {
-          const int b = a.table[place(a, s, j)];
-          free_here = in_pool(a, b) && a.last_release[b] == static_cast<int>(place(a, s, j)) + 1 && a.refcount[b] == 0;
-        }
-        frees += __popcll(__ballot(free_here));
-      }
-      const int b = shared_tail(a, r);
-      if (b >= 0 && b < a.num_blocks) {
-        const int refs = a.refcount[b];
-        copies = refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
-      }
-      takes = copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
-    }
-    if (lane == 0) {
-      agent_store(a.frees + s, frees);
-      agent_store(a.takes + s, takes);
-      agent_store(a.copy_off + s, copies);
-    }
-  }
-  // The last workgroup to get here has every row's numbers to sum.
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) last = atomicAdd(&a.totals->arrived, 1) == static_cast<int>(gridDim.x) - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  if (tid == 0) done = Sums{0, 0, 0, 0};
-  __syncthreads();
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kDecideThreads) {
+__global__ void __launch_bounds__(kSumThreads) tables_sum(TablesArgs a) {
+  constexpr int kWaves = kSumThreads / 64;
+  __shared__ Sums wave_sums[2][kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int front = a.queue[0], count = a.queue[1];
+  int status = a.totals->error;
+  Sums done{0, 0, 0, 0};
+  for (int s0 = 0, odd = 0; s0 < a.n_seqs; s0 += kSumThreads, odd ^= 1) {
     const int i = s0 + tid;
     Sums x{0, 0, 0, 0};
-    if (i < a.n_seqs) x = {max(a.n_new[i], 0), agent_load(a.frees + i), agent_load(a.takes + i), agent_load(a.copy_off + i)};
-    const Sums base = done, upto = base + block_scan(x, wave_sums);
+    if (i < a.n_seqs) x = {max(a.n_new[i], 0), a.frees[i], a.takes[i], a.copy_off[i]};
+    Sums upto{wave_scan(x.tokens), wave_scan(x.frees), wave_scan(x.takes), wave_scan(x.copies)};
+    if (lane == 63) wave_sums[odd][wave] = upto;
+    __syncthreads();  // (the other half is free again once everybody is here)
+    upto = upto + done;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const Sums y = wave_sums[odd][w];
+      if (w < wave) upto = upto + y;
+      done = done + y;
+    }
     if (i < a.n_seqs) {
       a.frees[i] = upto.frees - x.frees;
       a.takes[i] = upto.takes - x.takes;
       a.copy_off[i] = x.copies ? upto.copies - 1 : -1 - upto.copies;
       a.row_off[i + 1] = static_cast<int>(min(upto.tokens, static_cast<int64_t>(INT_MAX)));
     }
-    __syncthreads();
-    if (tid == kDecideThreads - 1) done = upto;
-    __syncthreads();
   }
   if (tid != 0) return;
-  const int front = a.queue[0], count = a.queue[1];
-  int status = agent_load(&a.totals->error);
   if (front < 0 || front >= a.num_blocks || count < 0 || count > a.num_blocks - done.frees) status = min(status, SPORK_E_INVAL);
   if (done.tokens > a.max_tokens) status = min(status, SPORK_E_CAPACITY);
   if (status == SPORK_OK && done.takes > count + done.frees) status = SPORK_E_NOBLOCKS;
@@ -217,7 +213,6 @@ __global__ void __launch_bounds__(kDecideThreads) tables_decide(TablesArgs a) {
   t->front = front;
   t->count = count;
   t->error = 0;
-  t->arrived = 0;
   *a.status = status;
   *a.n_copies = status == SPORK_OK ? done.copies : 0;
   a.row_off[0] = 0;
@@ -232,24 +227,21 @@ __device__ __forceinline__ int ring(const TablesArgs& a, int front, int64_t nth)
 }
 
 __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
-  __shared__ int freed[kRowThreads / 64];
+  __shared__ int freed[kAtOnce][kRowThreads / 64];
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const TablesTotals t = *a.totals;
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) return;
   if (t.status != SPORK_OK) {  // as it was: references back, words clear
-    if (r.parent >= 0) {
-      for (int j = tid; j < r.keep; j += kRowThreads) {
-        const int b = a.table[place(a, r.parent, j)];
+    if (r.parent >= 0)
+      each_entry(a, r.parent, 0, r.keep, [&](int, int b) {
         if (in_pool(a, b)) atomicAdd(a.refcount + b, -1);
-      }
-    }
-    for (int j = r.release_lo + tid; j < r.held; j += kRowThreads) {
-      const int b = a.table[place(a, s, j)];
-      if (!in_pool(a, b)) continue;
+      });
+    each_entry(a, s, r.release_lo, r.held, [&](int, int b) {
+      if (!in_pool(a, b)) return;
       atomicAdd(a.refcount + b, 1);
       a.last_release[b] = 0;
-    }
+    });
     if (tid == 0) {
       const int b = shared_tail(a, r);
       if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
@@ -257,30 +249,38 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
     return;
   }
   int at = a.frees[s];  // of the row's freed blocks among all
-  for (int j0 = r.release_lo; j0 < r.held; j0 += kRowThreads) {
-    const int j = j0 + tid;
-    int b = 0;
-    bool free_here = false;
-    if (j < r.held) {
-      b = a.table[place(a, s, j)];
-      // The last place alone clears the word: any other compares unequal before and after.
-      if (a.last_release[b] == static_cast<int>(place(a, s, j)) + 1) {
-        free_here = a.refcount[b] == 0;
-        a.last_release[b] = 0;
+  for (int j0 = r.release_lo; j0 < r.held; j0 += kAtOnce * kRowThreads) {
+    int b[kAtOnce];
+    bool here[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int j = j0 + q * kRowThreads + tid;
+      b[q] = j < r.held ? a.table[place(a, s, j)] : -1;
+    }
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) here[q] = b[q] >= 0 && frees_block(a, s, j0 + q * kRowThreads + tid, b[q]);
+    // The last place alone clears the word: any other compares unequal before and after.
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q)
+      if (b[q] >= 0 && a.last_release[b[q]] == static_cast<int>(place(a, s, j0 + q * kRowThreads + tid)) + 1) a.last_release[b[q]] = 0;
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const uint64_t bal = __ballot(here[q]);
+      if (lane == 0) freed[q][wave] = __popcll(bal);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      int rank = at + __popcll(__ballot(here[q]) & ((uint64_t{1} << lane) - 1));
+#pragma unroll
+      for (int w = 0; w < kRowThreads / 64; ++w) {
+        if (w < wave) rank += freed[q][w];
+        at += freed[q][w];
       }
+      if (here[q]) a.free_queue[ring(a, t.front, static_cast<int64_t>(t.count) + rank)] = b[q];
     }
-    const uint64_t bal = __ballot(free_here);
-    __syncthreads();
-    if (lane == 0) freed[wave] = __popcll(bal);
-    __syncthreads();
-    int rank = at + __popcll(bal & ((uint64_t{1} << lane) - 1));
-    for (int w = 0; w < kRowThreads / 64; ++w) {
-      if (w < wave) rank += freed[w];
-      at += freed[w];
-    }
-    if (free_here) a.free_queue[ring(a, t.front, static_cast<int64_t>(t.count) + rank)] = b;
+    __syncthreads();  // the counts are read
   }
-  __syncthreads();
   if (tid == 0) {
     const int b = shared_tail(a, r), c = a.copy_off[s];
     if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
@@ -289,8 +289,8 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
       a.copies[3 * c + 2] = r.len % a.block_size;
     }
   }
-  if (r.parent >= 0)
-    for (int j = tid; j < r.keep; j += kRowThreads) a.table[place(a, s, j)] = a.table[place(a, r.parent, j)];
+  // (the row's old entries are read: every thread is past the loop's last barrier)
+  if (r.parent >= 0) each_entry(a, r.parent, 0, r.keep, [&](int j, int b) { a.table[place(a, s, j)] = b; });
 }
 
 __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
@@ -375,26 +375,37 @@ __global__ void __launch_bounds__(256) words_clear_kernel(int32_t* words, int64_
 }
 
 // The copies of copy-on-write, from the list that a step wrote: a workgroup per
-// (copy, KV head), 16 bytes a thread. K: the first n_valid tokens are one run of
-// bytes. V: by element, the first n_valid of each channel's run of block_size.
-__global__ void __launch_bounds__(256) kv_copy_batch_kernel(int elem, int hkv, int D, int BS, int num_blocks, char* kc,
-                                                            char* vc, const int32_t* copies, const int32_t* n_copies,
-                                                            int max_copies) {
+// (copy, KV head). K: the first n_valid tokens are one run of bytes. V: of each
+// channel's run of block_size elements the first n_valid, 16 bytes at a time but
+// for the last ones.
+template <typename T>
+__global__ void __launch_bounds__(256) kv_copy_batch_kernel(int hkv, int D, int BS, int num_blocks, T* kc, T* vc,
+                                                            const int32_t* copies, const int32_t* n_copies, int max_copies) {
+  constexpr int VEC = 16 / sizeof(T);
   const int c = blockIdx.x / hkv, h = blockIdx.x % hkv;
   if (c >= min(*n_copies, max_copies)) return;
   const int src = copies[3 * c], dst = copies[3 * c + 1], nv = copies[3 * c + 2];
   if (src < 0 || src >= num_blocks || dst < 0 || dst >= num_blocks || src == dst || nv <= 0 || nv > BS) return;
-  const size_t bytes = static_cast<size_t>(D) * BS * elem;
-  const size_t from = (static_cast<size_t>(src) * hkv + h) * bytes, to = (static_cast<size_t>(dst) * hkv + h) * bytes;
+  const size_t size = static_cast<size_t>(D) * BS;
+  const size_t from = (static_cast<size_t>(src) * hkv + h) * size, to = (static_cast<size_t>(dst) * hkv + h) * size;
   const uint4* ks = reinterpret_cast<const uint4*>(kc + from);
   uint4* kd = reinterpret_cast<uint4*>(kc + to);
-  for (int i = threadIdx.x; i < nv * D * elem / 16; i += 256) kd[i] = ks[i];
-  const int run = BS * elem;
-  for (int i = threadIdx.x; i < D * run / elem; i += 256) {
-    const int t = i % BS;
-    if (t >= nv) continue;
-    if (elem == 2) reinterpret_cast<uint16_t*>(vc + to)[i] = reinterpret_cast<const uint16_t*>(vc + from)[i];
-    else reinterpret_cast<uint32_t*>(vc + to)[i] = reinterpret_cast<const uint32_t*>(vc + from)[i];
+  for (int i = threadIdx.x; i < nv * (D / VEC); i += 256) kd[i] = ks[i];
+  const T* vs = vc + from;
+  T* vd = vc + to;
+  if (BS % VEC == 0) {
+    const int pieces = BS / VEC;  // of a channel
+    for (int i = threadIdx.x; i < D * pieces; i += 256) {
+      const int n = nv - i % pieces * VEC;
+      if (n >= VEC) {
+        reinterpret_cast<uint4*>(vd)[i] = reinterpret_cast<const uint4*>(vs)[i];
+      } else {
+        for (int e = 0; e < n; ++e) vd[i * VEC + e] = vs[i * VEC + e];
+      }
+    }
+  } else {
+    for (int i = threadIdx.x; i < D * BS; i += 256)
+      if (i % BS < nv) vd[i] = vs[i];
   }
 }
 
@@ -435,7 +446,8 @@ hipError_t launch_words_clear(int32_t* words, int64_t n, hipStream_t stream) {
 hipError_t launch_tables_step(const TablesArgs& a, hipStream_t stream) {
   const unsigned rows = static_cast<unsigned>(a.n_seqs);
   hipLaunchKernelGGL(tables_count, dim3(rows), dim3(kRowThreads), 0, stream, a);
-  hipLaunchKernelGGL(tables_decide, dim3((rows + kDecideRows - 1) / kDecideRows), dim3(kDecideThreads), 0, stream, a);
+  hipLaunchKernelGGL(tables_rows, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  hipLaunchKernelGGL(tables_sum, dim3(1), dim3(kSumThreads), 0, stream, a);
   hipLaunchKernelGGL(tables_release, dim3(rows), dim3(kRowThreads), 0, stream, a);
   const unsigned tokens = (static_cast<unsigned>(a.max_tokens) + kRowThreads - 1) / kRowThreads;
   hipLaunchKernelGGL(tables_assign, dim3(rows + tokens), dim3(kRowThreads), 0, stream, a);
@@ -446,9 +458,13 @@ hipError_t launch_kv_copy_batch(int32_t elem_bytes, int32_t hkv, int32_t head_di
                                 void* k_cache, void* v_cache, const int32_t* copies, const int32_t* n_copies,
                                 int32_t max_copies, hipStream_t stream) {
   if (max_copies <= 0) return hipSuccess;
-  hipLaunchKernelGGL(kv_copy_batch_kernel, dim3(static_cast<unsigned>(max_copies) * static_cast<unsigned>(hkv)), dim3(256), 0,
-                     stream, elem_bytes, hkv, head_dim, block_size, num_blocks, static_cast<char*>(k_cache),
-                     static_cast<char*>(v_cache), copies, n_copies, max_copies);
+  const dim3 grid(static_cast<unsigned>(max_copies) * static_cast<unsigned>(hkv));
+  if (elem_bytes == 2)
+    hipLaunchKernelGGL(kv_copy_batch_kernel<uint16_t>, grid, dim3(256), 0, stream, hkv, head_dim, block_size, num_blocks,
+                       static_cast<uint16_t*>(k_cache), static_cast<uint16_t*>(v_cache), copies, n_copies, max_copies);
+  else
+    hipLaunchKernelGGL(kv_copy_batch_kernel<float>, grid, dim3(256), 0, stream, hkv, head_dim, block_size, num_blocks,
+                       static_cast<float*>(k_cache), static_cast<float*>(v_cache), copies, n_copies, max_copies);
   return hipGetLastError();
 }
 

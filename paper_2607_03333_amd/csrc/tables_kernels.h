@@ -12,10 +12,10 @@ namespace spork {
 // What the launches of a step leave each other: row results in row order and
 // the step's totals. All of it lies in the workspace, behind the block words.
 struct TablesTotals {
-  int32_t error;    // lowest status of the rows, 0 between steps
-  int32_t arrived;  // workgroups of the deciding launch that are done, 0 between steps
-  int32_t status;   // the step's status
-  int32_t front, count;  // the queue after the releases
+  int32_t error;         // lowest status of the rows, 0 between steps
+  int32_t zero;
+  int32_t status;        // the step's status
+  int32_t front, count;  // the queue before the step
   int32_t pad[3];
 };
 

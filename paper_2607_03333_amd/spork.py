@@ -170,11 +170,19 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_stream()  # (initialises the GPU, or says why it can't)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object: 0.5 us against 2.9
+        _raw_stream = (lambda: raw(torch.cuda.current_device())) if raw else lambda: torch.cuda.current_stream().cuda_stream
+    return _raw_stream()
 
 
 def _i32(a):
