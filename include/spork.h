@@ -459,7 +459,7 @@ int spork_tables_workspace_clear(const spork_tables* tables, void* workspace, si
  * The tables' own consistency (refcounts, queue contents) is not checked;
  * a bad one never reads or writes outside the buffers.
  * workspace (device, 256-byte aligned; words zero on entry, see above; steps
- * that share it must not overlap). Five launches. Same inputs, same tables:
+ * that share it must not overlap). Four launches, or five for many rows. Same inputs, same tables:
  * no result depends on the order of atomics. */
 int spork_tables_step(const spork_tables* tables, const int32_t* lens, const int32_t* n_new,
                       const int32_t* parents, int32_t max_tokens, int64_t* slots, int32_t* positions,

@@ -20,12 +20,14 @@
 // and last places go through atomics whose order does not matter (sums, maxima),
 // so the same step gives the same tables every time.
 //
-// Five launches: count (references and last places), rows (what each row frees and
-// takes), sum (over the rows, and whether the step fits), release (frees into the
-// queue, forked rows, copies), assign (fronts into the tables, slots). The
+// Four launches: count (references and last places), rows (what each row frees and
+// takes), release (the sums over the rows and whether the step fits; frees into
+// the queue, forked rows, copies), assign (fronts into the tables, slots). The
 // references are changed while they are counted, and changed back where the step
-// is refused. A workgroup per row but in sum, and four entries of its row in
-// flight per thread: a fork or the end of a long row is thousands of entries.
+// is refused. A workgroup per row, and four entries of its row in flight per
+// thread: a fork or the end of a long row is thousands of entries. Up to
+// kRowsSummedByAll rows every workgroup of release sums what it needs by itself;
+// more are summed once, by a launch between.
 #include "device_common.h"
 #include "spork.h"
 #include "tables_kernels.h"
@@ -37,6 +39,7 @@ namespace {
 constexpr int kRowThreads = 256;   // of a row's workgroup
 constexpr int kSumThreads = 1024;  // of the one workgroup that sums the rows
 constexpr int kAtOnce = 4;         // entries of a row that a thread loads together
+constexpr int kRowsSummedByAll = 1024;
 
 struct Row {
   int len, grow, parent, held;
@@ -99,6 +102,7 @@ __device__ __forceinline__ void each_entry(const TablesArgs& a, int s, int lo, i
 
 __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
   const int s = blockIdx.x;
+  if (s == 0 && threadIdx.x == 0) a.totals->front = a.queue[0];
   Row r;
   int err = read_row(a, s, &r);
   if (err == SPORK_OK) {
@@ -138,7 +142,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
   const int s = blockIdx.x, tid = threadIdx.x;
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) {  // the step is refused
-    if (tid == 0) a.frees[s] = a.takes[s] = a.copy_off[s] = 0;
+    if (tid == 0) a.frees[s] = a.takes[s] = a.copies_of[s] = 0;
     return;
   }
   int copies = 0;
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
   if (tid == 0) {
     a.frees[s] = frees;
     a.takes[s] = copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
-    a.copy_off[s] = copies;
+    a.copies_of[s] = copies;
   }
 }
 
@@ -175,50 +179,83 @@ struct Sums {
 __device__ __forceinline__ Sums operator+(const Sums& x, const Sums& y) {
   return {x.tokens + y.tokens, x.frees + y.frees, x.takes + y.takes, x.copies + y.copies};
 }
+__device__ __forceinline__ Sums row_sums(const TablesArgs& a, int i) {
+  return {max(a.n_new[i], 0), a.frees[i], a.takes[i], a.copies_of[i]};
+}
+
+// The step's status, from the sums over all rows.
+__device__ __forceinline__ int status_of(const TablesArgs& a, const Sums& all, int error, int front, int count) {
+  int status = error;
+  if (front < 0 || front >= a.num_blocks || count < 0 || count > a.num_blocks - all.frees) status = min(status, SPORK_E_INVAL);
+  if (all.tokens > a.max_tokens) status = min(status, SPORK_E_CAPACITY);
+  if (status == SPORK_OK && all.takes > count + all.frees) status = SPORK_E_NOBLOCKS;
+  return status;
+}
+
+__device__ __forceinline__ void write_row_sums(const TablesArgs& a, int i, const Sums& before, const Sums& own) {
+  a.free_off[i] = before.frees;
+  a.take_off[i] = before.takes;
+  a.copy_off[i] = own.copies ? before.copies : -1;
+  a.row_off[i + 1] = static_cast<int>(min(before.tokens + own.tokens, static_cast<int64_t>(INT_MAX)));
+  if (i == 0) a.row_off[0] = 0;
+}
+
+__device__ __forceinline__ void write_totals(const TablesArgs& a, const Sums& all, int status) {
+  a.totals->status = status;
+  a.totals->frees = all.frees;
+  a.totals->takes = all.takes;
+  *a.status = status;
+  *a.n_copies = status == SPORK_OK ? all.copies : 0;
+}
 
 __global__ void __launch_bounds__(kSumThreads) tables_sum(TablesArgs a) {
   constexpr int kWaves = kSumThreads / 64;
   __shared__ Sums wave_sums[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int front = a.queue[0], count = a.queue[1];
-  int status = a.totals->error;
+  const int front = a.queue[0], count = a.queue[1], error = a.totals->error;
   Sums done{0, 0, 0, 0};
   for (int s0 = 0, odd = 0; s0 < a.n_seqs; s0 += kSumThreads, odd ^= 1) {
     const int i = s0 + tid;
     Sums x{0, 0, 0, 0};
-    if (i < a.n_seqs) x = {max(a.n_new[i], 0), a.frees[i], a.takes[i], a.copy_off[i]};
-    Sums upto{wave_scan(x.tokens), wave_scan(x.frees), wave_scan(x.takes), wave_scan(x.copies)};
+    if (i < a.n_seqs) x = row_sums(a, i);
+    const Sums upto{wave_scan(x.tokens), wave_scan(x.frees), wave_scan(x.takes), wave_scan(x.copies)};
     if (lane == 63) wave_sums[odd][wave] = upto;
     __syncthreads();  // (the other half is free again once everybody is here)
-    upto = upto + done;
+    Sums before = done + Sums{upto.tokens - x.tokens, upto.frees - x.frees, upto.takes - x.takes, upto.copies - x.copies};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const Sums y = wave_sums[odd][w];
-      if (w < wave) upto = upto + y;
+      if (w < wave) before = before + y;
       done = done + y;
     }
-    if (i < a.n_seqs) {
-      a.frees[i] = upto.frees - x.frees;
-      a.takes[i] = upto.takes - x.takes;
-      a.copy_off[i] = x.copies ? upto.copies - 1 : -1 - upto.copies;
-      a.row_off[i + 1] = static_cast<int>(min(upto.tokens, static_cast<int64_t>(INT_MAX)));
-    }
+    if (i < a.n_seqs) write_row_sums(a, i, before, x);
   }
-  if (tid != 0) return;
-  if (front < 0 || front >= a.num_blocks || count < 0 || count > a.num_blocks - done.frees) status = min(status, SPORK_E_INVAL);
-  if (done.tokens > a.max_tokens) status = min(status, SPORK_E_CAPACITY);
-  if (status == SPORK_OK && done.takes > count + done.frees) status = SPORK_E_NOBLOCKS;
-  TablesTotals* t = a.totals;
-  t->status = status;
-  t->front = front;
-  t->count = count;
-  t->error = 0;
-  *a.status = status;
-  *a.n_copies = status == SPORK_OK ? done.copies : 0;
-  a.row_off[0] = 0;
-  if (status == SPORK_OK) {
-    a.queue[0] = static_cast<int>((static_cast<int64_t>(front) + done.takes) % a.num_blocks);
-    a.queue[1] = count + done.frees - done.takes;
+  if (tid == 0) write_totals(a, done, status_of(a, done, error, front, count));
+}
+
+// The same within a workgroup of release: the sums before row s and over all rows.
+__device__ __forceinline__ void sum_here(const TablesArgs& a, int s, Sums* before, Sums* all) {
+  constexpr int kWaves = kRowThreads / 64;
+  __shared__ Sums parts[2][kWaves];
+  const int tid = threadIdx.x;
+  Sums lo{0, 0, 0, 0}, hi = lo;
+  for (int i = tid; i < a.n_seqs; i += kRowThreads) {
+    const Sums x = row_sums(a, i);
+    if (i < s) lo = lo + x;
+    else hi = hi + x;
+  }
+  lo = {wave_scan(lo.tokens), wave_scan(lo.frees), wave_scan(lo.takes), wave_scan(lo.copies)};
+  hi = {wave_scan(hi.tokens), wave_scan(hi.frees), wave_scan(hi.takes), wave_scan(hi.copies)};
+  if ((tid & 63) == 63) {
+    parts[0][tid >> 6] = lo;
+    parts[1][tid >> 6] = hi;
+  }
+  __syncthreads();
+  *before = *all = {0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    *before = *before + parts[0][w];
+    *all = *all + parts[0][w] + parts[1][w];
   }
 }
 
@@ -226,13 +263,32 @@ __device__ __forceinline__ int ring(const TablesArgs& a, int front, int64_t nth)
   return static_cast<int>((front + nth) % a.num_blocks);
 }
 
+// kSummed: by tables_sum.
+template <bool kSummed>
 __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
   __shared__ int freed[kAtOnce][kRowThreads / 64];
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const TablesTotals t = *a.totals;
+  const int front = a.queue[0], count = a.queue[1];
+  int at, c, status;  // the row's freed blocks among all, its copy or -1
+  if constexpr (kSummed) {
+    at = a.free_off[s];
+    c = a.copy_off[s];
+    status = a.totals->status;
+  } else {
+    const int error = a.totals->error;
+    Sums before, all;
+    sum_here(a, s, &before, &all);
+    status = status_of(a, all, error, front, count);
+    at = before.frees;
+    c = a.copies_of[s] ? before.copies : -1;
+    if (tid == 0) {
+      write_row_sums(a, s, before, row_sums(a, s));
+      if (s == 0) write_totals(a, all, status);
+    }
+  }
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) return;
-  if (t.status != SPORK_OK) {  // as it was: references back, words clear
+  if (status != SPORK_OK) {  // as it was: references back, words clear
     if (r.parent >= 0)
       each_entry(a, r.parent, 0, r.keep, [&](int, int b) {
         if (in_pool(a, b)) atomicAdd(a.refcount + b, -1);
@@ -248,7 +304,6 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
     }
     return;
   }
-  int at = a.frees[s];  // of the row's freed blocks among all
   for (int j0 = r.release_lo; j0 < r.held; j0 += kAtOnce * kRowThreads) {
     int b[kAtOnce];
     bool here[kAtOnce];
@@ -277,12 +332,12 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
         if (w < wave) rank += freed[q][w];
         at += freed[q][w];
       }
-      if (here[q]) a.free_queue[ring(a, t.front, static_cast<int64_t>(t.count) + rank)] = b[q];
+      if (here[q]) a.free_queue[ring(a, front, static_cast<int64_t>(count) + rank)] = b[q];
     }
     __syncthreads();  // the counts are read
   }
   if (tid == 0) {
-    const int b = shared_tail(a, r), c = a.copy_off[s];
+    const int b = shared_tail(a, r);
     if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
     if (c >= 0) {
       a.copies[3 * c] = b;
@@ -295,10 +350,18 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
 
 __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
   const int tid = threadIdx.x, bs = a.block_size;
-  const TablesTotals t = *a.totals;
+  const int status = a.totals->status, front = a.totals->front;
   if (static_cast<int>(blockIdx.x) < a.n_seqs) {  // a row: its table and references
     const int s = blockIdx.x;
-    if (t.status != SPORK_OK) {
+    if (s == 0 && tid == 0) {
+      if (status == SPORK_OK) {
+        const TablesTotals t = *a.totals;
+        a.queue[0] = ring(a, front, t.takes);
+        a.queue[1] += t.frees - t.takes;
+      }
+      a.totals->error = 0;
+    }
+    if (status != SPORK_OK) {
       if (tid == 0) {
         a.row_off[s + 1] = 0;
         a.kv_len[s] = 0;
@@ -307,10 +370,10 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
     }
     const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
     const int c = a.copy_off[s];
-    int64_t first = a.takes[s];
+    int64_t first = a.take_off[s];
     if (c >= 0) {
       if (tid == 0) {
-        const int dst = a.free_queue[ring(a, t.front, first)];
+        const int dst = a.free_queue[ring(a, front, first)];
         atomicAdd(a.refcount + a.copies[3 * c], -1);
         a.copies[3 * c + 1] = dst;
         a.refcount[dst] = 1;
@@ -319,7 +382,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
       ++first;
     }
     for (int j = keep + tid; j < to; j += kRowThreads) {
-      const int b = a.free_queue[ring(a, t.front, first + j - keep)];
+      const int b = a.free_queue[ring(a, front, first + j - keep)];
       a.table[place(a, s, j)] = b;
       a.refcount[b] = 1;
     }
@@ -335,7 +398,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
   if (i >= a.max_tokens) return;
   int64_t slot = -1;
   int pos = -1;
-  if (t.status == SPORK_OK && i < a.row_off[a.n_seqs]) {
+  if (status == SPORK_OK && i < a.row_off[a.n_seqs]) {
     int lo = 0, hi = a.n_seqs - 1;  // the last row that starts at or before token i
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -345,10 +408,10 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
     const int s = lo, len = a.lens[s], keep = blocks_of(len, bs), c = a.copy_off[s];
     pos = len + i - a.row_off[s];
     const int col = pos / bs;
-    const int64_t first = a.takes[s] + (c >= 0 ? 1 : 0);
+    const int64_t first = a.take_off[s] + (c >= 0 ? 1 : 0);
     int b;
-    if (col >= keep) b = a.free_queue[ring(a, t.front, first + col - keep)];
-    else if (c >= 0) b = a.free_queue[ring(a, t.front, first - 1)];
+    if (col >= keep) b = a.free_queue[ring(a, front, first + col - keep)];
+    else if (c >= 0) b = a.free_queue[ring(a, front, first - 1)];
     else b = a.table[place(a, s, col)];
     slot = static_cast<int64_t>(b) * bs + pos % bs;
   }
@@ -416,7 +479,7 @@ size_t tables_control_bytes(int32_t num_blocks) {
 }
 
 size_t tables_workspace_bytes(int32_t num_blocks, int32_t n_seqs) {
-  return tables_control_bytes(num_blocks) + 3 * sizeof(int32_t) * static_cast<size_t>(n_seqs);
+  return tables_control_bytes(num_blocks) + 6 * sizeof(int32_t) * static_cast<size_t>(n_seqs);
 }
 
 void tables_workspace(TablesArgs* a, void* workspace) {
@@ -426,7 +489,10 @@ void tables_workspace(TablesArgs* a, void* workspace) {
   a->last_sharer = a->sharers + a->num_blocks;
   a->frees = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + tables_control_bytes(a->num_blocks));
   a->takes = a->frees + a->n_seqs;
-  a->copy_off = a->takes + a->n_seqs;
+  a->copies_of = a->takes + a->n_seqs;
+  a->free_off = a->copies_of + a->n_seqs;
+  a->take_off = a->free_off + a->n_seqs;
+  a->copy_off = a->take_off + a->n_seqs;
 }
 
 hipError_t launch_tables_init(const TablesArgs& a, const int32_t* free_order, hipStream_t stream) {
@@ -447,8 +513,12 @@ hipError_t launch_tables_step(const TablesArgs& a, hipStream_t stream) {
   const unsigned rows = static_cast<unsigned>(a.n_seqs);
   hipLaunchKernelGGL(tables_count, dim3(rows), dim3(kRowThreads), 0, stream, a);
   hipLaunchKernelGGL(tables_rows, dim3(rows), dim3(kRowThreads), 0, stream, a);
-  hipLaunchKernelGGL(tables_sum, dim3(1), dim3(kSumThreads), 0, stream, a);
-  hipLaunchKernelGGL(tables_release, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  if (a.n_seqs > kRowsSummedByAll) {
+    hipLaunchKernelGGL(tables_sum, dim3(1), dim3(kSumThreads), 0, stream, a);
+    hipLaunchKernelGGL(tables_release<true>, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL(tables_release<false>, dim3(rows), dim3(kRowThreads), 0, stream, a);
+  }
   const unsigned tokens = (static_cast<unsigned>(a.max_tokens) + kRowThreads - 1) / kRowThreads;
   hipLaunchKernelGGL(tables_assign, dim3(rows + tokens), dim3(kRowThreads), 0, stream, a);
   return hipGetLastError();

@@ -15,8 +15,9 @@ struct TablesTotals {
   int32_t error;         // lowest status of the rows, 0 between steps
   int32_t zero;
   int32_t status;        // the step's status
-  int32_t front, count;  // the queue before the step
-  int32_t pad[3];
+  int32_t front;         // the queue's front before the step
+  int32_t frees, takes;  // of all rows
+  int32_t pad[2];
 };
 
 struct TablesArgs {
@@ -41,9 +42,12 @@ struct TablesArgs {
   int32_t* sharers;       // rows that append inside the block
   int32_t* last_sharer;   // 1 + the last of them
   // ... and per row
-  int32_t* frees;     // blocks the row's releases put into the queue, then their exclusive sum
-  int32_t* takes;     // blocks the row takes from it, then their exclusive sum
-  int32_t* copy_off;  // copies before the row, or -1 - that number where the row makes none
+  int32_t* frees;      // blocks that the row's releases put into the queue
+  int32_t* takes;      // blocks that the row takes from it
+  int32_t* copies_of;  // 1: the row makes a copy
+  int32_t* free_off;   // sums of these over the rows before; copy_off: -1 where the row makes no copy
+  int32_t* take_off;
+  int32_t* copy_off;
   TablesTotals* totals;
 };
 

@@ -399,7 +399,7 @@ def _want(name, x, size, *shape):
     passes: the library says what may be NULL)."""
     if x is None:
         return None
-    if x.shape != shape or x.element_size() != size or x.is_floating_point() or not x.is_contiguous():
+    if x.shape != shape or x.element_size() != size or not x.is_contiguous() or x.is_floating_point():
         raise ValueError(f"{name} must be a contiguous tensor of {8 * size}-bit integers of shape {list(shape)}, "
                          f"not {x.dtype} {list(x.shape)}")
     return x.data_ptr()
