@@ -59,7 +59,7 @@ constexpr float kSlackSum = 256.0f;
 // HBM bounds it, about 9 ns on one compute unit.
 constexpr int kTileCost = 640;      // a tile's start-up and end
 constexpr int kMinSlice = 512;      // least length of a slice
-constexpr int kMinPiece = 64;       // tokens: a cut closer to a tile's end moves to it
+constexpr int kMinPiece = 256;      // least cost of a piece: a cut closer to a tile's end moves to it
 // A token of a tile of `heads` KV heads with so many row tiles each: bf16 by
 // bytes until the products weigh more; fp32 products (64 flop per cycle and SIMD)
 // weigh more from the first row tile.
@@ -144,7 +144,8 @@ __device__ __forceinline__ int cut(int64_t y, int64_t tile_cost, int cost, int e
   if (y <= 0) return 0;
   if (y >= tile_cost) return end;
   const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) / cost) & ~31;
-  return t < kMinPiece ? 0 : t > end - kMinPiece ? end : t;
+  const int least = max(32, kMinPiece / cost & ~31);
+  return t < least ? 0 : t > end - least ? end : t;
 }
 
 // --------------------------------------------------------------------------
@@ -1175,7 +1176,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 // lane. Lane i of a row takes the maximum and sum of pieces i, i + D / 4, ..., so
 // that the weights are there in one round trip; the pieces' rows then come in
 // sixteen at a time (four, where there are no more).
-constexpr int kMergeWaves = 4, kMergeGroups = 8;  // of a workgroup; workgroups of a slice
+constexpr int kMergeWaves = 4, kMergeGroups = 16;  // of a workgroup; workgroups of a slice
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kMergeWaves) chunk_merge_kernel(ChunkArgs a) {

@@ -87,17 +87,32 @@ __device__ __forceinline__ int shared_tail(const TablesArgs& a, const Row& r) {
   return a.table[place(a, r.from, r.len / a.block_size)];
 }
 
-// f(column, entry) for the columns [lo, hi) of table row s, each by one thread.
-template <typename F>
-__device__ __forceinline__ void each_entry(const TablesArgs& a, int s, int lo, int hi, F f) {
-  for (int j0 = lo + static_cast<int>(threadIdx.x); j0 < hi; j0 += kAtOnce * kRowThreads) {
-    int b[kAtOnce];
+// What forks and releases change in the columns of table row s from column j0 on,
+// kAtOnce of them per thread: the entry that was there and the one that comes.
+struct Changes {
+  int was[kAtOnce], now[kAtOnce];
+  bool loses[kAtOnce], gains[kAtOnce];
+};
+__device__ __forceinline__ int changes_lo(const Row& r) { return r.release_lo; }
+__device__ __forceinline__ int changes_hi(const Row& r) { return r.parent >= 0 ? max(r.held, r.keep) : r.held; }
+__device__ __forceinline__ int column(int j0, int q) { return j0 + q * kRowThreads + static_cast<int>(threadIdx.x); }
+__device__ __forceinline__ Changes changes(const TablesArgs& a, int s, const Row& r, int j0) {
+  Changes x;
 #pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) b[q] = j0 + q * kRowThreads < hi ? a.table[place(a, s, j0 + q * kRowThreads)] : -1;
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q)
-      if (j0 + q * kRowThreads < hi) f(j0 + q * kRowThreads, b[q]);
+  for (int q = 0; q < kAtOnce; ++q) {
+    const int j = column(j0, q);
+    x.loses[q] = j < r.held;
+    x.gains[q] = r.parent >= 0 && j < r.keep;
+    x.was[q] = x.loses[q] ? a.table[place(a, s, j)] : -1;
+    x.now[q] = x.gains[q] ? a.table[place(a, r.parent, j)] : -1;
   }
+  // An entry that a fork gives and takes at once stays as it is: a probe that forks
+  // again where it forked before, a few tokens on. (The block keeps this holder, so
+  // leaving out one reference more and one less frees nothing and keeps nothing.)
+#pragma unroll
+  for (int q = 0; q < kAtOnce; ++q)
+    if (x.loses[q] && x.gains[q] && x.was[q] == x.now[q] && in_pool(a, x.was[q])) x.loses[q] = x.gains[q] = false;
+  return x;
 }
 
 __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
@@ -106,19 +121,24 @@ __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
   Row r;
   int err = read_row(a, s, &r);
   if (err == SPORK_OK) {
-    if (r.parent >= 0)
-      each_entry(a, r.parent, 0, r.keep, [&](int, int b) {
-        if (in_pool(a, b)) atomicAdd(a.refcount + b, 1);
-        else err = SPORK_E_INVAL;
-      });
-    each_entry(a, s, r.release_lo, r.held, [&](int j, int b) {
-      if (in_pool(a, b)) {
-        atomicAdd(a.refcount + b, -1);
-        atomicMax(a.last_release + b, static_cast<int>(place(a, s, j)) + 1);
-      } else {
-        err = SPORK_E_INVAL;
+    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
+      const Changes x = changes(a, s, r, j0);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (x.gains[q]) {
+          if (in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], 1);
+          else err = SPORK_E_INVAL;
+        }
+        if (x.loses[q]) {
+          if (in_pool(a, x.was[q])) {
+            atomicAdd(a.refcount + x.was[q], -1);
+            atomicMax(a.last_release + x.was[q], static_cast<int>(place(a, s, column(j0, q))) + 1);
+          } else {
+            err = SPORK_E_INVAL;
+          }
+        }
       }
-    });
+    }
     if (threadIdx.x == 0 && r.grow != 0 && r.len % a.block_size != 0) {
       const int b = shared_tail(a, r);
       if (in_pool(a, b)) {
@@ -154,8 +174,12 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
     }
   }
   int frees = 0;
-  if (r.release_lo < r.held) {
-    each_entry(a, s, r.release_lo, r.held, [&](int j, int b) { frees += frees_block(a, s, j, b); });
+  if (changes_lo(r) < changes_hi(r)) {
+    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
+      const Changes x = changes(a, s, r, j0);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) frees += x.loses[q] && frees_block(a, s, column(j0, q), x.was[q]);
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o /= 2) frees += __shfl_xor(frees, o);
     if ((tid & 63) == 0) freed[tid >> 6] = frees;
@@ -289,37 +313,34 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) return;
   if (status != SPORK_OK) {  // as it was: references back, words clear
-    if (r.parent >= 0)
-      each_entry(a, r.parent, 0, r.keep, [&](int, int b) {
-        if (in_pool(a, b)) atomicAdd(a.refcount + b, -1);
-      });
-    each_entry(a, s, r.release_lo, r.held, [&](int, int b) {
-      if (!in_pool(a, b)) return;
-      atomicAdd(a.refcount + b, 1);
-      a.last_release[b] = 0;
-    });
+    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
+      const Changes x = changes(a, s, r, j0);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (x.gains[q] && in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], -1);
+        if (x.loses[q] && in_pool(a, x.was[q])) {
+          atomicAdd(a.refcount + x.was[q], 1);
+          a.last_release[x.was[q]] = 0;
+        }
+      }
+    }
     if (tid == 0) {
       const int b = shared_tail(a, r);
       if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
     }
     return;
   }
-  for (int j0 = r.release_lo; j0 < r.held; j0 += kAtOnce * kRowThreads) {
-    int b[kAtOnce];
+  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
+    const Changes x = changes(a, s, r, j0);
     bool here[kAtOnce];
 #pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) {
-      const int j = j0 + q * kRowThreads + tid;
-      b[q] = j < r.held ? a.table[place(a, s, j)] : -1;
-    }
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) here[q] = b[q] >= 0 && frees_block(a, s, j0 + q * kRowThreads + tid, b[q]);
-    // The last place alone clears the word: any other compares unequal before and after.
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q)
-      if (b[q] >= 0 && a.last_release[b[q]] == static_cast<int>(place(a, s, j0 + q * kRowThreads + tid)) + 1) a.last_release[b[q]] = 0;
+    for (int q = 0; q < kAtOnce; ++q) here[q] = x.loses[q] && frees_block(a, s, column(j0, q), x.was[q]);
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) {
+      const int place1 = static_cast<int>(place(a, s, column(j0, q))) + 1;
+      // The last place alone clears the word: any other compares unequal before and after.
+      if (x.loses[q] && a.last_release[x.was[q]] == place1) a.last_release[x.was[q]] = 0;
+      if (x.gains[q]) a.table[place1 - 1] = x.now[q];  // (this thread alone reads the column)
       const uint64_t bal = __ballot(here[q]);
       if (lane == 0) freed[q][wave] = __popcll(bal);
     }
@@ -332,7 +353,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
         if (w < wave) rank += freed[q][w];
         at += freed[q][w];
       }
-      if (here[q]) a.free_queue[ring(a, front, static_cast<int64_t>(count) + rank)] = b[q];
+      if (here[q]) a.free_queue[ring(a, front, static_cast<int64_t>(count) + rank)] = x.was[q];
     }
     __syncthreads();  // the counts are read
   }
@@ -344,8 +365,6 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
       a.copies[3 * c + 2] = r.len % a.block_size;
     }
   }
-  // (the row's old entries are read: every thread is past the loop's last barrier)
-  if (r.parent >= 0) each_entry(a, r.parent, 0, r.keep, [&](int j, int b) { a.table[place(a, s, j)] = b; });
 }
 
 __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {

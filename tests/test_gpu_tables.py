@@ -141,6 +141,26 @@ def test_long_rows_and_whole_batches_end():
     assert sorted(model.queue) == list(range(nb))
 
 
+def test_probes_that_fork_again_where_they_were():
+    """Rows that give up and take over the same entries in one step, with a parent that grows, is rolled back below
+    them or ends, and steps that are refused in between."""
+    bs, nb, n, most = 16, 700, 7, 40
+    order = np.random.default_rng(9).permutation(nb).tolist()
+    model, dev = TablesModel(n, nb, bs, most, order), Device(n, nb, bs, most, order)
+    fork = [-1, 0, 0, -1, 3, 3, 3]
+    steps = [([0] * n, [333, 0, 0, 100, 0, 0, 0], [-1] * n), ([333, 333, 320, 100, 100, 99, 96], [9, 30, 8, 1, 1, 1, 1], fork),
+             ([340, 338, 338, 101, 101, 101, 50], [3, 30, 50, 1, 0, 12, 1], fork), ([340, 340, 16, 101, 101, 101, 50], [800, 0, 0, 0, 0, 0, 0], fork),
+             ([20, 343, 343, 90, 102, 102, 0], [5, 1, 1, 0, 0, 0, 0], fork), ([0, 25, 25, 0, 90, 16, 90], [0, 3, 3, 0, 3, 3, 3], fork),
+             ([0, 28, 28, 0, 93, 19, 93], [0, 1, 1, 0, 1, 1, 1], [-1] * n), ([0] * n, [0] * n, [-1] * n)]
+    codes = []
+    for lens, new, parents in steps:
+        want = model.step(lens, new, parents, 500)
+        dev.step(lens, new, parents, 500)
+        dev.check(model, want, 500)
+        codes.append(want[0])
+    assert codes == [0, 0, 0, -4, 0, 0, 0, 0] and sorted(model.queue) == list(range(nb))
+
+
 def test_refused_steps_change_nothing():
     n, nb, bs, most = 4, 12, 16, 4
     model, dev = TablesModel(n, nb, bs, most), Device(n, nb, bs, most)
