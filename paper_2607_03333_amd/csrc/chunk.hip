@@ -1020,7 +1020,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       e.clear();
       const Pages pg{a.table + static_cast<size_t>(seq) * a.max_blocks, max(0, (sq.kv + BS - 1) / BS - 1), a.num_blocks};
       const int first = tok_lo + way * E::kTokens, stride = ways * E::kTokens;
-      const bool wide = kWide && row_tiles > kWaves / 2;
+      const bool wide = kWide && row_tiles > kWaves / 2 && tok_hi > tok_lo;  // rows with nothing to see: no stages
       const Bases at = E::bases(lane);
       int ent[E::kBlocks], ahead[E::kBlocks];  // blocks of the stage that is loaded next, and of the one behind it
       auto look_up = [&](int (&to)[E::kBlocks], int tb) __attribute__((always_inline)) {

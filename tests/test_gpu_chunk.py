@@ -95,11 +95,13 @@ def test_mixed_batches(dtype, hq, hkv, d, bs, new, kv):
     Case(dtype, hq, hkv, d, bs, new, kv, gap=16).run_and_check("mixed")
 
 
+@pytest.mark.parametrize("d", (64, 128))
 @pytest.mark.parametrize("dtype", (BF16, F32))
-@pytest.mark.parametrize("new,kv", [([20, 3], [5, 0]), ([300], [40]), ([1], [0]), ([64, 64], [63, 0]), ([700], [1])])
-def test_rows_with_nothing_to_see(dtype, new, kv):
+@pytest.mark.parametrize("new,kv", [([20, 3], [5, 0]), ([300], [40]), ([1], [0]), ([64, 64], [63, 0]), ([700], [1]),
+                                    ([257, 300], [0, 33])])
+def test_rows_with_nothing_to_see(dtype, new, kv, d):
     """More rows than positions: the first rows lie before the sequence's start."""
-    c = Case(dtype, 4, 2, 64, 16, new, kv)
+    c = Case(dtype, 4, 2, d, 16, new, kv)
     c.run()
     torch.cuda.synchronize()
     o, l = [], []
