@@ -50,8 +50,10 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kWaves = 8;
 constexpr int kDies = 8;
-// Cache policy of keys and values that one wave reads: non-temporal.
-constexpr int kStream = 2;
+// Cache policy of keys and values: non-temporal where one wave reads them, kept
+// where several row tiles do (24 prompts of up to 777 tokens with 16 heads of 64
+// channels, 78 us with non-temporal loads throughout, 69 without).
+constexpr int kStream = 2, kKeep = 0;
 constexpr float kSlack = 8.0f;    // base-2 headroom before the reference moves
 constexpr float kSlackSum = 256.0f;
 
@@ -284,6 +286,7 @@ struct Engine<__bf16, D, BS> {
 
   // K, or V, of the stage of the blocks `ent` (from their token `first`) into the
   // wave's slot.
+  template <int POLICY>
   static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[kBlocks], int head, int,
                                                  uint4* slot) {
     constexpr uint32_t kBytes = BS * D * 2;
@@ -295,9 +298,10 @@ struct Engine<__bf16, D, BS> {
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {  // tokens tk .. of the stage
       const int tk = 64 * k / kChunksPerToken;
-      load_lds<kStream>(from[tk / BS], kBytes, kl ^ (16u * kswz(tk)), 2 * (tk % BS) * D, slot + 64 * k);
+      load_lds<POLICY>(from[tk / BS], kBytes, kl ^ (16u * kswz(tk)), 2 * (tk % BS) * D, slot + 64 * k);
     }
   }
+  template <int POLICY>
   static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[kBlocks], int head, int,
                                                  uint4* slot) {
     constexpr uint32_t kBytes = BS * D * 2;
@@ -309,7 +313,7 @@ struct Engine<__bf16, D, BS> {
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {  // channels dk .. of a half, or of all 32 tokens
       const int dk = BS == 16 ? 64 * k % (kHalf / 2) / 2 : 16 * k;
-      load_lds<kStream>(from[BS == 16 ? 64 * k / (kHalf / 2) : 0], kBytes, vl ^ (16u * vswz(dk)), 2 * dk * BS,
+      load_lds<POLICY>(from[BS == 16 ? 64 * k / (kHalf / 2) : 0], kBytes, vl ^ (16u * vswz(dk)), 2 * dk * BS,
                         slot + kHalf + 64 * k);
     }
   }
@@ -463,6 +467,7 @@ struct Engine<float, D, BS> {
   static __device__ __forceinline__ const char* block(const ChunkArgs& a, const Pages& pg, const void* pool, int ent, int head) {
     return static_cast<const char*>(pool) + (static_cast<size_t>(pg.block(uniform(ent))) * a.hkv + head) * (BS * D * 4);
   }
+  template <int POLICY>
   static __device__ __forceinline__ void issue_k(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[1], int head, int first,
                                                  uint4* slot) {
     const char* from = block(a, pg, a.k_cache, ent[0], head);
@@ -470,16 +475,17 @@ struct Engine<float, D, BS> {
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
       const int tk = 64 * k / kChunksPerToken;
-      load_lds<kStream>(from, BS * D * 4, kl ^ (16u * kswz(tk)), 4 * (first + tk) * D, slot + 64 * k);
+      load_lds<POLICY>(from, BS * D * 4, kl ^ (16u * kswz(tk)), 4 * (first + tk) * D, slot + 64 * k);
     }
   }
+  template <int POLICY>
   static __device__ __forceinline__ void issue_v(const ChunkArgs& a, const Pages& pg, const Bases& x, const int (&ent)[1], int head, int first,
                                                  uint4* slot) {
     const char* from = block(a, pg, a.v_cache, ent[0], head);
     const uint32_t vl = anew(x.vload);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
-      load_lds<kStream>(from, BS * D * 4, vl, 4 * (16 * k * BS + first), slot + kHalf + 64 * k);
+      load_lds<POLICY>(from, BS * D * 4, vl, 4 * (16 * k * BS + first), slot + kHalf + 64 * k);
   }
 
   u32x4 kop[kDt], vop[kDt];
@@ -554,22 +560,20 @@ struct Engine<float, D, BS> {
 };
 
 // --------------------------------------------------------------------------
-// The wide path: bf16 tiles of more than 128 packed rows, head_dim 128. Each
-// wave owns one row tile of 32 and all of them share every 32-token stage (16
-// KB), which goes through a ring of eight in LDS; a barrier publishes two
-// stages at a time and frees the two that were read. The matrix cores bound a
-// stage (16 32x32x16 products per wave, 512 cycles, two waves to a SIMD), so
-// beside the softmax of stage s run the P.V products of stage s - 1 and the
-// scores of stage s + 1, one product and a few vector instructions at a time;
-// operand reads are spread over the slots likewise. The reads and barriers are
-// outside the compiler's view (it would wait for the loads of later stages at
-// every read), with waits that name the registers; no read is in flight where a
-// loop goes round.
+// The wide path: bf16 tiles of more than 128 packed rows. Each wave owns one row
+// tile of 32 and all of them share every 32-token stage (16 KB for 128 channels),
+// which goes through a ring of eight in LDS; a barrier publishes two stages at a
+// time and frees the two that were read. The matrix cores bound a stage (D / 8
+// 32x32x16 products per wave, 32 cycles each, two waves to a SIMD), so beside the
+// softmax of stage s run the P.V products of stage s - 1 and the scores of stage
+// s + 1, one product and a few vector instructions at a time; operand reads are
+// spread over the slots likewise. The reads and barriers are outside the
+// compiler's view (it would wait for the loads of later stages at every read),
+// with waits that name the registers; no read is in flight where a loop goes
+// round.
 // --------------------------------------------------------------------------
-constexpr int kStageChunks = 1024;   // 32 tokens x (K + V) x 128 channels x 2 bytes / 16
 constexpr int kRing = 8, kPer = 2;   // stages; stages that a barrier publishes
 constexpr int kAhead = kRing - kPer;
-constexpr int kStageLoads = 2;       // of a wave: the lower four load K, the upper four V
 
 __device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
@@ -581,12 +585,14 @@ struct Tile {
 };
 
 // A wave's loads of the shared stages: instruction k of wave w fills chunks
-// (2w + k) * 64 + lane of a stage, from one block, at a scalar base plus the
-// lane's fixed offset. The table goes through registers: lane i holds entry i of
-// the window of 64 that the loads are in, and of the next one.
-template <int BS>
+// (kStageLoads * w + k) * 64 + lane of a stage (the lower four waves K, the upper
+// four V), from one block, at a scalar base plus the lane's fixed offset. The
+// table goes through registers: lane i holds entry i of the window of 64 that the
+// loads are in, and of the next one.
+template <int D, int BS>
 struct RingLoader {
-  using E = Engine<__bf16, 128, BS>;
+  using E = Engine<__bf16, D, BS>;
+  static constexpr int kStageLoads = D / 64;
   static constexpr int kPerStage = 32 / BS;  // entries of a stage
   static constexpr int kWindow = 64 / kPerStage;  // stages of a window
   const char* pool;
@@ -611,13 +617,13 @@ struct RingLoader {
     for (int k = 0; k < kStageLoads; ++k) {
       const int chunk = (kStageLoads * wave + k) * 64 + lane;
       if (wave < 4) {
-        const int t = chunk >> 4;
-        off[k] = 2u * ((t % BS) * 128 + 8 * ((chunk & 15) ^ E::kswz(t)));
+        const int t = chunk / E::kChunksPerToken;
+        off[k] = 2u * ((t % BS) * D + 8 * ((chunk % E::kChunksPerToken) ^ E::kswz(t)));
       } else if (BS == 16) {
-        const int d = (chunk & 255) >> 1;
+        const int d = (chunk % (E::kHalf / 2)) >> 1;
         off[k] = 2u * (d * BS + 8 * ((chunk & 1) ^ E::vswz(d)));
       } else {
-        const int d = (chunk - 512) >> 2;
+        const int d = (chunk - E::kHalf) >> 2;
         off[k] = 2u * (d * BS + 8 * ((chunk & 3) ^ E::vswz(d)));
       }
     }
@@ -629,19 +635,25 @@ struct RingLoader {
   }
   __device__ __forceinline__ const char* block(int st) const {
     const int64_t e = pages.block(__builtin_amdgcn_readlane(now, st % kWindow * kPerStage + half));
-    return pool + (e * hkv + head) * (BS * 256);
+    return pool + (e * hkv + head) * (BS * D * 2);
   }
   __device__ __forceinline__ void load(const char* src, uint4* slot, int k) const {
-    load_lds<0>(src, BS * 256, off[k], 0, slot + (kStageLoads * wave + k) * 64);
+    load_lds<kKeep>(src, BS * D * 2, off[k], 0, slot + (kStageLoads * wave + k) * 64);
   }
 };
 
 // Every wave of the workgroup runs this for the same tile; on return e holds the
 // wave's row tile (nothing where wave * 32 >= n_packed), and its rows' loads are
 // done.
-template <int BS>
-__device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[kStageChunks],
-                                          int lane, int wave, Engine<__bf16, 128, BS>& e) {
+template <int D, int BS>
+__device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[D * 8], int lane,
+                                          int wave, Engine<__bf16, D, BS>& e) {
+  using E = Engine<__bf16, D, BS>;
+  using Loader = RingLoader<D, BS>;
+  constexpr int kStageLoads = Loader::kStageLoads;
+  constexpr int NP = D / 16;     // products of the scores, and of P.V: a slot each
+  constexpr int NCt = D / 32;
+  static_assert(2 * E::kHalf == D * 8, "a ring slot is a stage");
   const int r32 = lane & 31, g = lane >> 5;
   const bool owns = wave * 32 < w.n_packed;
   const int hmin = uniform(wave_min_int(e.hz[0]));
@@ -655,30 +667,25 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
   {
     const int t = 16 * (r32 >> 4) + 8 * ((r32 >> 2) & 1) + 4 * ((r32 >> 3) & 1) + (r32 & 3);
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      kaddr[s] = smem_base + 16u * (t * 16 + ((2 * s + g) ^ Engine<__bf16, 128, BS>::kswz(t)));
+    for (int s = 0; s < 4; ++s) kaddr[s] = smem_base + 16u * (t * E::kChunksPerToken + ((2 * s + g) ^ E::kswz(t)));
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      vaddr[h] = smem_base + 16u * (BS == 16 ? 512 + 256 * h + 2 * r32 + (g ^ Engine<__bf16, 128, BS>::vswz(r32))
-                                             : 512 + 4 * r32 + ((2 * h + g) ^ Engine<__bf16, 128, BS>::vswz(r32)));
+      vaddr[h] = smem_base + 16u * (E::kHalf + (BS == 16 ? E::kHalf / 2 * h + 2 * r32 + (g ^ E::vswz(r32))
+                                                         : 4 * r32 + ((2 * h + g) ^ E::vswz(r32))));
   }
-  auto slot_off = [&](int st) __attribute__((always_inline)) {
-    return static_cast<uint32_t>(st % kRing) * (kStageChunks * 16);
-  };
-  auto read_k = [&](u32x4 (&kr)[8], int s, uint32_t soff) __attribute__((always_inline)) {
+  auto slot_off = [&](int st) __attribute__((always_inline)) { return static_cast<uint32_t>(st % kRing) * (E::kHalf * 32); };
+  auto read_k = [&](u32x4 (&kr)[NP], int s, uint32_t soff) __attribute__((always_inline)) {
     kr[s] = lds_read_b128(s < 4 ? kaddr[s] + soff : (kaddr[s - 4] + soff) ^ 128u, 0);
   };
-  auto read_v = [&](u32x4 (&vr)[8], int i, uint32_t soff) __attribute__((always_inline)) {  // vr[4h + ct]
-    constexpr int kCt = BS == 16 ? 1024 : 2048;  // bytes between channel tiles; 16-token blocks: h 4 KB apart
-    const uint32_t va = vaddr[BS == 16 ? 0 : i >> 2] + soff;
-    const int step = BS == 16 ? i : i & 3;
-    vr[i] = lds_read_b128(va, step * kCt);
+  auto read_v = [&](u32x4 (&vr)[NP], int i, uint32_t soff) __attribute__((always_inline)) {  // vr[NCt * h + ct]
+    const int h = i / NCt, ct = i % NCt;
+    vr[i] = BS == 16 ? lds_read_b128(vaddr[0] + soff, E::kHalf * 8 * h + 1024 * ct) : lds_read_b128(vaddr[h] + soff, 2048 * ct);
   };
 
   {
     const int tb0 = w.tok_lo, tok_hi = w.tok_hi;
     const int nstage = (tok_hi - tb0 + 31) / 32;
-    RingLoader<BS> ld;
+    Loader ld;
     ld.init(a, pg, w.head, tb0, wave, lane);
     barrier_lds();  // the last tile's reads of the ring are done
     // Stages from here on hold positions outside the range or past a row's last.
@@ -687,9 +694,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
     struct State {
       f32x16 sc;       // scores of the stage
       uint32_t pw[8];  // probabilities of the stage before, as bf16 pairs
-      u32x4 vr[8];     // V of the stage before
+      u32x4 vr[NP];    // V of the stage before
     };
-    auto score_product = [&](f32x16& sc, int s, const u32x4 (&kr)[8]) __attribute__((always_inline)) {
+    auto score_product = [&](f32x16& sc, int s, const u32x4 (&kr)[NP]) __attribute__((always_inline)) {
       f32x16 acc;
       if (s == 0) {
 #pragma unroll
@@ -700,10 +707,10 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[s]), e.q[s], acc, 0, 0, 0);
     };
     auto pv_product = [&](int i, const State& x) __attribute__((always_inline)) {
-      const int h = 4 * (i >> 2);
-      o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+      const int h = 4 * (i / NCt), ct = i % NCt;
+      o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           __builtin_bit_cast(bf16x8, x.vr[i]),
-          __builtin_bit_cast(bf16x8, u32x4{x.pw[h], x.pw[h + 1], x.pw[h + 2], x.pw[h + 3]}), o[i & 3], 0, 0, 0);
+          __builtin_bit_cast(bf16x8, u32x4{x.pw[h], x.pw[h + 1], x.pw[h + 2], x.pw[h + 3]}), o[ct], 0, 0, 0);
     };
     // The pair of stages a publish makes room for, loaded until the next one.
     // Behind the last stage these are loads of blocks that nothing reads: so the
@@ -720,7 +727,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
     // and the barrier says so of every wave's), stages up to st - 1 are no longer
     // read. LOAD: first of the two loads issued here.
     auto stage = [&](auto owns_c, auto first_c, auto last_c, auto publish_c, auto load_c, int st, State& x,
-                     u32x4 (&kr)[8]) __attribute__((always_inline)) {
+                     u32x4 (&kr)[NP]) __attribute__((always_inline)) {
       constexpr bool OWNS = decltype(owns_c)::value, FIRST = decltype(first_c)::value;
       constexpr bool LAST = decltype(last_c)::value, PUBLISH = decltype(publish_c)::value;
       constexpr int LOAD = decltype(load_c)::value;
@@ -728,19 +735,19 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         wait_vmcnt<3 * kStageLoads>();
         barrier_only();
         st_load = st + kAhead;
-        if (st_load % RingLoader<BS>::kWindow == 0) ld.enter(st_load);
+        if (st_load % Loader::kWindow == 0) ld.enter(st_load);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) src[i] = ld.block(st_load + i);
       }
       if constexpr (!OWNS) {
         if constexpr (LOAD >= 0) {
-          load(LOAD);
-          load(LOAD + 1);
+#pragma unroll
+          for (int i = 0; i < kStageLoads; ++i) load(LOAD + i);
         }
       } else {
-        // 16 slots of one product each: 0-7 the P.V of the stage before, 8-15 the
-        // scores of the stage after. The steps of an element (scale, exponential,
-        // sum, conversion) lie one or more slots apart so that none waits.
+        // 2 NP slots of one product each: the first half the P.V of the stage before,
+        // the second the scores of the stage after. The steps of an element (scale,
+        // exponential, sum, conversion) lie one or more slots apart so that none waits.
         float sv[16], ex[16], pv[16], ps = 0.0f;
         uint32_t pw[8];
 #pragma unroll
@@ -752,29 +759,33 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         }
         const float nm = -m;
         const uint32_t k_off = slot_off(st + 1), v_off = slot_off(st);
+        // The slot that scales element i; its sum and conversion follow kLag later.
+        constexpr int kLag = NP == 8 ? 3 : 2;
+        auto slot_of = [](int i) { return 3 * i * NP / 32; };
+        // Slots between the read of a K operand and its product, and the LDS reads
+        // issued since at the wait for it. (Read as late as this, the operands of K
+        // and V fit the registers together.)
+        constexpr int kLate = NP == 8 ? 3 : 2, kFirstV = NP == 8 ? 6 : 3;
+        constexpr int kSince[8] = {NP == 8 ? 4 : 2, NP == 8 ? 5 : 3, NP == 8 ? 5 : 3, NP == 8 ? 5 : 2, 5, 5, 4, 2};
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-          if (!FIRST && t < 8) pv_product(t, x);
-          if (!LAST && t >= 8) {
-            // K operand t - 8, read three slots ago: all LDS reads but those issued
-            // since. (Read as late as this, the operands of K and V fit the registers
-            // together.)
-            constexpr int kSince[8] = {4, 5, 5, 5, 5, 5, 4, 2};
-            lds_wait(kr[t - 8], kSince[t - 8]);
-            score_product(x.sc, t - 8, kr);
+        for (int t = 0; t < 2 * NP; ++t) {
+          if (!FIRST && t < NP) pv_product(t, x);
+          if (!LAST && t >= NP) {
+            lds_wait(kr[t - NP], kSince[t - NP]);
+            score_product(x.sc, t - NP, kr);
           }
-          if (!LAST && t >= 5 && t < 13) read_k(kr, t - 5, k_off);
-          if (t >= 6 && t < 14) read_v(x.vr, t - 6, v_off);
+          if (!LAST && t >= NP - kLate && t < 2 * NP - kLate) read_k(kr, t - (NP - kLate), k_off);
+          if (t >= kFirstV && t < NP + kFirstV) read_v(x.vr, t - kFirstV, v_off);
           if (LOAD >= 0 && t % 8 == 4) load(LOAD + t / 8);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            if (t == 3 * i / 4) ex[i] = __builtin_fmaf(sv[i], c, nm);
-            if (t == 3 * i / 4 + 1) pv[i] = exp2_fast(ex[i]);
-            if (t == 3 * i / 4 + 3) ps += pv[i];
+            if (t == slot_of(i)) ex[i] = __builtin_fmaf(sv[i], c, nm);
+            if (t == slot_of(i) + 1) pv[i] = exp2_fast(ex[i]);
+            if (t == slot_of(i) + kLag) ps += pv[i];
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            if (t == 3 * (2 * i + 1) / 4 + 3) {
+            if (t == slot_of(2 * i + 1) + kLag) {
               pw[i] = pack2(pv[2 * i], pv[2 * i + 1]);
               asm volatile("" : "+v"(pw[i]));  // here, not behind the branch below
             }
@@ -790,7 +801,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
             const float alpha = exp2_fast(m - mx);
             l *= alpha;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] *= alpha;
+            for (int i = 0; i < NCt; ++i) o[i] *= alpha;
             m = mx;
           }
           const float ref = m == kNegInf ? 0.0f : m;
@@ -810,11 +821,10 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
           const int tb = tb0 + st * 32;
           if (tb + 32 > tok_hi) {  // what lies behind the end may be anything: 0 * NaN
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              x.vr[i] = Engine<__bf16, 128, BS>::zero_past(x.vr[i], tb + 16 * (i >> 2) + 8 * g, tok_hi);
+            for (int i = 0; i < NP; ++i) x.vr[i] = E::zero_past(x.vr[i], tb + 16 * (i / NCt) + 8 * g, tok_hi);
           }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) pv_product(i, x);
+          for (int i = 0; i < NP; ++i) pv_product(i, x);
         }
       }
     };
@@ -842,17 +852,17 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       constexpr std::false_type no{};
       constexpr std::integral_constant<int, -1> none{};
       constexpr std::integral_constant<int, 0> load0{};
-      constexpr std::integral_constant<int, 2> load2{};
+      constexpr std::integral_constant<int, kStageLoads> load1{};  // the second stage's
       State x;
-      u32x4 kr[8];
+      u32x4 kr[NP];
       wait_vmcnt<(kAhead - 1) * kStageLoads>();
       barrier_only();  // stage 0 is readable
       if constexpr (OWNS) {
 #pragma unroll
-        for (int s = 0; s < 8; ++s) read_k(kr, s, 0);
+        for (int s = 0; s < NP; ++s) read_k(kr, s, 0);
         lds_wait(kr);
 #pragma unroll
-        for (int s = 0; s < 8; ++s) score_product(x.sc, s, kr);
+        for (int s = 0; s < NP; ++s) score_product(x.sc, s, kr);
       }
       if (nstage == 1) {
         stage(owns_c, yes, yes, no, none, 0, x, kr);
@@ -860,7 +870,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
         stage(owns_c, yes, no, yes, load0, 0, x, kr);
         int st = 0;  // the last stage done
         while (st + 3 < nstage) {
-          stage(owns_c, no, no, no, load2, st + 1, x, kr);
+          stage(owns_c, no, no, no, load1, st + 1, x, kr);
           stage(owns_c, no, no, yes, load0, st + 2, x, kr);
           st += 2;
         }
@@ -963,7 +973,7 @@ template <typename T, int D, int BS>
 __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
   using E = Engine<T, D, BS>;
   constexpr int kFloat4s = D / 8;  // of a lane's accumulator
-  constexpr bool kWide = std::is_same_v<T, __bf16> && D == 128;
+  constexpr bool kWide = std::is_same_v<T, __bf16>;
   __shared__ __align__(256) uint4 smem[kWaves][2 * E::kHalf];  // a slot for each wave; wide: the ring
   __shared__ float2 ml[kWaves][32];
   __shared__ int64_t wave_sum[kWaves];
@@ -1027,11 +1037,20 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 #pragma unroll
         for (int b = 0; b < E::kBlocks; ++b) to[b] = pg.entry(tb / BS + b);
       };
+      const bool alone = row_tiles == 1;
+      auto issue_k = [&](int off) __attribute__((always_inline)) {
+        if (alone) E::template issue_k<kStream>(a, pg, at, ent, head, off, smem[wave]);
+        else E::template issue_k<kKeep>(a, pg, at, ent, head, off, smem[wave]);
+      };
+      auto issue_v = [&](int off) __attribute__((always_inline)) {
+        if (alone) E::template issue_v<kStream>(a, pg, at, ent, head, off, smem[wave]);
+        else E::template issue_v<kKeep>(a, pg, at, ent, head, off, smem[wave]);
+      };
       if (!wide && works && first < tok_hi) {
         look_up(ent, first);
         look_up(ahead, first + stride);
-        E::issue_k(a, pg, at, ent, head, first % BS, smem[wave]);
-        E::issue_v(a, pg, at, ent, head, first % BS, smem[wave]);
+        issue_k(first % BS);
+        issue_v(first % BS);
       }
       int least = INT_MAX;
       const bool second = E::kUnits == 1 || n_packed - 32 * rt > 16;
@@ -1049,7 +1068,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const float c = a.scale_log2;
       if (wide) {
         if constexpr (kWide)
-          wide_tile<BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, lane, wave, e);
+          wide_tile<D, BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, lane, wave, e);
         barrier_lds();  // the ring is read: a wave may load its slot for the next tile
       } else if (works) {
         // K and V of a stage are loaded as soon as the slot's halves have been read:
@@ -1066,12 +1085,12 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           for (int b = 0; b < E::kBlocks; ++b) ent[b] = ahead[b];
           look_up(ahead, tb + 2 * stride);
           asm volatile("" ::: "memory");
-          if (more) E::issue_k(a, pg, at, ent, head, (tb + stride) % BS, smem[wave]);
+          if (more) issue_k((tb + stride) % BS);
           e.softmax(tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second);
           if (more) wait_vmcnt<E::kLoads>();
           else wait_vmcnt<0>();
           e.read_v(slot, at);
-          if (more) E::issue_v(a, pg, at, ent, head, (tb + stride) % BS, smem[wave]);
+          if (more) issue_v((tb + stride) % BS);
           e.values(tb, tok_hi, lane, second);
         }
       }
