@@ -1026,6 +1026,10 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const int unit = wave % units, way = wave / units;
       const int head = head0 + unit / row_tiles, rt = unit % row_tiles;
       const bool works = way < ways;  // wide: every wave loads, those with a row tile compute
+      // The tokens of the piece that the wave's row tile sees end here. (Three fp32
+      // prompts of up to 200 rows, 2 KV heads of 64: 35 us where every wave went on to the
+      // piece's end, 31 so. A wide tile's waves stay together: it brought them nothing.)
+      const int seen = works ? min(tok_hi, sq.kv - sq.rows + r0 + (min(32 * rt + 32, n_packed) - 1) / group + 1) : 0;
       E e;
       e.clear();
       const Pages pg{a.table + static_cast<size_t>(seq) * a.max_blocks, max(0, (sq.kv + BS - 1) / BS - 1), a.num_blocks};
@@ -1046,7 +1050,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
         if (alone) E::template issue_v<kStream>(a, pg, at, ent, head, off, smem[wave]);
         else E::template issue_v<kKeep>(a, pg, at, ent, head, off, smem[wave]);
       };
-      if (!wide && works && first < tok_hi) {
+      if (!wide && first < seen) {
         look_up(ent, first);
         look_up(ahead, first + stride);
         issue_k(first % BS);
@@ -1077,8 +1081,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
         // make a wait longer.)
         const uint32_t slot = lds_addr(smem[wave]);
         e.settle_q();
-        for (int tb = first; tb < tok_hi; tb += stride) {
-          const bool more = tb + stride < tok_hi;
+        for (int tb = first; tb < seen; tb += stride) {
+          const bool more = tb + stride < seen;
           wait_vmcnt<E::kLoads>();
           e.read_k(slot, at);  // (waited for: the half may be written again)
 #pragma unroll
