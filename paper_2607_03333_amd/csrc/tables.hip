@@ -283,8 +283,10 @@ __device__ __forceinline__ void sum_here(const TablesArgs& a, int s, Sums* befor
   }
 }
 
-__device__ __forceinline__ int ring(const TablesArgs& a, int front, int64_t nth) {
-  return static_cast<int>((front + nth) % a.num_blocks);
+// Place in the ring of the nth entry (at most num_blocks) from the front.
+__device__ __forceinline__ int ring(const TablesArgs& a, int front, int nth) {
+  const uint32_t at = static_cast<uint32_t>(front) + static_cast<uint32_t>(nth), n = static_cast<uint32_t>(a.num_blocks);
+  return static_cast<int>(at >= n ? at - n : at);
 }
 
 // kSummed: by tables_sum.
@@ -353,7 +355,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
         if (w < wave) rank += freed[q][w];
         at += freed[q][w];
       }
-      if (here[q]) a.free_queue[ring(a, front, static_cast<int64_t>(count) + rank)] = x.was[q];
+      if (here[q]) a.free_queue[ring(a, front, count + rank)] = x.was[q];
     }
     __syncthreads();  // the counts are read
   }
@@ -389,13 +391,13 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
     }
     const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
     const int c = a.copy_off[s];
-    int64_t first = a.take_off[s];
+    int first = a.take_off[s];
     if (c >= 0) {
       if (tid == 0) {
         const int dst = a.free_queue[ring(a, front, first)];
         atomicAdd(a.refcount + a.copies[3 * c], -1);
         a.copies[3 * c + 1] = dst;
-        a.refcount[dst] = 1;
+        if (in_pool(a, dst)) a.refcount[dst] = 1;
         a.table[place(a, s, len / bs)] = dst;
       }
       ++first;
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
     for (int j = keep + tid; j < to; j += kRowThreads) {
       const int b = a.free_queue[ring(a, front, first + j - keep)];
       a.table[place(a, s, j)] = b;
-      a.refcount[b] = 1;
+      if (in_pool(a, b)) a.refcount[b] = 1;  // (the queue's contents are the caller's)
     }
     if (tid == 0) {
       a.held[s] = to;
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
     const int s = lo, len = a.lens[s], keep = blocks_of(len, bs), c = a.copy_off[s];
     pos = len + i - a.row_off[s];
     const int col = pos / bs;
-    const int64_t first = a.take_off[s] + (c >= 0 ? 1 : 0);
+    const int first = a.take_off[s] + (c >= 0 ? 1 : 0);
     int b;
     if (col >= keep) b = a.free_queue[ring(a, front, first + col - keep)];
     else if (c >= 0) b = a.free_queue[ring(a, front, first - 1)];

@@ -280,3 +280,27 @@ def test_copy_batch(dtype, hkv, d, bs):
     count.fill_(-1)
     spork.spork_kv_copy_batch(shape, dk, dv, nb, copies, count)
     assert torch.equal(dk.cpu(), k) and torch.equal(dv.cpu(), v)
+
+
+def test_a_queue_of_other_numbers_stays_inside_the_buffers():
+    """Free-queue entries that are no blocks: they come out as they went in, and nothing beside the references changes."""
+    for n, max_tokens in ((3, 200), (70, 6000)):
+        nb, bs, most = 64, 16, 8
+        ints = lambda *m: torch.full(m, -77, dtype=torch.int32, device="cuda")  # noqa: E731
+        guarded = ints(nb + 2 * 4096)  # references in the middle
+        dev = Device(n, nb, bs, most)
+        dev.refs = guarded[4096:4096 + nb]
+        dev.t = spork.make_tables(bs, dev.table, dev.held, dev.refs, dev.ring, dev.queue)
+        spork.spork_tables_init(dev.t)
+        odd = [-1, nb, nb + 4000, -4000, 5, 6, -(1 << 20), nb + 1]
+        dev.ring[:8] = torch.tensor(odd, dtype=torch.int32)
+        dev.step([0] * n, [100, 20] + [0] * (n - 2), None, max_tokens)
+        assert dev.status.item() == 0 and dev.queue.tolist() == [9, nb - 9]
+        assert dev.table[0, :7].tolist() == odd[:7] and dev.table[1, :2].tolist() == [odd[7], 8]
+        assert dev.slots[:100].tolist() == [odd[i // bs] * bs + i % bs for i in range(100)]
+        assert dev.refs.tolist() == [1 if i in (5, 6, 8) else 0 for i in range(nb)]
+        assert (guarded[:4096] == -77).all() and (guarded[4096 + nb:] == -77).all()
+        # rows with such entries are refused when they are released
+        dev.step([0] * n, [0] * n, [-1] * n, max_tokens)
+        assert dev.status.item() == spork.SPORK_E_INVAL and dev.refs.tolist() == [1 if i in (5, 6, 8) else 0 for i in range(nb)]
+        assert (guarded[:4096] == -77).all() and (guarded[4096 + nb:] == -77).all()
