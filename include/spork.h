@@ -459,8 +459,9 @@ int spork_tables_workspace_clear(const spork_tables* tables, void* workspace, si
  * The tables' own consistency (refcounts, queue contents) is not checked;
  * a bad one never reads or writes outside the buffers.
  * workspace (device, 256-byte aligned; words zero on entry, see above; steps
- * that share it must not overlap). Four launches, or five for many rows. Same inputs, same tables:
- * no result depends on the order of atomics. */
+ * that share it must not overlap). Four launches, or five for many rows; one
+ * for up to 16 rows of up to 512 blocks and up to 4,096 new tokens. Same
+ * inputs, same tables: no result depends on the order of atomics. */
 int spork_tables_step(const spork_tables* tables, const int32_t* lens, const int32_t* n_new,
                       const int32_t* parents, int32_t max_tokens, int64_t* slots, int32_t* positions,
                       int32_t* row_off, int32_t* kv_len, int32_t* copies, int32_t* n_copies,

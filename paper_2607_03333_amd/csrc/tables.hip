@@ -27,7 +27,8 @@
 // is refused. A workgroup per row, and four entries of its row in flight per
 // thread: a fork or the end of a long row is thousands of entries. Up to
 // kRowsSummedByAll rows every workgroup of release sums what it needs by itself;
-// more are summed once, by a launch between.
+// more are summed once, by a launch between. Few short rows go through the same
+// phases in one workgroup and one launch (tables_one), a row to a wave.
 #include "device_common.h"
 #include "spork.h"
 #include "tables_kernels.h"
@@ -40,6 +41,15 @@ constexpr int kRowThreads = 256;   // of a row's workgroup
 constexpr int kSumThreads = 1024;  // of the one workgroup that sums the rows
 constexpr int kAtOnce = 4;         // entries of a row that a thread loads together
 constexpr int kRowsSummedByAll = 1024;
+// Steps of one workgroup: at most so many rows (a wave each), entries of a row,
+// and new tokens. Half of the rows forking again, eager and in a graph, one launch
+// against four: 1 row 9.0 and 8.2 us against 16.0 and 9.3; 8 rows of 250 tokens 12.3
+// and 12.6 against 16.9 and 15.1; 16 rows 14.1 and 14.3 against 17.1 and 14.8; 16 rows
+// of 500 blocks 14.3 and 14.6 against 17.1 and 13.4, of 1,000 blocks 19.1 and 19.4
+// against 17.1 and 13.5; 4,096 new tokens 11.6 and 11.9 against 17.0 and 13.0.
+constexpr int kOneThreads = 1024;
+constexpr int kOneRows = 16, kOneEntries = 512, kOneTokens = 4096;
+static_assert(kOneRows * 64 == kOneThreads, "a wave for every row");
 
 struct Row {
   int len, grow, parent, held;
@@ -95,12 +105,17 @@ struct Changes {
 };
 __device__ __forceinline__ int changes_lo(const Row& r) { return r.release_lo; }
 __device__ __forceinline__ int changes_hi(const Row& r) { return r.parent >= 0 ? max(r.held, r.keep) : r.held; }
-__device__ __forceinline__ int column(int j0, int q) { return j0 + q * kRowThreads + static_cast<int>(threadIdx.x); }
+// kTeam: threads that work on a row, a workgroup or a wave.
+template <int kTeam>
+__device__ __forceinline__ int column(int j0, int q) {
+  return j0 + q * kTeam + static_cast<int>(threadIdx.x % kTeam);
+}
+template <int kTeam>
 __device__ __forceinline__ Changes changes(const TablesArgs& a, int s, const Row& r, int j0) {
   Changes x;
 #pragma unroll
   for (int q = 0; q < kAtOnce; ++q) {
-    const int j = column(j0, q);
+    const int j = column<kTeam>(j0, q);
     x.loses[q] = j < r.held;
     x.gains[q] = r.parent >= 0 && j < r.keep;
     x.was[q] = x.loses[q] ? a.table[place(a, s, j)] : -1;
@@ -115,46 +130,78 @@ __device__ __forceinline__ Changes changes(const TablesArgs& a, int s, const Row
   return x;
 }
 
+// References and last places of a row's changes; the status of its entries.
+template <int kTeam>
+__device__ __forceinline__ int count_row(const TablesArgs& a, int s, const Row& r) {
+  int err = SPORK_OK;
+  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
+    const Changes x = changes<kTeam>(a, s, r, j0);
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      if (x.gains[q]) {
+        if (in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], 1);
+        else err = SPORK_E_INVAL;
+      }
+      if (x.loses[q]) {
+        if (in_pool(a, x.was[q])) {
+          atomicAdd(a.refcount + x.was[q], -1);
+          atomicMax(a.last_release + x.was[q], static_cast<int>(place(a, s, column<kTeam>(j0, q))) + 1);
+        } else {
+          err = SPORK_E_INVAL;
+        }
+      }
+    }
+  }
+  if (threadIdx.x % kTeam == 0 && r.grow != 0 && r.len % a.block_size != 0) {
+    const int b = shared_tail(a, r);
+    if (in_pool(a, b)) {
+      atomicAdd(a.sharers + b, 1);
+      atomicMax(a.last_sharer + b, s + 1);
+    } else {
+      err = SPORK_E_INVAL;
+    }
+  }
+  return err;
+}
+
 __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
   const int s = blockIdx.x;
   if (s == 0 && threadIdx.x == 0) a.totals->front = a.queue[0];
   Row r;
   int err = read_row(a, s, &r);
-  if (err == SPORK_OK) {
-    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
-      const Changes x = changes(a, s, r, j0);
-#pragma unroll
-      for (int q = 0; q < kAtOnce; ++q) {
-        if (x.gains[q]) {
-          if (in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], 1);
-          else err = SPORK_E_INVAL;
-        }
-        if (x.loses[q]) {
-          if (in_pool(a, x.was[q])) {
-            atomicAdd(a.refcount + x.was[q], -1);
-            atomicMax(a.last_release + x.was[q], static_cast<int>(place(a, s, column(j0, q))) + 1);
-          } else {
-            err = SPORK_E_INVAL;
-          }
-        }
-      }
-    }
-    if (threadIdx.x == 0 && r.grow != 0 && r.len % a.block_size != 0) {
-      const int b = shared_tail(a, r);
-      if (in_pool(a, b)) {
-        atomicAdd(a.sharers + b, 1);
-        atomicMax(a.last_sharer + b, s + 1);
-      } else {
-        err = SPORK_E_INVAL;
-      }
-    }
-  }
+  if (err == SPORK_OK) err = count_row<kRowThreads>(a, s, r);
   if (err != SPORK_OK) atomicMin(&a.totals->error, err);
 }
 
 // Whether place (s, j) is the one that frees block b.
 __device__ __forceinline__ bool frees_block(const TablesArgs& a, int s, int j, int b) {
   return in_pool(a, b) && a.last_release[b] == static_cast<int>(place(a, s, j)) + 1 && a.refcount[b] == 0;
+}
+
+// Whether row s, which appends inside a block, copies it.
+__device__ __forceinline__ int copies_tail(const TablesArgs& a, int s, const Row& r) {
+  const int b = shared_tail(a, r);
+  if (!in_pool(a, b)) return 0;
+  const int refs = a.refcount[b];
+  return refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
+}
+
+// Blocks that the thread's entries of row s free, summed over its wave.
+template <int kTeam>
+__device__ __forceinline__ int wave_frees(const TablesArgs& a, int s, const Row& r) {
+  int frees = 0;
+  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
+    const Changes x = changes<kTeam>(a, s, r, j0);
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) frees += x.loses[q] && frees_block(a, s, column<kTeam>(j0, q), x.was[q]);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o /= 2) frees += __shfl_xor(frees, o);
+  return frees;
+}
+
+__device__ __forceinline__ int row_takes(const TablesArgs& a, const Row& r, int copies) {
+  return copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
 }
 
 __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
@@ -165,23 +212,10 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
     if (tid == 0) a.frees[s] = a.takes[s] = a.copies_of[s] = 0;
     return;
   }
-  int copies = 0;
-  if (tid == 0) {
-    const int b = shared_tail(a, r);
-    if (in_pool(a, b)) {
-      const int refs = a.refcount[b];
-      copies = refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
-    }
-  }
+  const int copies = tid == 0 ? copies_tail(a, s, r) : 0;
   int frees = 0;
   if (changes_lo(r) < changes_hi(r)) {
-    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
-      const Changes x = changes(a, s, r, j0);
-#pragma unroll
-      for (int q = 0; q < kAtOnce; ++q) frees += x.loses[q] && frees_block(a, s, column(j0, q), x.was[q]);
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o /= 2) frees += __shfl_xor(frees, o);
+    frees = wave_frees<kRowThreads>(a, s, r);
     if ((tid & 63) == 0) freed[tid >> 6] = frees;
     __syncthreads();
     frees = 0;
@@ -190,7 +224,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
   }
   if (tid == 0) {
     a.frees[s] = frees;
-    a.takes[s] = copies + blocks_of(static_cast<int64_t>(r.len) + r.grow, a.block_size) - r.keep;
+    a.takes[s] = row_takes(a, r, copies);
     a.copies_of[s] = copies;
   }
 }
@@ -289,11 +323,81 @@ __device__ __forceinline__ int ring(const TablesArgs& a, int front, int nth) {
   return static_cast<int>(at >= n ? at - n : at);
 }
 
+// Row s of a refused step: its references back, its words clear.
+template <int kTeam>
+__device__ __forceinline__ void undo_row(const TablesArgs& a, int s, const Row& r) {
+  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
+    const Changes x = changes<kTeam>(a, s, r, j0);
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      if (x.gains[q] && in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], -1);
+      if (x.loses[q] && in_pool(a, x.was[q])) {
+        atomicAdd(a.refcount + x.was[q], 1);
+        a.last_release[x.was[q]] = 0;
+      }
+    }
+  }
+  if (threadIdx.x % kTeam == 0) {
+    const int b = shared_tail(a, r);
+    if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
+  }
+}
+
+// The frees of row s into the queue, behind `at` others, and a forked row's
+// entries; its copy's entry (c: index of it, or -1).
+template <int kTeam>
+__device__ __forceinline__ void release_row(const TablesArgs& a, int s, const Row& r, int at, int c, int front, int count) {
+  constexpr int kTeamWaves = kTeam / 64;
+  __shared__ int freed[kAtOnce][kTeamWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x % kTeam >> 6;
+  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
+    const Changes x = changes<kTeam>(a, s, r, j0);
+    bool here[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) here[q] = x.loses[q] && frees_block(a, s, column<kTeam>(j0, q), x.was[q]);
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int place1 = static_cast<int>(place(a, s, column<kTeam>(j0, q))) + 1;
+      // The last place alone clears the word: any other compares unequal before and after.
+      if (x.loses[q] && a.last_release[x.was[q]] == place1) a.last_release[x.was[q]] = 0;
+      if (x.gains[q]) a.table[place1 - 1] = x.now[q];  // (this thread alone reads the column)
+      if constexpr (kTeamWaves > 1) {
+        const uint64_t bal = __ballot(here[q]);
+        if (lane == 0) freed[q][wave] = __popcll(bal);
+      }
+    }
+    if constexpr (kTeamWaves > 1) __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const uint64_t bal = __ballot(here[q]);
+      int rank = at + __popcll(bal & ((uint64_t{1} << lane) - 1));
+      if constexpr (kTeamWaves > 1) {
+#pragma unroll
+        for (int w = 0; w < kTeamWaves; ++w) {
+          if (w < wave) rank += freed[q][w];
+          at += freed[q][w];
+        }
+      } else {
+        at += __popcll(bal);
+      }
+      if (here[q]) a.free_queue[ring(a, front, count + rank)] = x.was[q];
+    }
+    if constexpr (kTeamWaves > 1) __syncthreads();  // the counts are read
+  }
+  if (threadIdx.x % kTeam == 0) {
+    const int b = shared_tail(a, r);
+    if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
+    if (c >= 0) {
+      a.copies[3 * c] = b;
+      a.copies[3 * c + 2] = r.len % a.block_size;
+    }
+  }
+}
+
 // kSummed: by tables_sum.
 template <bool kSummed>
 __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
-  __shared__ int freed[kAtOnce][kRowThreads / 64];
-  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int s = blockIdx.x, tid = threadIdx.x;
   const int front = a.queue[0], count = a.queue[1];
   int at, c, status;  // the row's freed blocks among all, its copy or -1
   if constexpr (kSummed) {
@@ -314,63 +418,53 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
   }
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) return;
-  if (status != SPORK_OK) {  // as it was: references back, words clear
-    for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
-      const Changes x = changes(a, s, r, j0);
-#pragma unroll
-      for (int q = 0; q < kAtOnce; ++q) {
-        if (x.gains[q] && in_pool(a, x.now[q])) atomicAdd(a.refcount + x.now[q], -1);
-        if (x.loses[q] && in_pool(a, x.was[q])) {
-          atomicAdd(a.refcount + x.was[q], 1);
-          a.last_release[x.was[q]] = 0;
-        }
-      }
-    }
+  if (status != SPORK_OK) undo_row<kRowThreads>(a, s, r);
+  else release_row<kRowThreads>(a, s, r, at, c, front, count);
+}
+
+// The fronts of row s, from the queue's nth on, into its table; its references
+// and length (c as above).
+template <int kTeam>
+__device__ __forceinline__ void assign_row(const TablesArgs& a, int s, int front, int nth, int c) {
+  const int tid = threadIdx.x % kTeam, bs = a.block_size;
+  const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
+  if (c >= 0) {
     if (tid == 0) {
-      const int b = shared_tail(a, r);
-      if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
+      const int dst = a.free_queue[ring(a, front, nth)];
+      atomicAdd(a.refcount + a.copies[3 * c], -1);
+      a.copies[3 * c + 1] = dst;
+      if (in_pool(a, dst)) a.refcount[dst] = 1;
+      a.table[place(a, s, len / bs)] = dst;
     }
-    return;
+    ++nth;
   }
-  for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kRowThreads) {
-    const Changes x = changes(a, s, r, j0);
-    bool here[kAtOnce];
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) here[q] = x.loses[q] && frees_block(a, s, column(j0, q), x.was[q]);
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) {
-      const int place1 = static_cast<int>(place(a, s, column(j0, q))) + 1;
-      // The last place alone clears the word: any other compares unequal before and after.
-      if (x.loses[q] && a.last_release[x.was[q]] == place1) a.last_release[x.was[q]] = 0;
-      if (x.gains[q]) a.table[place1 - 1] = x.now[q];  // (this thread alone reads the column)
-      const uint64_t bal = __ballot(here[q]);
-      if (lane == 0) freed[q][wave] = __popcll(bal);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) {
-      int rank = at + __popcll(__ballot(here[q]) & ((uint64_t{1} << lane) - 1));
-#pragma unroll
-      for (int w = 0; w < kRowThreads / 64; ++w) {
-        if (w < wave) rank += freed[q][w];
-        at += freed[q][w];
-      }
-      if (here[q]) a.free_queue[ring(a, front, count + rank)] = x.was[q];
-    }
-    __syncthreads();  // the counts are read
+  for (int j = keep + tid; j < to; j += kTeam) {
+    const int b = a.free_queue[ring(a, front, nth + j - keep)];
+    a.table[place(a, s, j)] = b;
+    if (in_pool(a, b)) a.refcount[b] = 1;  // (the queue's contents are the caller's)
   }
   if (tid == 0) {
-    const int b = shared_tail(a, r);
-    if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
-    if (c >= 0) {
-      a.copies[3 * c] = b;
-      a.copies[3 * c + 2] = r.len % a.block_size;
-    }
+    a.held[s] = to;
+    a.kv_len[s] = end;
   }
 }
 
+// Slot and position of the nth new token of row s: its block from the queue or,
+// in front of the row's first new block, from the tail or its copy.
+__device__ __forceinline__ int64_t slot_of(const TablesArgs& a, int s, int len, int nth, int front, int take_off, int c,
+                                          int* pos) {
+  const int bs = a.block_size, keep = blocks_of(len, bs);
+  *pos = len + nth;
+  const int col = *pos / bs;
+  int b;
+  if (col >= keep) b = a.free_queue[ring(a, front, take_off + (c >= 0 ? 1 : 0) + col - keep)];
+  else if (c >= 0) b = a.free_queue[ring(a, front, take_off)];
+  else b = a.table[place(a, s, col)];
+  return static_cast<int64_t>(b) * bs + *pos % bs;
+}
+
 __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
-  const int tid = threadIdx.x, bs = a.block_size;
+  const int tid = threadIdx.x;
   const int status = a.totals->status, front = a.totals->front;
   if (static_cast<int>(blockIdx.x) < a.n_seqs) {  // a row: its table and references
     const int s = blockIdx.x;
@@ -389,32 +483,10 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
       }
       return;
     }
-    const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
-    const int c = a.copy_off[s];
-    int first = a.take_off[s];
-    if (c >= 0) {
-      if (tid == 0) {
-        const int dst = a.free_queue[ring(a, front, first)];
-        atomicAdd(a.refcount + a.copies[3 * c], -1);
-        a.copies[3 * c + 1] = dst;
-        if (in_pool(a, dst)) a.refcount[dst] = 1;
-        a.table[place(a, s, len / bs)] = dst;
-      }
-      ++first;
-    }
-    for (int j = keep + tid; j < to; j += kRowThreads) {
-      const int b = a.free_queue[ring(a, front, first + j - keep)];
-      a.table[place(a, s, j)] = b;
-      if (in_pool(a, b)) a.refcount[b] = 1;  // (the queue's contents are the caller's)
-    }
-    if (tid == 0) {
-      a.held[s] = to;
-      a.kv_len[s] = end;
-    }
+    assign_row<kRowThreads>(a, s, front, a.take_off[s], a.copy_off[s]);
     return;
   }
-  // a token: its row by search in the offsets, its block from the queue or, in
-  // front of the row's first new block, from the tail or its copy
+  // a token: its row by search in the offsets
   const int i = (static_cast<int>(blockIdx.x) - a.n_seqs) * kRowThreads + tid;
   if (i >= a.max_tokens) return;
   int64_t slot = -1;
@@ -426,18 +498,104 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
       if (a.row_off[mid] <= i) lo = mid;
       else hi = mid - 1;
     }
-    const int s = lo, len = a.lens[s], keep = blocks_of(len, bs), c = a.copy_off[s];
-    pos = len + i - a.row_off[s];
-    const int col = pos / bs;
-    const int first = a.take_off[s] + (c >= 0 ? 1 : 0);
-    int b;
-    if (col >= keep) b = a.free_queue[ring(a, front, first + col - keep)];
-    else if (c >= 0) b = a.free_queue[ring(a, front, first - 1)];
-    else b = a.table[place(a, s, col)];
-    slot = static_cast<int64_t>(b) * bs + pos % bs;
+    slot = slot_of(a, lo, a.lens[lo], i - a.row_off[lo], front, a.take_off[lo], a.copy_off[lo], &pos);
   }
   a.slots[i] = slot;
   if (a.positions != nullptr) a.positions[i] = pos;
+}
+
+// The whole step in one workgroup: a row to a wave, the sums over the rows in
+// every wave's lanes. What the launches above leave each other in the workspace
+// is in LDS here; block words, queue and tables go through L2, past which a
+// phase's changes are waited for.
+__device__ __forceinline__ void settle() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // this wave's stores and atomics have arrived
+  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");  // nothing older is read from the first-level cache
+}
+
+__global__ void __launch_bounds__(kOneThreads) tables_one(TablesArgs a) {
+  __shared__ int error;
+  __shared__ int frees_of[kOneRows], takes_of[kOneRows], copies_of[kOneRows], take_off[kOneRows], copy_off[kOneRows], len_of[kOneRows],
+      row_off[kOneRows + 1];
+  const int tid = threadIdx.x, lane = tid & 63, n = a.n_seqs;
+  const int s = __builtin_amdgcn_readfirstlane(tid >> 6);  // the wave's row
+  const int front = a.queue[0], count = a.queue[1];
+  if (tid == 0) error = SPORK_OK;
+  __syncthreads();
+  Row r;
+  bool sound = false;
+  if (s < n) {
+    int err = read_row(a, s, &r);
+    sound = err == SPORK_OK;
+    if (sound) err = count_row<64>(a, s, r);
+    if (err != SPORK_OK) atomicMin(&error, err);
+  }
+  settle();
+  if (s < n) {
+    int copies = 0, frees = 0, takes = 0;
+    if (sound) {  // (else the step is refused)
+      copies = copies_tail(a, s, r);
+      frees = wave_frees<64>(a, s, r);
+      takes = row_takes(a, r, copies);
+    }
+    if (lane == 0) {
+      frees_of[s] = frees;
+      takes_of[s] = takes;
+      copies_of[s] = copies;
+    }
+  }
+  __syncthreads();
+  Sums x{0, 0, 0, 0};
+  if (lane < n) x = {max(a.n_new[lane], 0), frees_of[lane], takes_of[lane], copies_of[lane]};
+  const Sums upto{wave_scan(x.tokens), wave_scan(x.frees), wave_scan(x.takes), wave_scan(x.copies)};
+  const Sums all{static_cast<int64_t>(__shfl(static_cast<long long>(upto.tokens), 63)), __shfl(upto.frees, 63),
+                 __shfl(upto.takes, 63), __shfl(upto.copies, 63)};
+  const int status = status_of(a, all, error, front, count);
+  const bool fits = status == SPORK_OK;
+  const int copy = x.copies ? upto.copies - x.copies : -1;
+  if (s == 0) {
+    if (lane < n) {
+      take_off[lane] = upto.takes - x.takes;
+      copy_off[lane] = copy;
+      len_of[lane] = a.lens[lane];
+      row_off[lane + 1] = a.row_off[lane + 1] = fits ? static_cast<int>(upto.tokens) : 0;
+      if (!fits) a.kv_len[lane] = 0;
+    }
+    if (lane == 0) {
+      row_off[0] = a.row_off[0] = 0;
+      *a.status = status;
+      *a.n_copies = fits ? all.copies : 0;
+    }
+  }
+  if (sound) {
+    const int at = __shfl(upto.frees - x.frees, s), c = __shfl(copy, s);
+    if (fits) release_row<64>(a, s, r, at, c, front, count);
+    else undo_row<64>(a, s, r);
+  }
+  settle();
+  if (fits) {
+    if (tid == 0) {
+      a.queue[0] = ring(a, front, all.takes);
+      a.queue[1] = count + all.frees - all.takes;
+    }
+    if (s < n) assign_row<64>(a, s, front, take_off[s], copy_off[s]);
+  }
+  for (int i = tid; i < a.max_tokens; i += kOneThreads) {
+    int64_t slot = -1;
+    int pos = -1;
+    if (i < row_off[n]) {  // (0 where the step is refused)
+      int lo = 0, hi = n - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (row_off[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      slot = slot_of(a, lo, len_of[lo], i - row_off[lo], front, take_off[lo], copy_off[lo], &pos);
+    }
+    a.slots[i] = slot;
+    if (a.positions != nullptr) a.positions[i] = pos;
+  }
 }
 
 __global__ void __launch_bounds__(256) tables_init_kernel(TablesArgs a, const int32_t* free_order) {
@@ -532,6 +690,10 @@ hipError_t launch_words_clear(int32_t* words, int64_t n, hipStream_t stream) {
 
 hipError_t launch_tables_step(const TablesArgs& a, hipStream_t stream) {
   const unsigned rows = static_cast<unsigned>(a.n_seqs);
+  if (a.n_seqs <= kOneRows && a.max_blocks <= kOneEntries && a.max_tokens <= kOneTokens) {
+    hipLaunchKernelGGL(tables_one, dim3(1), dim3(kOneThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(tables_count, dim3(rows), dim3(kRowThreads), 0, stream, a);
   hipLaunchKernelGGL(tables_rows, dim3(rows), dim3(kRowThreads), 0, stream, a);
   if (a.n_seqs > kRowsSummedByAll) {

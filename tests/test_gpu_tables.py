@@ -304,3 +304,41 @@ def test_a_queue_of_other_numbers_stays_inside_the_buffers():
         dev.step([0] * n, [0] * n, [-1] * n, max_tokens)
         assert dev.status.item() == spork.SPORK_E_INVAL and dev.refs.tolist() == [1 if i in (5, 6, 8) else 0 for i in range(nb)]
         assert (guarded[:4096] == -77).all() and (guarded[4096 + nb:] == -77).all()
+
+
+def test_steps_of_one_launch_and_of_more_agree():
+    """Steps at the rows, entries of a row and new-token places that the single launch takes, and at one more of each."""
+    for n, most, extra in ((16, 9, 0), (17, 9, 0), (16, 9, 1), (3, 512, 0), (3, 513, 0), (1, 9, 0)):
+        rnd = random.Random(n)
+        nb, bs = 600, 16
+        model, dev = TablesModel(n, nb, bs, most), Device(n, nb, bs, most)
+        model.last = 0
+        for before, new, parents in _random_steps(rnd, n, bs, most, model, 8):
+            want = model.step(before, new, parents, 4096 + extra)
+            model.last = want[0]
+            dev.step(before, new, parents, 4096 + extra)
+            dev.check(model, want, 4096 + extra)
+        assert not control_words(dev.ws, 32 // 4 + 3 * nb).any()
+
+
+@pytest.mark.parametrize("n,most", [(16, 512), (16, 513)])
+def test_long_rows_of_one_launch(n, most):
+    """As many entries as the single launch takes, all forked, rolled back and ended at once."""
+    bs, nb = 4, 16 * 520
+    order = np.random.default_rng(most).permutation(nb).tolist()
+    model, dev = TablesModel(n, nb, bs, most, order), Device(n, nb, bs, most, order)
+    lens = [0] * n
+    for _ in range(4):
+        new = [min(520, most * bs - x) if s % 4 < 2 else 0 for s, x in enumerate(lens)]
+        new = [x if sum(new[:s + 1]) <= 4000 else 0 for s, x in enumerate(new)]
+        want = model.step(lens, new, [-1] * n, 4096)
+        assert want[0] == 0
+        dev.step(lens, new, [-1] * n, 4096)
+        dev.check(model, want, 4096)
+        lens = [a + b for a, b in zip(lens, new)]
+    for lens2, parents in (([lens[s - s % 4] - s % 4 if s % 4 > 1 else lens[s] for s in range(n)],
+                            [s - s % 4 if s % 4 > 1 else -1 for s in range(n)]), ([0] * n, [-1] * n)):
+        want = model.step([max(x, 0) for x in lens2], [0] * n, parents, 4096)
+        assert want[0] == 0
+        dev.step([max(x, 0) for x in lens2], [0] * n, parents, 4096)
+        dev.check(model, want, 4096)
