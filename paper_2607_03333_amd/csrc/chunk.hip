@@ -1201,71 +1201,142 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 }
 
 // Log-sum-exp merge of a split tile: D / 4 lanes per packed row, four channels a
-// lane. Lane i of a row takes the maximum and sum of pieces i, i + D / 4, ..., so
-// that the weights are there in one round trip; the pieces' rows then come in
-// sixteen at a time (four, where there are no more).
+// lane. What bounds it is the way of a load, so many are in flight: with up to
+// four pieces (most tiles that a cut goes through have two) a wave takes its next
+// rows together, their weights beside their outputs; with more, lane i of a row
+// takes the maximum and sum of pieces i, i + D / 4, ..., and the pieces' rows come
+// in eight or sixteen at a time, the first of them beside the weights. (Three long
+// chunks beside 29 tokens, nearly every tile in two pieces: 19 us when a wave took
+// its rows one after the other, 12 so; one token over 1,000 positions in 8 pieces:
+// 16.5 us of both launches when the rows came behind the weights, 15.6 so.)
 constexpr int kMergeWaves = 4, kMergeGroups = 16;  // of a workgroup; workgroups of a slice
+
+// A packed row of a split tile, as the merge reads and writes it.
+struct MergeRow {
+  int in_tile;  // of a piece's rows
+  size_t out;   // row of out and lse
+  __device__ __forceinline__ MergeRow(const ChunkArgs& a, const ChunkSplit& s, int at) {
+    const int head = at / s.n_rows, p = at - head * s.n_rows, row = p / a.group;
+    in_tile = head * s.row_tiles * 32 + p;
+    out = static_cast<size_t>(s.row0 + row) * a.hq + (s.head + head) * a.group + (p - row * a.group);
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void merge_out(const ChunkArgs& a, const MergeRow& r, int sub, f32x4 o, float m, float l) {
+  o *= l > 0.0f ? 1.0f / l : 0.0f;
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + r.out * D + 4 * sub) = o;
+  else
+    *reinterpret_cast<uint2*>(static_cast<__bf16*>(a.out) + r.out * D + 4 * sub) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+  if (a.lse != nullptr && sub == 0) a.lse[r.out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+}
+
+// Up to kPieces pieces, kTogether steps of rows at a time.
+template <typename T, int D, int kPieces, int kTogether>
+__device__ __forceinline__ void merge_few(const ChunkArgs& a, const ChunkSplit& s, int slice, int pieces, int lane, int first, int step) {
+  constexpr int LPR = D / 4, kRows = 64 / LPR;
+  const int rows = s.n_rows * s.heads, sub = lane % LPR;
+  bool there[kPieces];
+#pragma unroll
+  for (int q = 0; q < kPieces; ++q) there[q] = q == 0 || (q < pieces && a.continues[slice + min(q, pieces - 1)] != 0);
+  // (the lanes of a wave stay together: rows past the last are computed again)
+  for (int i0 = first * kRows * kTogether; i0 < rows; i0 += step * kRows * kTogether) {
+    float2 x[kTogether][kPieces];
+    f32x4 v[kTogether][kPieces];
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      const MergeRow r(a, s, min(i0 + k * kRows + lane / LPR, rows - 1));
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) {
+        const int i = min(q, pieces - 1);
+        const size_t at = piece_row(slice + i, i == 0) + r.in_tile;
+        x[k][q] = reinterpret_cast<const float2*>(a.part_ml)[at];
+        v[k][q] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * sub);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) {
+      float m = x[k][0].x;
+#pragma unroll
+      for (int q = 1; q < kPieces; ++q) m = there[q] ? fmaxf(m, x[k][q].x) : m;
+      const float ref = m == kNegInf ? 0.0f : m;
+      float l = 0.0f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) {  // (what is no piece's may hold anything)
+        const float w = there[q] ? exp2_fast(x[k][q].x - ref) : 0.0f;
+        if (there[q]) l += x[k][q].y * w;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] += there[q] ? v[k][q][c] * w : 0.0f;
+      }
+      merge_out<T, D>(a, MergeRow(a, s, min(i0 + k * kRows + lane / LPR, rows - 1)), sub, o, m, l);
+    }
+  }
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kMergeWaves) chunk_merge_kernel(ChunkArgs a) {
   constexpr int LPR = D / 4, kRows = 64 / LPR;
-  const int slice = blockIdx.x, lane = threadIdx.x & 63, group = a.group, sub = lane % LPR;
+  const int slice = blockIdx.x, lane = threadIdx.x & 63, sub = lane % LPR;
   const ChunkSplit s = a.splits[slice];
+  if (s.n_rows == 0) return;
   const int pieces = s.last - slice + 1, rows = s.n_rows * s.heads;
-  // (the lanes of a wave stay together: rows past the last are computed again)
-  for (int i0 = (blockIdx.y * kMergeWaves + (threadIdx.x >> 6)) * kRows; i0 < rows; i0 += kMergeGroups * kMergeWaves * kRows) {
-    const int at = min(i0 + lane / LPR, rows - 1), head = at / s.n_rows, p = at - head * s.n_rows;
-    const int in_tile = head * s.row_tiles * 32 + p;
+  const int first = blockIdx.y * kMergeWaves + static_cast<int>(threadIdx.x >> 6), step = kMergeGroups * kMergeWaves;
+  if (pieces <= 2) {
+    merge_few<T, D, 2, 4>(a, s, slice, pieces, lane, first, step);
+    return;
+  }
+  if (pieces <= 4) {
+    merge_few<T, D, 4, 2>(a, s, slice, pieces, lane, first, step);
+    return;
+  }
+  for (int i0 = first * kRows; i0 < rows; i0 += step * kRows) {
+    const MergeRow r(a, s, min(i0 + lane / LPR, rows - 1));
     float m = kNegInf, l = 0.0f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int base = 0; base < pieces; base += LPR) {
-      const int i = base + sub;
-      float2 x = make_float2(kNegInf, 0.0f);
-      if (i < pieces && (i == 0 || a.continues[slice + i] != 0))
-        x = reinterpret_cast<const float2*>(a.part_ml)[piece_row(slice + i, i == 0) + in_tile];
-      float top = x.x;
-#pragma unroll
-      for (int by = LPR / 2; by >= 1; by /= 2) top = fmaxf(top, __shfl_xor(top, by));
-      top = fmaxf(top, m);
-      const float ref = top == kNegInf ? 0.0f : top, mine = exp2_fast(m - ref), f = exp2_fast(x.x - ref);
-      float sum = x.y * f;
-#pragma unroll
-      for (int by = LPR / 2; by >= 1; by /= 2) sum += __shfl_xor(sum, by);
-      l = l * mine + sum;
-      m = top;
-      o *= mine;
-      const int n = min(LPR, pieces - base);
+      const int n = min(LPR, pieces - base), i = base + min(sub, n - 1);
+      float2 x = reinterpret_cast<const float2*>(a.part_ml)[piece_row(slice + i, i == 0) + r.in_tile];
+      const bool there = sub < n && (i == 0 || a.continues[slice + i] != 0);
+      // (what is no piece's may hold anything; a weight of zero leaves it out)
       auto rows_of = [&](auto batch_c) __attribute__((always_inline)) {
         constexpr int kBatch = decltype(batch_c)::value;
-        for (int j = 0; j < n; j += kBatch) {
-          float w[kBatch];
-          f32x4 v[kBatch];
+        f32x4 v[kBatch];
+        auto load = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
           for (int q = 0; q < kBatch; ++q) {
-            // a piece that is none, or whose rows see nothing, weighs nothing: the
-            // first one's row stands in for it
-            const int k = min(j + q, n - 1);
-            w[q] = __shfl(f, lane - sub + k);
-            if (j + q >= n) w[q] = 0.0f;
-            const bool there = w[q] != 0.0f;
-            v[q] = *reinterpret_cast<const f32x4*>(
-                a.part_o + (piece_row(there ? slice + base + k : slice, !there || base + k == 0) + in_tile) * D + 4 * sub);
+            const int k = base + min(from + q, n - 1);
+            v[q] = *reinterpret_cast<const f32x4*>(a.part_o + (piece_row(slice + k, k == 0) + r.in_tile) * D + 4 * sub);
           }
+        };
+        load(0);  // beside the weights
+        if (!there) x = make_float2(kNegInf, 0.0f);
+        float top = x.x;
 #pragma unroll
-          for (int q = 0; q < kBatch; ++q) o += v[q] * w[q];
+        for (int by = LPR / 2; by >= 1; by /= 2) top = fmaxf(top, __shfl_xor(top, by));
+        top = fmaxf(top, m);
+        const float ref = top == kNegInf ? 0.0f : top, mine = exp2_fast(m - ref), f = exp2_fast(x.x - ref);
+        float sum = x.y * f;
+#pragma unroll
+        for (int by = LPR / 2; by >= 1; by /= 2) sum += __shfl_xor(sum, by);
+        l = l * mine + sum;
+        m = top;
+        o *= mine;
+        for (int from = 0; from < n; from += kBatch) {
+          if (from > 0) load(from);
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) {
+            const float w = from + q < n ? __shfl(f, lane - sub + min(from + q, n - 1)) : 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] += w != 0.0f ? v[q][c] * w : 0.0f;
+          }
         }
       };
-      if (n <= 4) rows_of(std::integral_constant<int, 4>{});
+      if (n <= 8) rows_of(std::integral_constant<int, 8>{});
       else rows_of(std::integral_constant<int, 16>{});
     }
-    const int row = p / group;
-    const size_t out = static_cast<size_t>(s.row0 + row) * a.hq + (s.head + head) * group + (p - row * group);
-    o *= l > 0.0f ? 1.0f / l : 0.0f;
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + out * D + 4 * sub) = o;
-    else
-      *reinterpret_cast<uint2*>(static_cast<__bf16*>(a.out) + out * D + 4 * sub) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-    if (a.lse != nullptr && sub == 0) a.lse[out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+    merge_out<T, D>(a, r, sub, o, m, l);
   }
 }
 
