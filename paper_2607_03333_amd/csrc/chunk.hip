@@ -9,7 +9,8 @@
 // of 32, against the positions up to its last row's. A sequence of up to 256
 // packed rows is one tile per KV head: then there are row tiles for only some of
 // the workgroup's 8 waves, and the others take other tokens of the tile (8, 4 or
-// 2 ways), joined through LDS at its end.
+// 2 ways), joined through LDS at its end, or other KV heads where the batch has
+// tiles enough for every compute unit (chunk_tile_heads).
 //
 // Slices. All tiles in a row, each as long as it costs (a start-up plus its
 // tokens), make a line that is cut into equal slices, one per compute unit. A
@@ -21,10 +22,12 @@
 // log-sum-exp. Neighbouring slices (the row tiles of one sequence and KV head,
 // which read the same keys and values) go to one die, whose L2 they share.
 //
-// Each wave streams its 32-token stages (fp32: 16) of K and V into a slot of its
-// own in LDS by direct loads (lane i of an instruction lands at its base + 16 i)
-// and reads them from there as operands; the loads of the next stage are in
-// flight while it computes, and no wave waits for another inside a tile.
+// In tiles of up to four row tiles, and all of fp32's, each wave streams its
+// 32-token stages (fp32: 16) of K and V into a slot of its own in LDS by direct
+// loads (lane i of an instruction lands at its base + 16 i) and reads them from
+// there as operands; the loads of the next stage are in flight while it computes,
+// and no wave waits for another inside a tile. In bf16 tiles of more row tiles the
+// waves share their stages (wide_tile).
 //   bf16  S^T = K Q^T and O^T += V^T P^T in 32x32x16 products. A-row r of the
 //         scores is token 16*(r/16) + 8*(r/4%2) + 4*(r/8%2) + r%4, so that a lane
 //         receives its query row's scores of tokens 16h + 8g + j (element 8h + j,
@@ -34,7 +37,7 @@
 // Softmax in base 2 with a lazily moved reference: it moves, and the accumulator
 // is rescaled, only where a lane's probabilities of a stage sum past 2^8.
 // Probabilities enter the second product in the input type (bf16: rounded to
-// nearest, 2^-9 of each; the row sum is of the unrounded ones); sums, reference
+// nearest, at most 2^-8 of each; the row sum is of the unrounded ones); sums, reference
 // and accumulators are fp32.
 #include "chunk_kernels.h"
 #include "device_common.h"
