@@ -63,8 +63,8 @@ constexpr float kSlackSum = 256.0f;
 // The line's unit is half the time that a token of 128 bf16 channels takes where
 // HBM bounds it, about 9 ns on one compute unit.
 // A tile's start-up and end: 24 prompts of up to 777 tokens with 16 heads of 64
-// took 54.5 us at 640, 52.7 at 1,000, 53.1 at 1,400 (a long chunk beside 96 single
-// tokens 157, 156, 160).
+// took 54.5 us at 640, 52.7 at 1,000, 53.1 at 1,400 (three long chunks beside 29
+// single tokens 157, 156, 160).
 constexpr int kTileCost = 1000;
 // Least length of a slice: three fp32 prompts took 47.4 us at 2,048, 33.2 at 1,024,
 // 31.3 at 512, 27.8 at 320; one token over 1,000 positions 25.5, 17.8, 16.9, 16.5.

@@ -130,12 +130,13 @@ __device__ __forceinline__ Changes changes(const TablesArgs& a, int s, const Row
   return x;
 }
 
-// References and last places of a row's changes; the status of its entries.
+// References and last places of a row's changes (`head`: the first of them, of each
+// thread kAtOnce); the status of its entries.
 template <int kTeam>
-__device__ __forceinline__ int count_row(const TablesArgs& a, int s, const Row& r) {
+__device__ __forceinline__ int count_row(const TablesArgs& a, int s, const Row& r, const Changes& head) {
   int err = SPORK_OK;
   for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
-    const Changes x = changes<kTeam>(a, s, r, j0);
+    const Changes x = j0 == changes_lo(r) ? head : changes<kTeam>(a, s, r, j0);
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) {
       if (x.gains[q]) {
@@ -169,7 +170,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_count(TablesArgs a) {
   if (s == 0 && threadIdx.x == 0) a.totals->front = a.queue[0];
   Row r;
   int err = read_row(a, s, &r);
-  if (err == SPORK_OK) err = count_row<kRowThreads>(a, s, r);
+  if (err == SPORK_OK) err = count_row<kRowThreads>(a, s, r, changes<kRowThreads>(a, s, r, changes_lo(r)));
   if (err != SPORK_OK) atomicMin(&a.totals->error, err);
 }
 
@@ -188,10 +189,10 @@ __device__ __forceinline__ int copies_tail(const TablesArgs& a, int s, const Row
 
 // Blocks that the thread's entries of row s free, summed over its wave.
 template <int kTeam>
-__device__ __forceinline__ int wave_frees(const TablesArgs& a, int s, const Row& r) {
+__device__ __forceinline__ int wave_frees(const TablesArgs& a, int s, const Row& r, const Changes& head) {
   int frees = 0;
   for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
-    const Changes x = changes<kTeam>(a, s, r, j0);
+    const Changes x = j0 == changes_lo(r) ? head : changes<kTeam>(a, s, r, j0);
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) frees += x.loses[q] && frees_block(a, s, column<kTeam>(j0, q), x.was[q]);
   }
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_rows(TablesArgs a) {
   const int copies = tid == 0 ? copies_tail(a, s, r) : 0;
   int frees = 0;
   if (changes_lo(r) < changes_hi(r)) {
-    frees = wave_frees<kRowThreads>(a, s, r);
+    frees = wave_frees<kRowThreads>(a, s, r, changes<kRowThreads>(a, s, r, changes_lo(r)));
     if ((tid & 63) == 0) freed[tid >> 6] = frees;
     __syncthreads();
     frees = 0;
@@ -346,12 +347,13 @@ __device__ __forceinline__ void undo_row(const TablesArgs& a, int s, const Row& 
 // The frees of row s into the queue, behind `at` others, and a forked row's
 // entries; its copy's entry (c: index of it, or -1).
 template <int kTeam>
-__device__ __forceinline__ void release_row(const TablesArgs& a, int s, const Row& r, int at, int c, int front, int count) {
+__device__ __forceinline__ void release_row(const TablesArgs& a, int s, const Row& r, const Changes& head, int at, int c, int front,
+                                            int count) {
   constexpr int kTeamWaves = kTeam / 64;
   __shared__ int freed[kAtOnce][kTeamWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x % kTeam >> 6;
   for (int j0 = changes_lo(r); j0 < changes_hi(r); j0 += kAtOnce * kTeam) {
-    const Changes x = changes<kTeam>(a, s, r, j0);
+    const Changes x = j0 == changes_lo(r) ? head : changes<kTeam>(a, s, r, j0);
     bool here[kAtOnce];
 #pragma unroll
     for (int q = 0; q < kAtOnce; ++q) here[q] = x.loses[q] && frees_block(a, s, column<kTeam>(j0, q), x.was[q]);
@@ -419,7 +421,7 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
   Row r;
   if (read_row(a, s, &r) != SPORK_OK) return;
   if (status != SPORK_OK) undo_row<kRowThreads>(a, s, r);
-  else release_row<kRowThreads>(a, s, r, at, c, front, count);
+  else release_row<kRowThreads>(a, s, r, changes<kRowThreads>(a, s, r, changes_lo(r)), at, c, front, count);
 }
 
 // The fronts of row s, from the queue's nth on, into its table; its references
@@ -524,11 +526,15 @@ __global__ void __launch_bounds__(kOneThreads) tables_one(TablesArgs a) {
   if (tid == 0) error = SPORK_OK;
   __syncthreads();
   Row r;
+  Changes head;  // (the tables change only behind the last use)
   bool sound = false;
   if (s < n) {
     int err = read_row(a, s, &r);
     sound = err == SPORK_OK;
-    if (sound) err = count_row<64>(a, s, r);
+    if (sound) {
+      head = changes<64>(a, s, r, changes_lo(r));
+      err = count_row<64>(a, s, r, head);
+    }
     if (err != SPORK_OK) atomicMin(&error, err);
   }
   settle();
@@ -536,7 +542,7 @@ __global__ void __launch_bounds__(kOneThreads) tables_one(TablesArgs a) {
     int copies = 0, frees = 0, takes = 0;
     if (sound) {  // (else the step is refused)
       copies = copies_tail(a, s, r);
-      frees = wave_frees<64>(a, s, r);
+      frees = wave_frees<64>(a, s, r, head);
       takes = row_takes(a, r, copies);
     }
     if (lane == 0) {
@@ -570,7 +576,7 @@ __global__ void __launch_bounds__(kOneThreads) tables_one(TablesArgs a) {
   }
   if (sound) {
     const int at = __shfl(upto.frees - x.frees, s), c = __shfl(copy, s);
-    if (fits) release_row<64>(a, s, r, at, c, front, count);
+    if (fits) release_row<64>(a, s, r, head, at, c, front, count);
     else undo_row<64>(a, s, r);
   }
   settle();
