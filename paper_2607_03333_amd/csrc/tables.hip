@@ -43,10 +43,10 @@ constexpr int kAtOnce = 4;         // entries of a row that a thread loads toget
 constexpr int kRowsSummedByAll = 1024;
 // Steps of one workgroup: at most so many rows (a wave each), entries of a row,
 // and new tokens. Half of the rows forking again, eager and in a graph, one launch
-// against four: 1 row 9.0 and 8.2 us against 16.0 and 9.3; 8 rows of 250 tokens 12.3
-// and 12.6 against 16.9 and 15.1; 16 rows 14.1 and 14.3 against 17.1 and 14.8; 16 rows
-// of 500 blocks 14.3 and 14.6 against 17.1 and 13.4, of 1,000 blocks 19.1 and 19.4
-// against 17.1 and 13.5; 4,096 new tokens 11.6 and 11.9 against 17.0 and 13.0.
+// against four: 1 row 9.0 and 8.4 us against 16.0 and 9.3; 8 rows of 250 tokens 11.5
+// and 11.8 against 16.9 and 15.1; 16 rows 12.6 and 12.9 against 17.1 and 14.8; 16 rows
+// of 500 blocks 13.2 and 13.5 against 17.1 and 13.4, of 1,000 blocks 19.1 and 19.4
+// against 17.1 and 13.5; 4,096 new tokens 10.7 and 10.9 against 17.0 and 13.0.
 constexpr int kOneThreads = 1024;
 constexpr int kOneRows = 16, kOneEntries = 512, kOneTokens = 4096;
 static_assert(kOneRows * 64 == kOneThreads, "a wave for every row");
@@ -56,9 +56,14 @@ struct Row {
   int keep;        // blocks of the tokens that stay
   int from;        // row that those blocks stand in
   int release_lo;  // first entry of the old row that is released
+  int tail;        // block that the row appends into behind tokens that stay, or -1
 };
 
 __device__ __forceinline__ int blocks_of(int64_t tokens, int bs) { return static_cast<int>((tokens + bs - 1) / bs); }
+
+__device__ __forceinline__ size_t place(const TablesArgs& a, int s, int col) {
+  return static_cast<size_t>(s) * a.max_blocks + col;
+}
 
 // Row s as the step asks for it, and the status of that: its fields are used
 // only where it is SPORK_OK, and then every index that follows from them is in
@@ -82,20 +87,11 @@ __device__ __forceinline__ int read_row(const TablesArgs& a, int s, Row* r) {
   r->keep = blocks_of(r->len, a.block_size);
   r->from = r->parent >= 0 ? r->parent : s;
   r->release_lo = r->parent >= 0 ? 0 : r->keep;
+  r->tail = r->grow == 0 || r->len % a.block_size == 0 ? -1 : a.table[place(a, r->from, r->len / a.block_size)];
   return SPORK_OK;
 }
 
 __device__ __forceinline__ bool in_pool(const TablesArgs& a, int block) { return block >= 0 && block < a.num_blocks; }
-
-__device__ __forceinline__ size_t place(const TablesArgs& a, int s, int col) {
-  return static_cast<size_t>(s) * a.max_blocks + col;
-}
-
-// Block that row s appends into behind tokens that stay, or -1.
-__device__ __forceinline__ int shared_tail(const TablesArgs& a, const Row& r) {
-  if (r.grow == 0 || r.len % a.block_size == 0) return -1;
-  return a.table[place(a, r.from, r.len / a.block_size)];
-}
 
 // What forks and releases change in the columns of table row s from column j0 on,
 // kAtOnce of them per thread: the entry that was there and the one that comes.
@@ -154,10 +150,9 @@ __device__ __forceinline__ int count_row(const TablesArgs& a, int s, const Row& 
     }
   }
   if (threadIdx.x % kTeam == 0 && r.grow != 0 && r.len % a.block_size != 0) {
-    const int b = shared_tail(a, r);
-    if (in_pool(a, b)) {
-      atomicAdd(a.sharers + b, 1);
-      atomicMax(a.last_sharer + b, s + 1);
+    if (in_pool(a, r.tail)) {
+      atomicAdd(a.sharers + r.tail, 1);
+      atomicMax(a.last_sharer + r.tail, s + 1);
     } else {
       err = SPORK_E_INVAL;
     }
@@ -181,10 +176,9 @@ __device__ __forceinline__ bool frees_block(const TablesArgs& a, int s, int j, i
 
 // Whether row s, which appends inside a block, copies it.
 __device__ __forceinline__ int copies_tail(const TablesArgs& a, int s, const Row& r) {
-  const int b = shared_tail(a, r);
-  if (!in_pool(a, b)) return 0;
-  const int refs = a.refcount[b];
-  return refs > 1 && !(a.sharers[b] == refs && a.last_sharer[b] == s + 1);
+  if (!in_pool(a, r.tail)) return 0;
+  const int refs = a.refcount[r.tail], sharers = a.sharers[r.tail], last = a.last_sharer[r.tail];
+  return refs > 1 && !(sharers == refs && last == s + 1);
 }
 
 // Blocks that the thread's entries of row s free, summed over its wave.
@@ -339,8 +333,7 @@ __device__ __forceinline__ void undo_row(const TablesArgs& a, int s, const Row& 
     }
   }
   if (threadIdx.x % kTeam == 0) {
-    const int b = shared_tail(a, r);
-    if (in_pool(a, b)) a.sharers[b] = a.last_sharer[b] = 0;
+    if (in_pool(a, r.tail)) a.sharers[r.tail] = a.last_sharer[r.tail] = 0;
   }
 }
 
@@ -387,10 +380,9 @@ __device__ __forceinline__ void release_row(const TablesArgs& a, int s, const Ro
     if constexpr (kTeamWaves > 1) __syncthreads();  // the counts are read
   }
   if (threadIdx.x % kTeam == 0) {
-    const int b = shared_tail(a, r);
-    if (b >= 0) a.sharers[b] = a.last_sharer[b] = 0;
+    if (r.tail >= 0) a.sharers[r.tail] = a.last_sharer[r.tail] = 0;
     if (c >= 0) {
-      a.copies[3 * c] = b;
+      a.copies[3 * c] = r.tail;
       a.copies[3 * c + 2] = r.len % a.block_size;
     }
   }
@@ -425,15 +417,15 @@ __global__ void __launch_bounds__(kRowThreads) tables_release(TablesArgs a) {
 }
 
 // The fronts of row s, from the queue's nth on, into its table; its references
-// and length (c as above).
+// and length (c as above; src: the block that is copied).
 template <int kTeam>
-__device__ __forceinline__ void assign_row(const TablesArgs& a, int s, int front, int nth, int c) {
+__device__ __forceinline__ void assign_row(const TablesArgs& a, int s, int front, int nth, int c, int src) {
   const int tid = threadIdx.x % kTeam, bs = a.block_size;
   const int len = a.lens[s], end = len + a.n_new[s], keep = blocks_of(len, bs), to = blocks_of(end, bs);
   if (c >= 0) {
     if (tid == 0) {
       const int dst = a.free_queue[ring(a, front, nth)];
-      atomicAdd(a.refcount + a.copies[3 * c], -1);
+      atomicAdd(a.refcount + src, -1);
       a.copies[3 * c + 1] = dst;
       if (in_pool(a, dst)) a.refcount[dst] = 1;
       a.table[place(a, s, len / bs)] = dst;
@@ -485,7 +477,8 @@ __global__ void __launch_bounds__(kRowThreads) tables_assign(TablesArgs a) {
       }
       return;
     }
-    assign_row<kRowThreads>(a, s, front, a.take_off[s], a.copy_off[s]);
+    const int c = a.copy_off[s];
+    assign_row<kRowThreads>(a, s, front, a.take_off[s], c, c >= 0 ? a.copies[3 * c] : -1);
     return;
   }
   // a token: its row by search in the offsets
@@ -585,7 +578,7 @@ __global__ void __launch_bounds__(kOneThreads) tables_one(TablesArgs a) {
       a.queue[0] = ring(a, front, all.takes);
       a.queue[1] = count + all.frees - all.takes;
     }
-    if (s < n) assign_row<64>(a, s, front, take_off[s], copy_off[s]);
+    if (s < n) assign_row<64>(a, s, front, take_off[s], copy_off[s], r.tail);
   }
   for (int i = tid; i < a.max_tokens; i += kOneThreads) {
     int64_t slot = -1;
