@@ -15,6 +15,9 @@ namespace {
 
 using namespace spork::capi;
 
+// A launch has fewer than 2^32 threads: so many workgroups of 256.
+constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
+
 bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) == 0; }
 
 // The sizes that every tables call checks.
@@ -22,9 +25,9 @@ int check_tables(const spork_tables* t) {
   if (t == nullptr) return fail(SPORK_E_INVAL, "tables is NULL");
   if (t->num_blocks <= 0 || t->block_size <= 0 || t->n_seqs <= 0 || t->max_blocks <= 0)
     return fail(SPORK_E_INVAL, "num_blocks, block_size, n_seqs and max_blocks must be positive");
-  if (static_cast<int64_t>(t->n_seqs) * t->max_blocks >= INT_MAX ||
+  if (t->n_seqs * (int64_t{1} + t->max_blocks) >= INT_MAX ||
       static_cast<int64_t>(t->max_blocks) * t->block_size > INT_MAX)
-    return fail(SPORK_E_UNSUPPORTED, "n_seqs * max_blocks and max_blocks * block_size must be below 2^31");
+    return fail(SPORK_E_UNSUPPORTED, "n_seqs * (max_blocks + 1) and max_blocks * block_size must be below 2^31");
   return SPORK_OK;
 }
 
@@ -112,6 +115,8 @@ int spork_tables_step(const spork_tables* tables, const int32_t* lens, const int
     if (max_tokens < 0) return fail(SPORK_E_INVAL, "max_tokens must be >= 0");
     if (!lens || !n_new || !row_off || !kv_len || !copies || !n_copies || !status || (max_tokens > 0 && !slots))
       return fail(SPORK_E_INVAL, "NULL pointer");
+    if (tables->n_seqs + (max_tokens + int64_t{255}) / 256 > kMostGroups)
+      return fail(SPORK_E_UNSUPPORTED, "n_seqs + max_tokens / 256 must be below 2^24");
     rc = check_tables_workspace(tables, workspace, ws_bytes);
     if (rc != SPORK_OK) return rc;
     spork::TablesArgs a = tables_args(tables);
@@ -143,9 +148,9 @@ int spork_kv_copy_batch(const spork_shape* shape, void* k_cache, void* v_cache, 
     if (shape->head_dim * static_cast<int64_t>(elem) % 16 != 0)
       return fail(SPORK_E_UNSUPPORTED, "head_dim must fill 16-byte vectors");
     if (!aligned16(k_cache) || !aligned16(v_cache)) return fail(SPORK_E_INVAL, "pools must be 16-byte aligned");
-    if (static_cast<int64_t>(max_copies) * shape->hkv > INT_MAX ||
+    if (static_cast<int64_t>(max_copies) * shape->hkv > kMostGroups ||
         static_cast<int64_t>(shape->head_dim) * shape->block_size * elem > INT_MAX)
-      return fail(SPORK_E_UNSUPPORTED, "max_copies * hkv and a block's bytes per head must be below 2^31");
+      return fail(SPORK_E_UNSUPPORTED, "max_copies * hkv must be below 2^24 and a block's bytes per head below 2^31");
     return hip_status(spork::launch_kv_copy_batch(elem, shape->hkv, shape->head_dim, shape->block_size, num_blocks, k_cache,
                                                   v_cache, copies, n_copies, max_copies, stream),
                       "spork_kv_copy_batch");

@@ -67,6 +67,16 @@ def test_tables_arguments():
     assert lib.spork_tables_step(None, *[P] * 3, 9, *[P] * 8, 1 << 20, None) == INVAL
 
 
+def test_steps_larger_than_a_launch():
+    """Threads of a launch are counted in 32 bits: refused before anything is launched."""
+    many = dict(n_seqs=1 << 24, max_blocks=1)
+    assert step(tables(**many), size=1 << 40) == UNSUPPORTED
+    assert step(tables(n_seqs=(1 << 24) - 2, max_blocks=1), max_tokens=300, size=1 << 40) == UNSUPPORTED
+    assert step(tables(n_seqs=1 << 30, max_blocks=1), size=1 << 40) == UNSUPPORTED  # takes of two blocks a row: 2^31
+    call = spork.lib().spork_kv_copy_batch
+    assert call(shape(hq=8, hkv=8), P, P, 10, P, P, 1 << 21, None) == UNSUPPORTED
+
+
 def test_copy_batch_arguments():
     call = spork.lib().spork_kv_copy_batch
     assert call(shape(), P, P, 10, P, P, 0, None) == 0  # nothing to copy
