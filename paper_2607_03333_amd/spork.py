@@ -406,9 +406,19 @@ def _want(name, x, size, *shape):
 
 
 def _on_gpu(*tensors):
+    """In the memory of the current device, where the launches go (integers are pointers and pass)."""
+    here = None
     for x in tensors:
-        if x is not None and not x.is_cuda:
+        if x is None or isinstance(x, int):
+            continue
+        at = x.get_device()
+        if at < 0:
             raise ValueError("tensor arguments must be in GPU memory")
+        if here is None:
+            import torch
+            here = torch.cuda.current_device()
+        if at != here:
+            raise ValueError(f"tensor arguments must be on the current device ({here}), not on {at}")
 
 
 def make_tables(block_size, table, held, refcount, free_queue, queue):
@@ -424,8 +434,9 @@ def make_tables(block_size, table, held, refcount, free_queue, queue):
 
 
 def spork_tables_init(tables, free_order=None, stream=None):
-    _check(lib().spork_tables_init(ctypes.byref(tables), _want("free_order", free_order, 4, tables.num_blocks),
-                                   _stream(stream)))
+    order = _want("free_order", free_order, 4, tables.num_blocks)
+    _on_gpu(*tables.tensors, free_order)
+    _check(lib().spork_tables_init(ctypes.byref(tables), order, _stream(stream)))
 
 
 def spork_tables_workspace_bytes(tables):
@@ -435,6 +446,7 @@ def spork_tables_workspace_bytes(tables):
 
 
 def spork_tables_workspace_clear(tables, workspace, stream=None):
+    _on_gpu(workspace)
     _check(lib().spork_tables_workspace_clear(ctypes.byref(tables), _ptr(workspace), _bytes(workspace), _stream(stream)))
 
 
@@ -446,7 +458,7 @@ def spork_tables_step(tables, lens, n_new, parents, slots, positions, row_off, k
             _want("slots", slots, 8, most), _want("positions", positions, 4, most), _want("row_off", row_off, 4, n + 1),
             _want("kv_len", kv_len, 4, n), _want("copies", copies, 4, n, 3), _want("n_copies", n_copies, 4, 1),
             _want("status", status, 4, 1), _ptr(workspace), _bytes(workspace))
-    _on_gpu(tables.tensors[0], lens, n_new, parents, slots, positions, row_off, kv_len, copies, n_copies, status, workspace)
+    _on_gpu(*tables.tensors, lens, n_new, parents, slots, positions, row_off, kv_len, copies, n_copies, status, workspace)
     _check(lib().spork_tables_step(ctypes.byref(tables), *args, _stream(stream)))
 
 
@@ -479,7 +491,7 @@ def spork_chunk_attn(shape, q, k_cache, v_cache, table, row_off, kv_len, out, ls
     bs = shape.block_size
     if tuple(k_cache.shape) != (blocks, shape.hkv, bs, d) or tuple(v_cache.shape) != (blocks, shape.hkv, d, bs):
         raise ValueError("the pools must be [blocks, hkv, block_size, head_dim] and [blocks, hkv, head_dim, block_size]")
-    stride = q.stride(0) if n_rows > 1 else max(hq * d, q.stride(0))
+    stride = q.stride(0) if n_rows > 1 else hq * d
     args = (q.data_ptr(), stride, _ptr(k_cache), _ptr(v_cache), blocks, _want("table", table, 4, n_seqs, max_blocks),
             max_blocks, _want("row_off", row_off, 4, n_seqs + 1), _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows,
             _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace))

@@ -206,3 +206,40 @@ def test_accepted_drafts_decide_the_next_step(graph):
         assert accepted.tolist() == want and token.tolist() == [greedy[j, w].item() for j, w in enumerate(want)]
         lens = [a + 1 + w for a, w in zip(lens, want)]
         assert s.lens.tolist() == lens
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Launches go to the current device: with another one current, nothing is launched."""
+    s = Server(BF16, 4, 2, 64, 16, 2, 9, 4, 8, seed=1)
+    s.projections()
+    s.set([0, 0], [3, 2], [N] * 2)
+    stream = torch.cuda.current_stream()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    q = s.fused[:, :s.hq * s.d].unflatten(1, (s.hq, s.d))
+    calls = (lambda: spork.spork_tables_init(s.t, stream=stream),
+             lambda: spork.spork_tables_workspace_clear(s.t, s.tables_ws, stream=stream),
+             lambda: spork.spork_tables_step(s.t, s.lens, s.new, s.parents, s.slots, s.positions, s.row_off, s.kv_len, s.copies,
+                                             s.n_copies, s.status, s.tables_ws, stream=stream),
+             lambda: spork.spork_kv_copy_batch(s.shape, s.k, s.v, 9, s.copies, s.n_copies, stream=stream),
+             lambda: spork.spork_chunk_attn(s.shape, q, s.k, s.v, s.table, s.row_off, s.kv_len, s.out, s.lse, s.chunk_ws,
+                                            stream=stream))
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert (s.out == 7.5).all()
+
+
+def test_one_row_of_a_wider_buffer():
+    """A single query row: the distance to the next one does not matter."""
+    s = Server(F32, 4, 2, 64, 16, 1, 9, 4, 1, seed=2)
+    s.projections()
+    s.set([0], [1], [N])
+    s.tokens([0], [1], [N])
+    s.launch()
+    wide = torch.zeros(1, 4 * 64 + 3, device="cuda")
+    wide[:, :256] = s.fused[:, :256]
+    spork.spork_chunk_attn(s.shape, wide[:, :256].unflatten(1, (4, 64)), s.k, s.v, s.table, s.row_off, s.kv_len, s.out, s.lse,
+                           s.chunk_ws)
+    s.check([1], "one row")

@@ -151,6 +151,10 @@ def test_binding_checks_what_it_hands_over():
         assert "GPU" not in str(e.value)
     with pytest.raises(ValueError, match="GPU"):  # host tensors
         spork.spork_tables_step(t, *good, stream=0)
+    with pytest.raises(ValueError, match="GPU"):
+        spork.spork_tables_init(t, stream=0)
+    with pytest.raises(ValueError, match="GPU"):
+        spork.spork_tables_workspace_clear(t, torch.zeros(1 << 12, dtype=torch.uint8), stream=0)
     sh = spork.make_shape(4, 2, 64, 16, F32, 0.1)
     q, k, v = torch.zeros(3, 4, 64), torch.zeros(5, 2, 16, 64), torch.zeros(5, 2, 64, 16)
     good = [q, k, v, i32(2, 4), i32(3), i32(2), torch.zeros(3, 4, 64), torch.zeros(3, 4), torch.zeros(64)]
