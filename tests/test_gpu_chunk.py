@@ -277,3 +277,37 @@ def test_captured_calls_follow_the_lengths():
         c.run()  # eager, on its own buffers
         torch.cuda.synchronize()
         assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+
+
+@pytest.mark.parametrize("new", ([1, 3], [300, 1]))
+def test_blocks_past_4_gib(new):
+    """Blocks whose bytes begin beyond 2^32 of a pool, and the copy of one."""
+    c = Case(BF16, 8, 8, 128, 32, new, [400, 333], seed=6)
+    nb, used = 68000, c.k.shape[0]  # 64 KiB a block
+    k, v = (torch.empty(nb, *x.shape[1:], dtype=BF16, device="cuda") for x in (c.k, c.v))
+    k[nb - used:], v[nb - used:] = c.k, c.v
+    table = c.table + (nb - used)
+    spork.spork_chunk_attn(c.shape, c.q, k, v, table, c.row_off, c.kv_len, c.out, c.lse, c.ws)
+    c.check("past 4 GiB")
+    copies = torch.tensor([[nb - 1, nb - used - 1, 7]], dtype=torch.int32, device="cuda")
+    spork.spork_kv_copy_batch(c.shape, k, v, nb, copies, torch.ones(1, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert torch.equal(k[nb - used - 1, :, :7].view(torch.int16), k[nb - 1, :, :7].view(torch.int16))
+    assert torch.equal(v[nb - used - 1, :, :, :7].view(torch.int16), v[nb - 1, :, :, :7].view(torch.int16))
+
+
+@pytest.mark.parametrize("new", ([2, 1], [40, 1]))
+def test_rows_past_4_gib(new):
+    """Query and output rows beyond 2^31 elements; the rows in front of them belong to no sequence."""
+    c = Case(BF16, 64, 8, 128, 16, new, [90, 33], seed=7, spare_rows=0)
+    rows = c.rows
+    n = (1 << 31) // (64 * 128) + 9 + rows
+    q, out = (torch.empty(n, 64, 128, dtype=BF16, device="cuda") for _ in range(2))
+    lse = torch.empty(n, 64, device="cuda")
+    q[n - rows:], out[-rows - 5:], lse[-rows - 5:] = c.q, 7.5, 7.5
+    spork.spork_chunk_attn(c.shape, q, c.k, c.v, c.table, c.row_off + (n - rows), c.kv_len, out, lse, c.ws)
+    torch.cuda.synchronize()
+    assert (out[-rows - 5:-rows] == 7.5).all() and (lse[-rows - 5:-rows] == 7.5).all()
+    c.out.copy_(out[-rows:])
+    c.lse.copy_(lse[-rows:])
+    c.check("rows past 4 GiB")

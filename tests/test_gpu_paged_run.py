@@ -243,3 +243,20 @@ def test_one_row_of_a_wider_buffer():
     spork.spork_chunk_attn(s.shape, wide[:, :256].unflatten(1, (4, 64)), s.k, s.v, s.table, s.row_off, s.kv_len, s.out, s.lse,
                            s.chunk_ws)
     s.check([1], "one row")
+
+
+def test_two_batches_on_two_streams():
+    """Two batches with tables, pools and workspaces of their own, their steps in flight at the same time."""
+    servers = [Server(BF16, 8, 2, 128, 16, 6, 80, 24, 300, seed=21), Server(F32, 4, 2, 64, 32, 6, 80, 24, 300, seed=22)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i, (lens, new, parents) in enumerate(STEPS):
+        for s in servers:
+            s.projections()
+            s.set(lens, new, parents)
+            s.tokens(lens, new, parents)
+        torch.cuda.synchronize()
+        for s, stream in zip(servers, streams):
+            with torch.cuda.stream(stream):
+                s.launch()
+        for s in servers:
+            s.check(new, f"step {i}")

@@ -342,3 +342,18 @@ def test_long_rows_of_one_launch(n, most):
         assert want[0] == 0
         dev.step([max(x, 0) for x in lens2], [0] * n, parents, 4096)
         dev.check(model, want, 4096)
+
+
+@pytest.mark.parametrize("n", (3, 20))
+def test_slots_past_32_bits(n):
+    """Slots of blocks at the end of a pool of 2^27 + 9 blocks of 64 tokens, and behind its wrap."""
+    nb, bs, most = (1 << 27) + 9, 64, 8
+    dev = Device(n, nb, bs, most)
+    dev.queue[0] = nb - 3
+    dev.step([0] * n, [200, 70] + [0] * (n - 2), None, 300)
+    assert dev.status.item() == 0 and dev.queue.tolist() == [3, nb - 6]
+    rows = [[nb - 3, nb - 2, nb - 1, 0], [1, 2]]
+    assert [dev.table[s, :len(r)].tolist() for s, r in enumerate(rows)] == rows
+    want = [rows[0][i // bs] * bs + i % bs for i in range(200)] + [rows[1][i // bs] * bs + i % bs for i in range(70)]
+    assert dev.slots.tolist() == want + [-1] * 30 and max(want) > 1 << 32
+    assert dev.refs.sum().item() == 6
