@@ -578,7 +578,10 @@ struct Engine<float, D, BS> {
 // spread over the slots likewise. The reads and barriers are outside the
 // compiler's view (it would wait for the loads of later stages at every read),
 // with waits that name the registers; no read is in flight where a loop goes
-// round.
+// round. 2,048 rows behind 30,000 positions, 64 heads in groups of 8: 1.72 to 1.84 ms,
+// 1.13 to 1.21 PFLOP/s, at the 1.65 to 1.75 GHz that power leaves. (With stages of each
+// wave's own, a prompt of 4,096 tokens took 202 us against 134, three long chunks
+// beside 29 tokens 222 against 154, 24 prompts with heads of 64 channels 69 against 52.)
 // --------------------------------------------------------------------------
 constexpr int kRing = 8, kPer = 2;   // stages; stages that a barrier publishes
 constexpr int kAhead = kRing - kPer;
@@ -1373,6 +1376,11 @@ ChunkKernel pick_merge(int d) {
 
 }  // namespace
 
+// (Single tokens, 32 query and 8 KV heads of 128, a tile per KV head against this
+// rule: 128 sequences of up to 400 positions 51.1 and 38.3 us, 1,024 of up to 64
+// 209 and 66, of up to 400 309 and 234, of up to 2,000 994 and 1,002, 256 of up to
+// 2,000 254 and 264; 16 heads of 64, 256 of up to 400 127 and 61, 1,024 of up to 2,000
+// 1,037 and 955.)
 int32_t chunk_tile_heads(int32_t n_seqs, int32_t hkv) {
   int32_t n = 1;
   while (2 * n <= hkv && 2 * n <= kWaves && static_cast<int64_t>(n_seqs) * hkv >= 2ll * n * kChunkSlices) n *= 2;

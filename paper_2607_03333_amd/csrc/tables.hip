@@ -40,6 +40,9 @@ namespace {
 constexpr int kRowThreads = 256;   // of a row's workgroup
 constexpr int kSumThreads = 1024;  // of the one workgroup that sums the rows
 constexpr int kAtOnce = 4;         // entries of a row that a thread loads together
+// One token for each row, eager and in a graph, summed by all against a launch: 256
+// rows 18.7 and 12.8 us against 19.8 and 13.7, 1,024 18.1 and 17.4 against 19.5 and
+// 17.8, 2,048 25.3 and 25.4 against 25.1 and 24.9, 4,096 41 against 38.
 constexpr int kRowsSummedByAll = 1024;
 // Steps of one workgroup: at most so many rows (a wave each), entries of a row,
 // and new tokens. Half of the rows forking again, eager and in a graph, one launch
