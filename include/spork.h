@@ -439,7 +439,9 @@ int spork_tables_workspace_clear(const spork_tables* tables, void* workspace, si
  *      private copy (one copies entry); then one front per block that its
  *      new tokens open.
  * A row that neither changes nor appends has its own length in lens and 0 in
- * n_new. Outputs (device):
+ * n_new. What a step writes (tables, outputs, workspace) must not overlap itself
+ * or the inputs (SPORK_E_INVAL): lengths are advanced by a copy of kv_len behind
+ * the step, not by kv_len in place of lens. Outputs (device):
  *   slots[max_tokens] int64: the slot of every new token, in row order;
  *     -1 behind the last one (spork_kv_write skips those). NULL if
  *     max_tokens = 0;

@@ -1,0 +1,49 @@
+"""Calls of the entry points for steps whose lengths live on the GPU that are
+refused on the host because the kernels could not answer them: buffers that
+overlap, sizes at the end of 32 bits. On the CPU; nothing is launched."""
+import ctypes
+
+import pytest
+
+from paper_2607_03333_amd import spork
+
+INVAL, UNSUPPORTED = spork.SPORK_E_INVAL, spork.SPORK_E_UNSUPPORTED
+N, BLOCKS, MOST, TOKENS = 40, 100, 8, 64
+WS = 1 << 20
+
+
+def step_args(**kw):
+    """A step of N rows whose buffers lie apart, 16 MiB each from the next; nothing follows the pointers."""
+    names = ("table", "held", "refcount", "free_queue", "queue", "lens", "n_new", "parents", "slots", "positions", "row_off",
+             "kv_len", "copies", "n_copies", "status", "workspace")
+    f = {name: (i + 1) << 24 for i, name in enumerate(names)}
+    f.update(kw)
+    return f
+
+
+def step(f):
+    t = spork.spork_tables(BLOCKS, 16, N, MOST, f["table"], f["held"], f["refcount"], f["free_queue"], f["queue"])
+    rc = spork.lib().spork_tables_step(ctypes.byref(t), f["lens"], f["n_new"], f["parents"], TOKENS, f["slots"], f["positions"],
+                                       f["row_off"], f["kv_len"], f["copies"], f["n_copies"], f["status"], f["workspace"], WS, None)
+    return rc, spork.lib().spork_last_error().decode()
+
+
+INPUTS = ("lens", "n_new", "parents")
+WRITTEN = {"table": 4 * N * MOST, "held": 4 * N, "refcount": 4 * BLOCKS, "free_queue": 4 * BLOCKS, "queue": 8, "slots": 8 * TOKENS,
+           "positions": 4 * TOKENS, "row_off": 4 * (N + 1), "kv_len": 4 * N, "copies": 12 * N, "n_copies": 4, "status": 4}
+
+
+@pytest.mark.parametrize("written", sorted(WRITTEN))
+def test_what_a_step_writes_lies_apart(written):
+    """The buffer itself in place of another, and its last four bytes as the first of another."""
+    for other in INPUTS + tuple(w for w in WRITTEN if w != written):
+        apart = step_args()
+        for at in (apart[written], apart[written] + WRITTEN[written] - 4):
+            rc, why = step(step_args(**{other: at}))
+            assert rc == INVAL and "overlap" in why, (written, other)
+
+
+def test_the_workspace_lies_apart():
+    for other in INPUTS + tuple(WRITTEN):
+        rc, why = step(step_args(**{other: step_args()["workspace"] + 4}))
+        assert rc == INVAL and "overlap" in why, other
