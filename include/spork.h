@@ -493,7 +493,8 @@ int spork_chunk_workspace_bytes(const spork_shape* shape, int32_t n_seqs, int32_
  * int32 [n_seqs]): as spork_tables_step makes them. Sequence s owns query rows
  * row_off[s] .. row_off[s+1]-1, the last of its kv_len[s] positions: row r of
  * n attends to positions 0 .. kv_len[s] - n + r. A row with no position to
- * attend to (kv_len[s] < n) gives zeros and an lse of -inf. A sequence without
+ * attend to (kv_len[s] < n) gives zeros and an lse of -inf; one whose scores hold
+ * a NaN or +inf gives NaN in both, and no other row changes. A sequence without
  * rows is not read.
  * out (device [n_rows][Hq][D] dtype), lse (device [n_rows][Hq] float32, natural
  * log, nullable). Rows that no sequence owns are left as they are.

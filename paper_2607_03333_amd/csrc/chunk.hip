@@ -899,6 +899,14 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
   }
 }
 
+// A row's factor and log-sum-exp from its reference (base 2) and sum: zero and -inf
+// where it attends to nothing, which is where the sum is zero. (One that is no
+// number goes on into both.)
+__device__ __forceinline__ float reciprocal_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // Eight channels of a row, in the output type.
 __device__ __forceinline__ void store_out(float* p, f32x4 x, f32x4 y) {
   reinterpret_cast<f32x4*>(p)[0] = x;
@@ -1163,9 +1171,9 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           const int row = p / group;
           const size_t at_row =
               static_cast<size_t>(sq.row0 + r0 + row) * a.hq + (head0 + tr / row_tiles) * group + (p - row * group);
-          const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+          const float inv = reciprocal_sum(l);
           store_out(static_cast<T*>(a.out) + at_row * D + 4 * c, x * inv, y * inv);
-          if (a.lse != nullptr && c == 0) a.lse[at_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+          if (a.lse != nullptr && c == 0) a.lse[at_row] = log_sum(m, l);
         } else {
           const size_t at_row = piece_row(slice, tok_lo == 0 ? 1 : 0) + 32 * tr + r;
           store_out(a.part_o + at_row * D + 4 * c, x, y);
@@ -1243,12 +1251,12 @@ struct MergeRow {
 
 template <typename T, int D>
 __device__ __forceinline__ void merge_out(const ChunkArgs& a, const MergeRow& r, int sub, f32x4 o, float m, float l) {
-  o *= l > 0.0f ? 1.0f / l : 0.0f;
+  o *= reciprocal_sum(l);
   if constexpr (sizeof(T) == 4)
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + r.out * D + 4 * sub) = o;
   else
     *reinterpret_cast<uint2*>(static_cast<__bf16*>(a.out) + r.out * D + 4 * sub) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-  if (a.lse != nullptr && sub == 0) a.lse[r.out] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+  if (a.lse != nullptr && sub == 0) a.lse[r.out] = log_sum(m, l);
 }
 
 // Up to kPieces pieces, kTogether steps of rows at a time.

@@ -1,0 +1,38 @@
+"""spork_chunk_attn on values that are not ordinary: queries that are no
+numbers."""
+import pytest
+import torch
+
+from paged_cases import bounds
+from test_gpu_chunk import BF16, F32, Case
+
+pytestmark = pytest.mark.gpu
+
+# new tokens, contexts, query and KV heads: tiles that no cut goes through (of one wave's rows, of several and of a
+# whole workgroup's), and tiles in pieces
+BATCHES = [([3, 1], [40, 200], 4, 2), ([70, 1], [90, 30], 2, 1), ([64], [80], 4, 1), ([1], [3001], 2, 2), ([1], [20011], 1, 1),
+           ([300], [2500], 4, 1), ([9], [9000], 4, 1)]
+
+
+@pytest.mark.parametrize("bad", (float("nan"), float("inf")))
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("new,kv,hq,hkv", BATCHES)
+def test_a_query_row_that_is_no_number(new, kv, hq, hkv, d, dtype, bad):
+    """Its outputs and lse are NaN, not those of a row with nothing to see, and every other row's are right. (Eight
+    infinite channels of both signs: a score is NaN or infinite, and not -inf for all of a row's 17 keys or more.)"""
+    c = Case(dtype, hq, hkv, d, 16, new, kv)
+    ref = c.reference()
+    hit = torch.zeros_like(c.lse, dtype=torch.bool)
+    for row, head in ((0, 0), (c.rows - 1, hq - 1)):
+        hit[row, head] = True
+        c.q[row, head, 4:12] = bad
+        c.q[row, head, 4:12:2] *= -1
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.isnan(c.out[hit]).all() and torch.isnan(c.lse[hit]).all()
+    o_tol, l_tol = bounds(dtype, *ref, c.scale, max(kv), d)
+    rest = ~hit[:c.rows].cpu()
+    assert ((c.out[:c.rows].double().cpu() - ref[0]).abs() <= o_tol)[rest].all()
+    assert ((c.lse[:c.rows].double().cpu() - ref[1]).abs() <= l_tol)[rest].all()
+    assert (c.out[c.rows:] == 7.5).all() and (c.lse[c.rows:] == 7.5).all()
