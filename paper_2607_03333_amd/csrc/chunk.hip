@@ -531,7 +531,7 @@ struct Engine<float, D, BS> {
       if (__ballot(mx > m[u] + kSlack) != 0) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (mx > m[u]) {
+        if (mx > m[u] + kSlack) {  // a row's own: its bits do not depend on its neighbours
           const float alpha = exp2_fast(m[u] - mx);
           l[u] *= alpha;
 #pragma unroll
@@ -820,7 +820,8 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
             const float p0 = exp2_fast(__builtin_fmaf(sv[i], c, -ref)), p1 = exp2_fast(__builtin_fmaf(sv[i + 1], c, -ref));
-            ps += p0 + p1;
+            ps += p0;  // in the order above: rows that stay keep their bits
+            ps += p1;
             pw[i / 2] = pack2(p0, p1);
           }
         }

@@ -1,5 +1,5 @@
 """spork_chunk_attn on values that are not ordinary: queries that are no
-numbers."""
+numbers, and what their rows do to others."""
 import pytest
 import torch
 
@@ -36,3 +36,23 @@ def test_a_query_row_that_is_no_number(new, kv, hq, hkv, d, dtype, bad):
     assert ((c.out[:c.rows].double().cpu() - ref[0]).abs() <= o_tol)[rest].all()
     assert ((c.lse[:c.rows].double().cpu() - ref[1]).abs() <= l_tol)[rest].all()
     assert (c.out[c.rows:] == 7.5).all() and (c.lse[c.rows:] == 7.5).all()
+
+
+@pytest.mark.parametrize("change", ("nan", "inf", "larger"))
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("new,kv,hq,hkv", BATCHES)
+def test_rows_do_not_depend_on_their_neighbours(new, kv, hq, hkv, d, dtype, change):
+    """Another query in one row, the scores of which take the softmax other ways: every other row's bits stay."""
+    c = Case(dtype, hq, hkv, d, 16, new, kv, gain=0.5)
+    c.run()
+    torch.cuda.synchronize()
+    out, lse = c.out.clone(), c.lse.clone()
+    rest = torch.ones_like(lse, dtype=torch.bool)
+    for row, head in ((0, 0), (c.rows - 1, hq - 1)):
+        rest[row, head] = False
+        c.q[row, head] *= {"nan": float("nan"), "inf": float("inf"), "larger": 40.0}[change]
+    c.run()
+    torch.cuda.synchronize()
+    assert not torch.equal(c.lse, lse)
+    assert torch.equal(c.out[rest], out[rest]) and torch.equal(c.lse[rest], lse[rest])
