@@ -1,5 +1,6 @@
 """spork_chunk_attn on values that are not ordinary: queries that are no
-numbers, and what their rows do to others."""
+numbers, and what their rows do to others; scores that rise behind a row's first
+stage."""
 import pytest
 import torch
 
@@ -56,3 +57,49 @@ def test_rows_do_not_depend_on_their_neighbours(new, kv, hq, hkv, d, dtype, chan
     torch.cuda.synchronize()
     assert not torch.equal(c.lse, lse)
     assert torch.equal(c.out[rest], out[rest]) and torch.equal(c.lse[rest], lse[rest])
+
+
+def raise_scores(c, up):
+    """Scores of the first 32 positions as they are, those behind them `up` (base 2) higher: channel 0 of every query is 1,
+    of those keys what makes the difference."""
+    bs = c.k.shape[2]
+    key = torch.tensor(up * 0.6931471805599453 / c.scale).to(c.dtype)
+    c.q[:, :, 0] = 1.0
+    for s, length in enumerate(c.kv):
+        at = torch.arange(length, device="cuda")
+        values = torch.where(at < 32, 0.0, key.item()).to(c.dtype)
+        c.k[c.table[s].long()[at // bs], :, at % bs, 0] = values[:, None]
+        c.contexts[s][0][:, :, 0] = values.double().cpu()[:, None]
+
+
+@pytest.mark.parametrize("up", (3.5, 6.0, 7.5, 9.0))
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_scores_that_rise_behind_the_first_stage(dtype, d, up):
+    for new, kv, hq, hkv in (([70, 1], [900, 300], 4, 1), ([3], [700], 2, 2), ([300], [300], 4, 1)):
+        c = Case(dtype, hq, hkv, d, 16, new, kv, gain=0.5)
+        raise_scores(c, up)
+        c.run_and_check(f"rise of {up}")
+
+
+@pytest.mark.parametrize("hq,hkv,d,bs,new,kv", [(16, 16, 64, 32, [512] * 8, [4512] * 8), (64, 8, 128, 16, [1024], [16000])])
+def test_scores_that_rise_cost_no_more(hq, hkv, d, bs, new, kv):
+    """A reference that is below all later scores moves once: no stage behind that takes the long way. (Where it stayed,
+    these took 1.5 and 1.34 times as long; the bound is between that and the same.)"""
+    calls = []
+    for up in (0.0, 6.0):
+        c = Case(BF16, hq, hkv, d, bs, new, kv, gain=0.3)
+        raise_scores(c, up)
+        c.run()
+        calls.append((c, []))
+    for _ in range(7):
+        for c, times in calls:
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            for _ in range(10):
+                c.run()
+            end.record()
+            torch.cuda.synchronize()
+            times.append(begin.elapsed_time(end))
+    (_, level), (_, raised) = calls
+    assert sorted(raised)[3] < 1.2 * sorted(level)[3], (level, raised)
