@@ -484,7 +484,8 @@ int spork_chunk_workspace_bytes(const spork_shape* shape, int32_t n_seqs, int32_
 
 /* Attention of the new tokens of a ragged batch over the paged cache: prompt
  * chunks of any length beside single tokens (head_dim 64 or 128, block_size
- * 16 or 32, at most 256 query heads per KV head).
+ * 16 or 32, at most 256 query heads per KV head, max_blocks * block_size below
+ * 2^31 - 4096).
  * q (device, n_rows rows of [Hq][D] dtype, q_stride elements apart, rows
  * 16-byte aligned: the query part of a fused projection's rows will do);
  * k_cache, v_cache (device pools of num_blocks blocks; the rows' own keys and

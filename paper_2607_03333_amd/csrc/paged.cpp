@@ -18,6 +18,10 @@ using namespace spork::capi;
 // A launch has fewer than 2^32 threads: so many workgroups of 256.
 constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
 
+// Loops over positions count in 32 bits and look a few steps ahead, of at most 1,024
+// each: so far below 2^31 they end.
+constexpr int64_t kHeadroom = 4096;
+
 bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) == 0; }
 
 // The sizes that every tables call checks.
@@ -213,8 +217,8 @@ int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, 
       return fail(SPORK_E_INVAL, "q_stride must cover a query row and keep rows 16-byte aligned");
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
       return fail(SPORK_E_INVAL, "q, pools and out must be 16-byte aligned");
-    if (static_cast<int64_t>(max_blocks) * shape->block_size > INT_MAX)
-      return fail(SPORK_E_UNSUPPORTED, "max_blocks * block_size must be below 2^31");
+    if (static_cast<int64_t>(max_blocks) * shape->block_size > INT_MAX - kHeadroom)
+      return fail(SPORK_E_UNSUPPORTED, "max_blocks * block_size must be below 2^31 - 4096");
     const float scale_log2 = shape->sm_scale * 1.4426950408889634f;
     if (!std::isfinite(scale_log2)) return fail(SPORK_E_INVAL, "sm_scale is out of range");
     if (workspace == nullptr || !aligned256(workspace))

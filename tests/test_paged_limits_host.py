@@ -47,3 +47,18 @@ def test_the_workspace_lies_apart():
     for other in INPUTS + tuple(WRITTEN):
         rc, why = step(step_args(**{other: step_args()["workspace"] + 4}))
         assert rc == INVAL and "overlap" in why, other
+
+
+@pytest.mark.parametrize("block_size", (16, 32))
+def test_contexts_near_the_end_of_32_bits(block_size):
+    """The kernel's positions run a few stages past a context's end, in 32 bits: wider tables are refused. (Without a
+    workspace, so that nothing is launched where the size is taken.)"""
+    shape = ctypes.byref(spork.make_shape(8, 2, 64, block_size, spork.SPORK_DTYPE_BF16, 0.1))
+    p = 1 << 20
+
+    def call(max_blocks):
+        return spork.lib().spork_chunk_attn(shape, p, 8 * 64, p, p, 9, p, max_blocks, p, p, 1, 1, p, None, None, 0, None)
+
+    least = ((1 << 31) - 4096) // block_size
+    assert [call(m) for m in (least, least + 1, (1 << 31) // block_size - 1, (1 << 31) - 1)] == [UNSUPPORTED] * 4
+    assert call(least - 1) == INVAL
