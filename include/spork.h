@@ -393,7 +393,9 @@ int spork_ngram_propose(const int32_t* tokens, const int64_t* seq_off, int32_t n
 
 /* Block tables in device memory, owned by the caller. Row s is a sequence
  * (or a place for one); entries 0 .. held[s]-1 of its table row are its
- * blocks in order. The rules are the block manager's (above). */
+ * blocks in order. The rules are the block manager's (above). Sizes
+ * (SPORK_E_UNSUPPORTED): n_seqs * (max_blocks + 1) below 2^31 - 1, max_blocks *
+ * block_size below 2^31, max_blocks below 2^31 - 4096. */
 typedef struct spork_tables {
   int32_t num_blocks; /* blocks of the pools */
   int32_t block_size; /* tokens per block */

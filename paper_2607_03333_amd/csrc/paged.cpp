@@ -18,8 +18,8 @@ using namespace spork::capi;
 // A launch has fewer than 2^32 threads: so many workgroups of 256.
 constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
 
-// Loops over positions count in 32 bits and look a few steps ahead, of at most 1,024
-// each: so far below 2^31 they end.
+// Loops over positions and table columns count in 32 bits and run a step of up to
+// 1,024 past the last, or look a few of 256 ahead: so far below 2^31 none wraps.
 constexpr int64_t kHeadroom = 4096;
 
 bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) == 0; }
@@ -30,8 +30,9 @@ int check_tables(const spork_tables* t) {
   if (t->num_blocks <= 0 || t->block_size <= 0 || t->n_seqs <= 0 || t->max_blocks <= 0)
     return fail(SPORK_E_INVAL, "num_blocks, block_size, n_seqs and max_blocks must be positive");
   if (t->n_seqs * (int64_t{1} + t->max_blocks) >= INT_MAX ||
-      static_cast<int64_t>(t->max_blocks) * t->block_size > INT_MAX)
-    return fail(SPORK_E_UNSUPPORTED, "n_seqs * (max_blocks + 1) and max_blocks * block_size must be below 2^31");
+      static_cast<int64_t>(t->max_blocks) * t->block_size > INT_MAX || t->max_blocks > INT_MAX - kHeadroom)
+    return fail(SPORK_E_UNSUPPORTED,
+                "n_seqs * (max_blocks + 1) must be below 2^31 - 1, max_blocks * block_size below 2^31 and max_blocks below 2^31 - 4096");
   return SPORK_OK;
 }
 

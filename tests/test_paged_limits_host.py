@@ -62,3 +62,21 @@ def test_contexts_near_the_end_of_32_bits(block_size):
     least = ((1 << 31) - 4096) // block_size
     assert [call(m) for m in (least, least + 1, (1 << 31) // block_size - 1, (1 << 31) - 1)] == [UNSUPPORTED] * 4
     assert call(least - 1) == INVAL
+
+
+def test_rows_near_the_end_of_32_bits():
+    """The kernels' columns run up to 1,024 entries past a row's last one, in 32 bits: wider rows are refused."""
+    size = ctypes.c_size_t()
+
+    def need(max_blocks):
+        t = spork.spork_tables(9, 1, 1, max_blocks, None, None, None, None, None)
+        return spork.lib().spork_tables_workspace_bytes(ctypes.byref(t), ctypes.byref(size))
+
+    least = (1 << 31) - 4096
+    assert [need(m) for m in (least, least + 1, (1 << 31) - 3)] == [UNSUPPORTED] * 3
+    assert need(least - 1) == spork.SPORK_OK and size.value > 0
+    f = step_args()
+    t = spork.spork_tables(BLOCKS, 1, 1, least, f["table"], f["held"], f["refcount"], f["free_queue"], f["queue"])
+    rc = spork.lib().spork_tables_step(ctypes.byref(t), f["lens"], f["n_new"], f["parents"], TOKENS, f["slots"], f["positions"],
+                                       f["row_off"], f["kv_len"], f["copies"], f["n_copies"], f["status"], None, WS, None)
+    assert rc == UNSUPPORTED
