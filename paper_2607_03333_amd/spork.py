@@ -399,10 +399,23 @@ def _want(name, x, size, *shape):
     passes: the library says what may be NULL)."""
     if x is None:
         return None
-    if x.shape != shape or x.element_size() != size or not x.is_contiguous() or x.is_floating_point():
+    if x.shape != shape or x.element_size() != size or not x.is_contiguous() or x.is_floating_point() or x.is_complex():
         raise ValueError(f"{name} must be a contiguous tensor of {8 * size}-bit integers of shape {list(shape)}, "
                          f"not {x.dtype} {list(x.shape)}")
     return x.data_ptr()
+
+
+_element_types = {}
+
+
+def _of_dtype(dtype, *tensors):
+    """Whether all are of the library's dtype, or its bits as integers (integers are pointers and pass)."""
+    if not _element_types:
+        import torch
+        _element_types.update({SPORK_DTYPE_BF16: (torch.bfloat16, torch.int16, torch.uint16),
+                               SPORK_DTYPE_F32: (torch.float32, torch.int32, torch.uint32)})
+    types = _element_types.get(dtype, ())
+    return all(x is None or isinstance(x, int) or x.dtype in types for x in tensors)
 
 
 def _on_gpu(*tensors):
@@ -464,6 +477,8 @@ def spork_tables_step(tables, lens, n_new, parents, slots, positions, row_off, k
 
 def spork_kv_copy_batch(shape, k_cache, v_cache, num_blocks, copies, n_copies, stream=None):
     most = copies.shape[0]
+    if not _of_dtype(shape.dtype, k_cache, v_cache):
+        raise ValueError("the pools must be of the shape's dtype")
     _on_gpu(k_cache, v_cache, copies, n_copies)
     _check(lib().spork_kv_copy_batch(ctypes.byref(shape), _ptr(k_cache), _ptr(v_cache), num_blocks,
                                      _want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1),
@@ -485,8 +500,7 @@ def spork_chunk_attn(shape, q, k_cache, v_cache, table, row_off, kv_len, out, ls
         raise ValueError("the rows of q must be contiguous")
     if tuple(out.shape) != (n_rows, hq, d) or (lse is not None and tuple(lse.shape) != (n_rows, hq)):
         raise ValueError("out must be [rows, hq, head_dim] and lse [rows, hq]")
-    elem = {SPORK_DTYPE_F32: 4, SPORK_DTYPE_BF16: 2}.get(shape.dtype)  # bf16 may come as 16-bit integers
-    if any(x.element_size() != elem for x in (q, k_cache, v_cache, out)) or (lse is not None and lse.element_size() != 4):
+    if not _of_dtype(shape.dtype, q, k_cache, v_cache, out) or not _of_dtype(SPORK_DTYPE_F32, lse):
         raise ValueError("q, the pools and out must be of the shape's dtype and lse float32")
     bs = shape.block_size
     if tuple(k_cache.shape) != (blocks, shape.hkv, bs, d) or tuple(v_cache.shape) != (blocks, shape.hkv, d, bs):
