@@ -1352,12 +1352,13 @@ __global__ void __launch_bounds__(256) merge_kernel(AttnArgs a) {
     for (int c0 = beg; c0 < end; c0 += 8)
       merge_batch<8, D, OutT>(a, c0, min(8, end - c0), c0 == beg, lane, run_max, mu, sum, acc);
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  // (a sum that is no number, of a query that holds one, goes on into both)
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   OutT* out = static_cast<OutT*>(a.out) + static_cast<size_t>(o) * D + merge_channel<D, OutT>(lane);
 #pragma unroll
   for (int e = 0; e < PER; ++e) out[e] = static_cast<OutT>(acc[e] * inv);
   if (lane == 0 && a.lse != nullptr)
-    a.lse[o] = sum > 0.0f ? (mu + __log2f(sum)) * kLn2 : kNegInf;
+    a.lse[o] = sum == 0.0f ? kNegInf : (mu + __log2f(sum)) * kLn2;
 }
 
 __global__ void __launch_bounds__(256) counter_reset_kernel(int32_t* counters, int32_t n) {
