@@ -600,7 +600,6 @@ __device__ __forceinline__ void barrier_lds() { asm volatile("s_waitcnt lgkmcnt(
 __device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
 // A tile, or the piece of it that a slice works on.
 struct Tile {
-  int row0, hz0;        // query row of the first packed row, and its last visible position
   int n_packed, head;
   int tok_lo, tok_hi;
 };
@@ -1104,7 +1103,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       const float c = a.scale_log2;
       if (wide) {
         if constexpr (kWide)
-          wide_tile<D, BS>(a, Tile{sq.row0 + r0, sq.kv - sq.rows + r0, n_packed, head, tok_lo, tok_hi}, pg, smem, lane, wave, e);
+          wide_tile<D, BS>(a, Tile{n_packed, head, tok_lo, tok_hi}, pg, smem, lane, wave, e);
         barrier_lds();  // the ring is read: a wave may load its slot for the next tile
       } else if (works) {
         // K and V of a stage are loaded as soon as the slot's halves have been read:

@@ -249,7 +249,6 @@ __device__ __forceinline__ int status_of(const TablesArgs& a, const Sums& all, i
 }
 
 __device__ __forceinline__ void write_row_sums(const TablesArgs& a, int i, const Sums& before, const Sums& own) {
-  a.free_off[i] = before.frees;
   a.take_off[i] = before.takes;
   a.copy_off[i] = own.copies ? before.copies : -1;
   a.row_off[i + 1] = static_cast<int>(min(before.tokens + own.tokens, static_cast<int64_t>(INT_MAX)));
@@ -284,7 +283,10 @@ __global__ void __launch_bounds__(kSumThreads) tables_sum(TablesArgs a) {
       if (w < wave) before = before + y;
       done = done + y;
     }
-    if (i < a.n_seqs) write_row_sums(a, i, before, x);
+    if (i < a.n_seqs) {
+      a.free_off[i] = before.frees;
+      write_row_sums(a, i, before, x);
+    }
   }
   if (tid == 0) write_totals(a, done, status_of(a, done, error, front, count));
 }

@@ -13,11 +13,11 @@ namespace spork {
 // the step's totals. All of it lies in the workspace, behind the block words.
 struct TablesTotals {
   int32_t error;         // lowest status of the rows, 0 between steps
-  int32_t zero;
+  int32_t pad0;
   int32_t status;        // the step's status
   int32_t front;         // the queue's front before the step
   int32_t frees, takes;  // of all rows
-  int32_t pad[2];
+  int32_t pad1[2];
 };
 
 struct TablesArgs {
@@ -45,7 +45,8 @@ struct TablesArgs {
   int32_t* frees;      // blocks that the row's releases put into the queue
   int32_t* takes;      // blocks that the row takes from it
   int32_t* copies_of;  // 1: the row makes a copy
-  int32_t* free_off;   // sums of these over the rows before; copy_off: -1 where the row makes no copy
+  int32_t* free_off;   // sums of these over the rows before (free_off: where tables_sum makes them); copy_off: -1 where
+                       // the row makes no copy
   int32_t* take_off;
   int32_t* copy_off;
   TablesTotals* totals;
