@@ -70,10 +70,19 @@ constexpr int kTileCost = 1000;
 // Least length of a slice: three fp32 prompts took 47.4 us at 2,048, 33.2 at 1,024,
 // 31.3 at 512, 27.8 at 320; one token over 1,000 positions 25.5, 17.8, 16.9, 16.5.
 constexpr int kMinSlice = 320;
-constexpr int kMinPiece = 256;      // least cost of a piece: a cut closer to a tile's end moves to it
+// Least cost of a piece: a cut closer to a tile's end moves to it. At 64, 256, 512 and
+// 1,024: eight fp32 tokens over up to 1,500 positions 16.9, 18.2, 19.1, 26.5 us, one
+// bf16 token over 1,000 17.0, 16.6, 17.5, 20.4; pieces of many rows, which cost more
+// to write and join, 24 prompts of up to 777 tokens 54.9, 53.7, 53.8, 51.9, four
+// chunks beside 60 tokens, 64 heads, 193, 193, 192, 188; the other batches the same.
+constexpr int kMinPiece = 256;
 // A token of a tile of `heads` KV heads with so many row tiles each: bf16 by
 // bytes until the products weigh more; fp32 products (64 flop per cycle and SIMD)
-// weigh more from the first row tile.
+// weigh more from the first row tile. Three bf16 chunks beside 29 tokens 157 us, with
+// one price for all tiles 185, with twice as much from five row tiles on 197; four
+// chunks beside 60 tokens 193, 215, 237. Three fp32 prompts 28 us, at half the price
+// 30, at twice 27.5, at one price for any number of row tiles 57; two fp32 chunks
+// behind 1,500 to 2,000 positions 38.8, 38.9, 42.6, 59.
 __device__ __forceinline__ int token_cost(const ChunkArgs& a, int row_tiles, int heads) {
   const int wide = a.head_dim == 128 ? 2 : 1;
   if (a.dtype == 0) return 2 * wide * row_tiles * heads;
@@ -1395,6 +1404,7 @@ ChunkKernel pick_merge(int d) {
 
 }  // namespace
 
+// By the sequences that there may be: how many have rows only the GPU knows.
 // (Single tokens, 32 query and 8 KV heads of 128, a tile per KV head against this
 // rule: 128 sequences of up to 400 positions 51.1 and 38.3 us, 1,024 of up to 64
 // 209 and 66, of up to 400 309 and 234, of up to 2,000 994 and 1,002, 256 of up to

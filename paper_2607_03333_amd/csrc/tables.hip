@@ -49,7 +49,12 @@ constexpr int kRowsSummedByAll = 1024;
 // against four: 1 row 9.0 and 8.4 us against 16.0 and 9.3; 8 rows of 250 tokens 11.5
 // and 11.8 against 16.9 and 15.1; 16 rows 12.6 and 12.9 against 17.1 and 14.8; 16 rows
 // of 500 blocks 13.2 and 13.5 against 17.1 and 13.4, of 1,000 blocks 19.1 and 19.4
-// against 17.1 and 13.5; 4,096 new tokens 10.7 and 10.9 against 17.0 and 13.0.
+// against 17.1 and 13.5; 4,096 new tokens 10.7 and 10.9 against 17.0 and 13.0. Long
+// rows gain where they append one token (4 rows of 2,000 entries 12.4 and 9.4 against
+// 21.2 and 12.2, of 8,100 12.2 and 9.4 against 21.1 and 12.3) and lose more where they
+// fork (22.6 and 22.8 against 21.7 and 15.3; 69 against 30) or end, each step alone
+// (of 500 entries 29 against 27, of 2,000 69 against 34, of 8,100 210 against 72).
+// What a step does only the GPU knows, so the limit is on what a row can hold.
 constexpr int kOneThreads = 1024;
 constexpr int kOneRows = 16, kOneEntries = 512, kOneTokens = 4096;
 static_assert(kOneRows * 64 == kOneThreads, "a wave for every row");
