@@ -500,7 +500,9 @@ int spork_chunk_workspace_bytes(const spork_shape* shape, int32_t n_seqs, int32_
  * a NaN or +inf gives NaN in both, and no other row changes. A sequence without
  * rows is not read.
  * out (device [n_rows][Hq][D] dtype), lse (device [n_rows][Hq] float32, natural
- * log, nullable). Rows that no sequence owns are left as they are.
+ * log, nullable). Rows that no sequence owns are left as they are. bf16: scores,
+ * sums and outputs are float32 up to the end; probabilities are rounded to bf16
+ * (by at most 2^-8 of each) before they weigh the values, outputs when stored.
  * Keys and values of positions below kv_len must be finite (an infinity or NaN
  * in one may show in rows that don't attend to it); whatever else the blocks
  * hold is not seen. Offsets are clamped to n_rows, lengths to what max_blocks
