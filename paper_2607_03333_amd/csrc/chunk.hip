@@ -233,7 +233,7 @@ __device__ __forceinline__ void lds_wait(u32x4 (&r)[N]) {
 // Whether the lane or the other one of its row (32 lanes on) is among `past`: the
 // row's reference then moves to its largest score, however little that lies above
 // it. (Scores 4 to 8 above the reference would take every stage back here: 2,048
-// rows behind 30,000 positions, each 6 above its first stage, 2.24 ms against 1.66.)
+// rows behind 30,000 positions, each 6 above its first stage, 2.24 ms against 1.60.)
 __device__ __forceinline__ bool row_past(uint64_t past, int lane) {
   return ((past | past >> 32 | past << 32) >> lane & 1) != 0;
 }
