@@ -1,0 +1,577 @@
+"""From a projection's rows to attention over a cache in 8 bits, as cases that can be timed.
+
+Three kinds of call: queries and keys rotated by their positions, with or without
+their norm (``spork_qk_rope``); the new tokens of a step on their way into a cache
+of 8-bit codes with a scale for each block and head, where keys and queries are
+normed and rotated on the way (``spork_kv8_write``, behind the copies of
+copy-on-write by ``spork_kv8_copy_batch``); and the attention of prompt chunks and
+single tokens that reads that cache (``spork_kv8_attn``).
+
+``own`` chooses between the library's calls and the same in plain torch.
+``listed()`` are sizes that a server meets, ``draw(rng)`` spreads them over
+their ranges. Lengths come from the case itself (``lens``), values from the seed.
+"""
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+_TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+_ELEM = {"bf16": 2, "f32": 4}
+
+# Query heads, KV heads and head size: the models that the library's workloads are shaped on, and other groupings.
+QWEN3_4B = dict(hq=32, hkv=8, d=128)
+QWEN3_32B = dict(hq=64, hkv=8, d=128)
+QWEN3_30B_A3B = dict(hq=32, hkv=4, d=128)
+SMALL_F32 = dict(hq=4, hkv=2, d=64)
+GROUPS_OF_7 = dict(hq=28, hkv=4, d=128)
+NARROW_HEADS = dict(hq=16, hkv=16, d=64)
+ONE_KV_HEAD = dict(hq=16, hkv=1, d=128)
+_HEADS = (QWEN3_4B, QWEN3_32B, QWEN3_30B_A3B, GROUPS_OF_7, NARROW_HEADS, ONE_KV_HEAD)
+
+# The rotation: base of the frequencies, and the scaling by parts of a context four times as long as the one trained on.
+_BASE, _FACTOR, _TRAINED, _FAST, _SLOW = 1e6, 4.0, 32768, 32.0, 1.0
+_EPS = 1e-6
+_TOP = 448.0  # of the 8-bit codes
+_LEAST, _MOST_EXP = -100, 120  # of a scale's exponent
+
+
+def _rotate(name, heads, **kw):
+    """Queries and keys of `rows` tokens at positions up to pos_hi, inside the rows of a fused projection."""
+    case = dict(name=name, kind="rotate", dtype="bf16", rows=1, pos_hi=1, rotary=heads["d"], interleaved=False, norm=False,
+                scaled=False)
+    case.update(heads)
+    case.update(kw)
+    return case
+
+
+def _append(name, heads, **kw):
+    """new_lo..new_hi new tokens of each of `seqs` sequences behind ctx_lo..ctx_hi tokens, into the cache in 8 bits; `rotary`,
+    `norm`: what happens to queries and keys on the way (neither: keys and values only). copies: the block that a sequence
+    ends in is another's as well and is copied first."""
+    case = dict(name=name, kind="append", dtype="bf16", block_size=16, seqs=1, new_lo=1, new_hi=1, ctx_lo=0, ctx_hi=0,
+                rotary=heads["d"], interleaved=False, norm=True, scaled=False, copies=False, lens=1)
+    case.update(heads)
+    case.update(kw)
+    return case
+
+
+def _attend(name, heads, **kw):
+    """An attention call: `chunks` sequences with chunk_lo..chunk_hi new tokens and `singles` with one, each behind
+    ctx_lo..ctx_hi tokens of context. `fused`: the query rows lie inside rows that hold keys and values too."""
+    case = dict(name=name, kind="attend", dtype="bf16", block_size=16, chunks=0, chunk_lo=1, chunk_hi=1, singles=0,
+                ctx_lo=0, ctx_hi=0, fused=False, q_gain=1.0, lens=1)
+    case.update(heads)
+    case.update(kw)
+    return case
+
+
+def listed():
+    return [
+        # One user's next token, far along: the latency of a launch.
+        _rotate("rotate-one", QWEN3_4B, pos_hi=120000),
+        # A prompt in full precision, pairs side by side, half of each head.
+        _rotate("rotate-part", SMALL_F32, dtype="f32", rows=4001, pos_hi=4000, rotary=32, interleaved=True),
+        # A decode batch, normed and rotated.
+        _rotate("norm-rotate-decode", QWEN3_32B, rows=96, pos_hi=32768, norm=True),
+        # A long chunk at the end of a context that needed scaling.
+        _rotate("norm-rotate-prompt", QWEN3_30B_A3B, rows=8192, pos_hi=131071, norm=True, scaled=True),
+        # A decode step of a batch: one token each, inside half-filled blocks.
+        _append("append-decode", QWEN3_4B, seqs=96, ctx_lo=3, ctx_hi=8190),
+        # The whole of a prompt.
+        _append("append-prompt", QWEN3_4B, new_lo=4096, new_hi=4096),
+        # Forks with their openers: the blocks that they end in are copied, keys and values come ready.
+        _append("append-forks", QWEN3_30B_A3B, seqs=192, new_lo=8, new_hi=50, ctx_lo=500, ctx_hi=32768, rotary=0, norm=False,
+                copies=True),
+        # One user's next token behind a short context.
+        _attend("attend-one", QWEN3_4B, singles=1, ctx_lo=1000, ctx_hi=1000),
+        # A decode batch of very different lengths, the queries inside the rows of a fused projection.
+        _attend("attend-decode", QWEN3_4B, singles=96, ctx_lo=3, ctx_hi=8190, fused=True, q_gain=3.0),
+        # Two very long contexts, one token each: few rows, a long axis.
+        _attend("attend-long", QWEN3_30B_A3B, singles=2, ctx_lo=120000, ctx_hi=131070, block_size=32),
+        # A late chunk of a long prompt: the largest.
+        _attend("attend-late-chunk", QWEN3_32B, chunks=1, chunk_lo=2048, chunk_hi=2048, ctx_lo=30000, ctx_hi=30000, q_gain=3.0),
+        # Chunks of prompts beside sequences that decode, as a server mixes them.
+        _attend("attend-mixed", QWEN3_30B_A3B, chunks=3, chunk_lo=300, chunk_hi=512, singles=29, ctx_lo=1, ctx_hi=8000),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(math.exp(rng.uniform(math.log(max(lo, 1)), math.log(hi + 1))))))
+
+
+# Most that a drawn attention may cost: by type, bytes and operations below those of the largest listed case.
+_MOST = {"bf16": (5e8, 2.0e12), "f32": (2e8, 2e10)}
+_MOST_SCORES = 4.2e9  # padded score elements of the plain form
+
+
+def _draw_rotary(rng, d):
+    return rng.choice((d, d, 16 * rng.randint(1, d // 16)))
+
+
+def draw(rng):
+    f32 = rng.random() < 0.2
+    heads = dict(SMALL_F32, d=rng.choice((64, 128))) if f32 else rng.choice(_HEADS)
+    dtype = "f32" if f32 else "bf16"
+    kind = rng.random()
+    if kind < 0.3:
+        case = _rotate("", heads, dtype=dtype, rows=_log_int(rng, 1, 8192), pos_hi=_log_int(rng, 1, 131071),
+                       rotary=_draw_rotary(rng, heads["d"]), interleaved=rng.random() < 0.3, norm=rng.random() < 0.6,
+                       scaled=rng.random() < 0.3)
+        del case["name"]
+        return case
+    if kind < 0.6:
+        seqs = _log_int(rng, 1, 256)
+        new_hi = _log_int(rng, 1, max(1, 6000 // seqs))
+        ctx_hi = _log_int(rng, 1, 32768)
+        ready = rng.random() < 0.3
+        case = _append("", heads, dtype=dtype, block_size=rng.choice((16, 16, 32)), seqs=seqs, new_hi=new_hi,
+                       new_lo=rng.choice((1, new_hi, 1 + new_hi // 2)), ctx_hi=ctx_hi,
+                       ctx_lo=rng.choice((0, ctx_hi, 1 + ctx_hi // 2)), rotary=0 if ready else _draw_rotary(rng, heads["d"]),
+                       interleaved=rng.random() < 0.3, norm=not ready and rng.random() < 0.7, scaled=rng.random() < 0.3,
+                       copies=rng.random() < 0.3, lens=rng.randrange(1 << 20))
+        del case["name"]
+        return case
+    while True:
+        mode = rng.choice(("singles", "chunks", "both"))
+        ctx_hi = _log_int(rng, 1, 2048 if f32 else 32768)
+        chunk_hi = _log_int(rng, 2, 256 if f32 else 4096)
+        case = _attend("", heads, dtype=dtype, block_size=rng.choice((16, 16, 32)),
+                       chunks=0 if mode == "singles" else _log_int(rng, 1, 16),
+                       singles=0 if mode == "chunks" else _log_int(rng, 1, 128), chunk_hi=chunk_hi,
+                       chunk_lo=rng.choice((1, chunk_hi, 1 + chunk_hi // 2)), ctx_hi=ctx_hi,
+                       ctx_lo=rng.choice((0, ctx_hi, 1 + ctx_hi // 2)), fused=rng.random() < 0.4,
+                       q_gain=rng.choice((1.0, 3.0)), lens=rng.randrange(1 << 20))
+        del case["name"]
+        new, kv = _lengths(case)
+        w, most = work(case), _MOST[dtype]
+        scores = len(new) * max(new) * case["hq"] * max(kv)
+        cache = len(new) * max(kv) * case["hkv"] * case["d"]
+        if w["bytes"] <= most[0] and w["flops"] <= most[1] and scores <= _MOST_SCORES and cache <= 2e9:
+            return case
+
+
+# ---- what a case's lengths are ---------------------------------------------------------
+def _lengths(case):
+    """New tokens and context length with them of every sequence; an attention's single tokens are spread among the chunks."""
+    r = random.Random(case["lens"])
+    if case["kind"] == "append":
+        new = [r.randint(case["new_lo"], case["new_hi"]) for _ in range(case["seqs"])]
+    else:
+        new = [r.randint(case["chunk_lo"], case["chunk_hi"]) for _ in range(case["chunks"])] + [1] * case["singles"]
+        r.shuffle(new)
+    return new, [n + r.randint(case["ctx_lo"], case["ctx_hi"]) for n in new]
+
+
+def _blocks(n, bs):
+    return (n + bs - 1) // bs
+
+
+def work(case):
+    hq, hkv, d, e = case["hq"], case["hkv"], case["d"], _ELEM[case["dtype"]]
+    if case["kind"] == "rotate":
+        # every row in and out, its position; the frequencies and the norms' weights once
+        rows = case["rows"] * (hq + hkv)
+        return {"bytes": 2 * rows * d * e + 4 * case["rows"] + 4 * case["rotary"] + 2 * d * e * case["norm"],
+                "flops": rows * (3 * case["rotary"] + 4 * d * case["norm"])}
+    new, kv = _lengths(case)
+    bs = case["block_size"]
+    if case["kind"] == "append":
+        rows = sum(new)
+        ready = case["rotary"] == 0 and not case["norm"]
+        blocks = sum(_blocks(k, bs) - (k - n) // bs for n, k in zip(new, kv))
+        kept = sum((k - n) % bs for n, k in zip(new, kv)) if case["copies"] else 0
+        # queries in and out, keys and values in, their codes out, slots and positions; scales of the blocks in and out; copies
+        return {"bytes": (0 if ready else 2 * rows * hq * d * e) + 2 * rows * hkv * d * (e + 1) + 12 * rows +
+                4 * blocks * hkv + 4 * kept * hkv * d,
+                "flops": rows * ((hq + hkv) * (3 * case["rotary"] + 4 * d * case["norm"]) + 4 * hkv * d)}
+    # row r of n sees kv - n + 1 + r positions
+    pairs = sum(n * (k - n) + n * (n + 1) // 2 for n, k in zip(new, kv))
+    held = sum(_blocks(k, bs) for k in kv)
+    return {"bytes": sum(new) * hq * (2 * d * e + 4) + 2 * sum(kv) * hkv * d + 2 * held * hkv + 4 * held + 8 * len(new),
+            "flops": 4 * hq * d * pairs}
+
+
+# ---- inputs ----------------------------------------------------------------------------
+def _gen(seed, part):
+    return torch.Generator(device=DEVICE).manual_seed(seed * 16 + part)
+
+
+def _normal(shape, dtype, gen, gain=1.0):
+    return (torch.randn(shape, generator=gen, device=DEVICE, dtype=torch.float32) * gain).to(_TORCH[dtype])
+
+
+def _ints(x, dtype=torch.int32):
+    return torch.as_tensor(np.asarray(x), dtype=dtype).to(DEVICE)
+
+
+def _codes(shape, gen):
+    """8-bit codes of normal values, as a block's scale leaves them: the largest of a block near the codes' top."""
+    x = torch.randn(shape, generator=gen, device=DEVICE, dtype=torch.bfloat16)
+    return (x * 80).clamp_(-_TOP, _TOP).to(torch.float8_e4m3fn)
+
+
+def _cache(blocks, case, seed):
+    hkv, bs, d = case["hkv"], case["block_size"], case["d"]
+    scale = lambda part: torch.randint(119, 122, (blocks, hkv), generator=_gen(seed, part), device=DEVICE,  # noqa: E731
+                                       dtype=torch.uint8)
+    return dict(k_codes=_codes((blocks, hkv, bs, d), _gen(seed, 2)), v_codes=_codes((blocks, hkv, d, bs), _gen(seed, 3)),
+                k_scale=scale(4), v_scale=scale(5))
+
+
+def _frequencies(rotary, scaled):
+    """Radians per position of each pair, and what the rotated channels are multiplied by."""
+    i = np.arange(rotary // 2, dtype=np.float64)
+    freq = _BASE ** (-2 * i / max(rotary, 1))
+    if not scaled:
+        return freq, 1.0
+    pair = lambda turns: rotary * math.log(_TRAINED / (turns * 2 * math.pi)) / (2 * math.log(_BASE))  # noqa: E731
+    low, high = max(math.floor(pair(_FAST)), 0), min(math.ceil(pair(_SLOW)), rotary - 1)
+    ramp = np.clip((i - low) / max(high - low, 1e-3), 0, 1)  # 0: as trained, 1: stretched
+    return freq * (1 - ramp) + freq / _FACTOR * ramp, 0.1 * math.log(_FACTOR) + 1
+
+
+def _rows(case, n, seed):
+    """A fused projection's rows, and their queries, keys and values."""
+    hq, hkv, d = case["hq"], case["hkv"], case["d"]
+    rows = _normal((n, (hq + 2 * hkv) * d), case["dtype"], _gen(seed, 1), 1.5)
+    part = lambda a, h: rows[:, a * d:(a + h) * d].unflatten(1, (h, d))  # noqa: E731
+    return part(0, hq), part(hq, hkv), part(hq + hkv, hkv)
+
+
+def _model(case, seed):
+    """What a model keeps: frequencies, and the weights of the norms."""
+    freq, magnitude = _frequencies(case["rotary"], case["scaled"])
+    gen = _gen(seed, 6)
+    weight = lambda: (1 + 0.2 * torch.randn(case["d"], generator=gen, device=DEVICE)).to(_TORCH[case["dtype"]])  # noqa: E731
+    return dict(rotary=case["rotary"], interleaved=case["interleaved"], magnitude=magnitude,
+                inv_freq=torch.from_numpy(freq).to(DEVICE) if case["rotary"] else None,
+                weights=(weight(), weight()) if case["norm"] else None)
+
+
+def _prepare_rotate(case, seed):
+    n, hq, hkv, d = case["rows"], case["hq"], case["hkv"], case["d"]
+    q, k, _ = _rows(case, n, seed)
+    first = max(0, case["pos_hi"] - n + 1)
+    positions = torch.arange(first, first + n, dtype=torch.int32, device=DEVICE)
+    if n <= 256:  # a batch: positions of many sequences
+        positions = torch.randint(0, case["pos_hi"] + 1, (n,), generator=_gen(seed, 7), device=DEVICE, dtype=torch.int32)
+        positions[0] = case["pos_hi"]
+    out = lambda h: torch.zeros((n, h, d), dtype=_TORCH[case["dtype"]], device=DEVICE)  # noqa: E731
+    return dict(kind="rotate", heads=(hq, hkv, d, 16), dtype=case["dtype"], q=q, k=k, positions=positions, q_out=out(hq),
+                k_out=out(hkv), keep={}, **_model(case, seed))
+
+
+def _prepare_append(case, seed):
+    new, kv = _lengths(case)
+    bs, hq, hkv, d = case["block_size"], case["hq"], case["hkv"], case["d"]
+    rows = sum(new)
+    touched = [_blocks(k, bs) - (k - n) // bs for n, k in zip(new, kv)]
+    tails = [i for i, (n, k) in enumerate(zip(new, kv)) if (k - n) % bs]
+    blocks = sum(touched) + len(tails) + 8
+    order = np.random.default_rng(seed).permutation(blocks)
+    slots, positions, first_rows, copies, at, row = [], [], [], [], 0, 0
+    for n, k, t in zip(new, kv, touched):
+        pos = np.arange(k - n, k)
+        slots.append(order[at + pos // bs - (k - n) // bs] * bs + pos % bs)
+        positions.append(pos)
+        starts = np.flatnonzero((pos % bs == 0) | (pos == k - n))
+        first_rows.append(row + starts)
+        if (k - n) % bs:
+            copies.append((order[blocks - 8 - len(tails) + len(copies)], order[at], (k - n) % bs))
+        at += t
+        row += n
+    first_row = np.concatenate(first_rows)
+    run = np.zeros(rows, np.int64)
+    run[first_row] = 1
+    q, k_new, v_new = _rows(case, rows, seed)
+    ready = case["rotary"] == 0 and not case["norm"]
+    return dict(kind="append", heads=(hq, hkv, d, bs), dtype=case["dtype"], cache=_cache(blocks, case, seed),
+                slots=_ints(np.concatenate(slots), torch.int64), positions=_ints(np.concatenate(positions)),
+                q=None if ready else q, k=k_new.contiguous() if ready else k_new, v=v_new.contiguous() if ready else v_new,
+                q_out=None if ready else torch.zeros((rows, hq, d), dtype=_TORCH[case["dtype"]], device=DEVICE),
+                first_row=_ints(first_row, torch.int64), run=_ints(np.cumsum(run) - 1, torch.int64),
+                copies=_ints(copies) if case["copies"] and copies else None,
+                n_copies=_ints([len(copies)]) if case["copies"] and copies else None, keep={}, **_model(case, seed))
+
+
+def _prepare_attend(case, seed):
+    new, kv = _lengths(case)
+    hq, hkv, d, bs, dtype = case["hq"], case["hkv"], case["d"], case["block_size"], case["dtype"]
+    n, rows, held = len(new), sum(new), [_blocks(k, bs) for k in kv]
+    blocks, most = sum(held) + 8, max(held)
+    order = np.random.default_rng(seed).permutation(blocks)
+    table = np.zeros((n, most), np.int32)
+    at = 0
+    for s, h in enumerate(held):
+        table[s, :h] = order[at:at + h]
+        at += h
+    width = (hq + 2 * hkv) * d if case["fused"] else hq * d
+    q = _normal((rows, width), dtype, _gen(seed, 1), case["q_gain"])[:, :hq * d].unflatten(1, (hq, d))
+    return dict(kind="attend", heads=(hq, hkv, d, bs), dtype=dtype, scale=float(np.float32(1.0 / math.sqrt(d))), q=q,
+                cache=_cache(blocks, case, seed), table=_ints(table), row_off=_ints(np.cumsum([0] + new)), kv_len=_ints(kv),
+                most_new=max(new), most_kv=max(kv), out=torch.zeros((rows, hq, d), dtype=_TORCH[dtype], device=DEVICE),
+                lse=torch.zeros((rows, hq), dtype=torch.float32, device=DEVICE), keep={})
+
+
+def prepare(case, seed):
+    return {"rotate": _prepare_rotate, "append": _prepare_append, "attend": _prepare_attend}[case["kind"]](case, seed)
+
+
+# ---- one pass: the library's calls -------------------------------------------------------
+def _kept(s):
+    """What a program makes once: the shape, and the library's views of frequencies, weights and cache."""
+    from paper_2607_03333_amd import spork
+    keep = s["keep"]
+    if not keep:
+        keep["shape"] = spork.make_shape(*s["heads"], spork.SPORK_DTYPE_BF16 if s["dtype"] == "bf16" else
+                                         spork.SPORK_DTYPE_F32, s.get("scale", 1.0))
+        if "cache" in s:
+            keep["cache"] = spork.make_kv8(**s["cache"])
+        if s["kind"] == "attend":
+            need = spork.spork_chunk_workspace_bytes(keep["shape"], len(s["kv_len"]), len(s["q"]))
+            keep["workspace"] = torch.empty(max(need, 256), dtype=torch.uint8, device=DEVICE)
+        else:
+            layout = spork.SPORK_ROPE_INTERLEAVED if s["interleaved"] else spork.SPORK_ROPE_HALF
+            keep["rope"] = spork.make_rope(s["inv_freq"], layout, s["magnitude"]) if s["rotary"] else None
+            keep["norm"] = spork.make_qk_norm(*s["weights"], _EPS) if s["weights"] else None
+    return spork, keep
+
+
+def _run_own(s):
+    spork, keep = _kept(s)
+    if s["kind"] == "rotate":
+        spork.spork_qk_rope(keep["shape"], keep["rope"], keep["norm"], s["positions"], s["q"], s["k"], s["q_out"], s["k_out"])
+    elif s["kind"] == "append":
+        if s["copies"] is not None:
+            spork.spork_kv8_copy_batch(keep["shape"], keep["cache"], s["copies"], s["n_copies"])
+        spork.spork_kv8_write(keep["shape"], keep["cache"], keep["rope"], keep["norm"], s["slots"], s["positions"], s["q"],
+                              s["k"], s["v"], s["q_out"])
+    else:
+        spork.spork_kv8_attn(keep["shape"], s["q"], keep["cache"], s["table"], s["row_off"], s["kv_len"], s["out"], s["lse"],
+                             keep["workspace"])
+
+
+# ---- one pass: the same in plain torch ----------------------------------------------------
+def _turned(s, x, which, dtype):
+    """Rows x [n, heads, d], normed and rotated, in `dtype`."""
+    x = x.to(dtype)
+    if s["weights"]:
+        x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + _EPS) * s["weights"][which].to(dtype)
+    r = s["rotary"]
+    if not r:
+        return x
+    angle = s["positions"].double()[:, None] * s["inv_freq"]  # 64 bits: far positions
+    cos, sin = ((f(angle) * s["magnitude"]).to(dtype)[:, None] for f in (torch.cos, torch.sin))
+    turned, rest = x[..., :r], x[..., r:]
+    if s["interleaved"]:
+        a, b = turned[..., 0::2], turned[..., 1::2]
+        turned = torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2)
+    else:
+        a, b = turned[..., :r // 2], turned[..., r // 2:]
+        turned = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+    return torch.cat([turned, rest], -1)
+
+
+def _rounded(x):
+    """64-bit values within the codes' range as codes: to the nearest, ties to even (a detour over 32 bits would round twice)."""
+    step = torch.exp2(torch.frexp(x)[1].clamp(min=-5).double() - 4)
+    return (torch.round(x / step) * step).float().to(torch.float8_e4m3fn)
+
+
+def _exponent(top):
+    """Least exponent of a scale that brings `top` into the codes' range."""
+    m, e = torch.frexp(top)
+    return torch.where(top > 0, torch.where(m <= 0.875, e - 9, e - 8), _LEAST).clamp(_LEAST, _MOST_EXP)
+
+
+def _append_pool(s, codes, scale, x, channel_major):
+    """New rows x [n, hkv, d] into the blocks of a pool: a block's scale is the least that holds its new tokens, or the one
+    that the tokens in front of them have, and those are coded anew where it grows."""
+    bs, run = s["heads"][3], s["run"]
+    first = s["slots"][s["first_row"]]
+    block, kept = first // bs, first % bs
+    top = torch.zeros((len(block), x.shape[1]), dtype=torch.float64, device=DEVICE)
+    top.index_reduce_(0, run, x.abs().amax(-1).double(), "amax")
+    before = scale[block].int() - 127
+    now = _exponent(top)
+    now = torch.where(kept[:, None] > 0, torch.maximum(before, now), now)
+    held = codes[block]
+    if channel_major:
+        held = held.transpose(2, 3)
+    at = torch.arange(bs, device=DEVICE)
+    again = (held.float() * torch.exp2((before - now).float())[:, :, None, None]).to(torch.float8_e4m3fn)
+    older = (at < kept[:, None])[:, None, :, None]
+    merged = torch.where(older, again.view(torch.uint8), held.view(torch.uint8))
+    fresh = _rounded(x.double() * torch.exp2(-now.double())[run][:, :, None])
+    merged[run, :, s["slots"] % bs] = fresh.view(torch.uint8)
+    if channel_major:
+        merged = merged.transpose(2, 3)
+    codes.view(torch.uint8)[block] = merged.contiguous()
+    scale[block] = (now + 127).to(torch.uint8)
+
+
+def _append_plain(s):
+    c, bs = s["cache"], s["heads"][3]
+    if s["copies"] is not None:
+        src, dst, valid = s["copies"].long().unbind(1)
+        part = torch.arange(bs, device=DEVICE)[None] < valid[:, None]
+        k, v = c["k_codes"].view(torch.uint8), c["v_codes"].view(torch.uint8)
+        k[dst] = torch.where(part[:, None, :, None], k[src], k[dst])
+        v[dst] = torch.where(part[:, None, None, :], v[src], v[dst])
+        for scale in (c["k_scale"], c["v_scale"]):
+            scale[dst] = scale[src]
+    # keys in 64 bits: their codes, not only their values, have to be the nearest
+    _append_pool(s, c["k_codes"], c["k_scale"], _turned(s, s["k"], 1, torch.float64), False)
+    _append_pool(s, c["v_codes"], c["v_scale"], s["v"], True)
+    if s["q"] is not None:
+        s["q_out"].copy_(_turned(s, s["q"], 0, torch.float32))
+
+
+def _attend_plain(s):
+    """The padded batch: every sequence's context gathered from its blocks, all its rows against all of it."""
+    q, c, table, kv_len, off = s["q"], s["cache"], s["table"].long(), s["kv_len"].long(), s["row_off"].long()
+    rows, hq, d = q.shape
+    hkv, bs = s["heads"][1], s["heads"][3]
+    n, most_new, most_kv, g = len(kv_len), s["most_new"], s["most_kv"], hq // hkv
+    tokens = table.shape[1] * bs
+    values = lambda codes, scale: codes[table].float() * torch.exp2(scale[table].float() - 127)[..., None, None]  # noqa: E731
+    k = values(c["k_codes"], c["k_scale"]).permute(0, 2, 1, 3, 4).reshape(n, hkv, tokens, d)[:, :, :most_kv]
+    v = values(c["v_codes"], c["v_scale"]).permute(0, 2, 1, 4, 3).reshape(n, hkv, tokens, d)[:, :, :most_kv]
+    at = torch.arange(most_kv, device=DEVICE)
+    v = torch.where(at[None, None, :, None] < kv_len[:, None, None, None], v, 0.0)
+    j = torch.arange(most_new, device=DEVICE)
+    new = off[1:] - off[:-1]
+    pick = torch.clamp(off[:-1, None] + j, max=rows - 1)
+    qp = q[pick].float().reshape(n, most_new, hkv, g, d).permute(0, 2, 1, 3, 4).reshape(n, hkv, most_new * g, d)
+    scores = torch.matmul(qp, k.transpose(2, 3).contiguous()).mul_(s["scale"])
+    sees = at[None, None] <= (kv_len - new)[:, None, None] + j[None, :, None]  # [n, new, kv]
+    scores = scores.reshape(n, hkv, most_new, g, most_kv).masked_fill_(~sees[:, None, :, None], -math.inf)
+    top = scores.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    p = scores.sub_(top).exp_()
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.reshape(n, hkv, most_new * g, most_kv), v.contiguous()).reshape(n, hkv, most_new, g, d)
+    o = torch.where(total > 0, o / total, 0.0).permute(0, 2, 1, 3, 4).reshape(n, most_new, hq, d)
+    lse = (top + total.log())[..., 0].permute(0, 2, 1, 3).reshape(n, most_new, hq)
+    r = torch.arange(rows, device=DEVICE)
+    seq = torch.searchsorted(off[1:].contiguous(), r, right=True)
+    s["out"].copy_(o[seq, r - off[seq]])
+    s["lse"].copy_(lse[seq, r - off[seq]])
+
+
+def _run_plain(s):
+    if s["kind"] == "rotate":
+        s["q_out"].copy_(_turned(s, s["q"], 0, torch.float32))
+        s["k_out"].copy_(_turned(s, s["k"], 1, torch.float32))
+    elif s["kind"] == "append":
+        _append_plain(s)
+    else:
+        _attend_plain(s)
+
+
+def run(s):
+    if own:
+        _run_own(s)
+    else:
+        _run_plain(s)
+    if s["kind"] == "rotate":
+        return {"q": s["q_out"], "k": s["k_out"]}
+    if s["kind"] == "append":
+        return {"q": s["q_out"], **s["cache"]}
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+# ---- the same in 64 bits, from the definitions ----------------------------------------------
+def _exact_turned(x, weight, s):
+    """Norm, then the rotation as a product of complex numbers."""
+    x = x.double().clone()
+    if weight is not None:
+        x = x / (x.pow(2).sum(-1, keepdim=True) / x.shape[-1] + _EPS).sqrt() * weight.double()
+    r = s["rotary"]
+    if r:
+        at = [slice(0, r, 2), slice(1, r, 2)] if s["interleaved"] else [slice(0, r // 2), slice(r // 2, r)]
+        angle = torch.outer(s["positions"].double(), s["inv_freq"])
+        z = torch.complex(x[..., at[0]].contiguous(), x[..., at[1]].contiguous()) * torch.polar(
+            torch.full_like(angle, s["magnitude"]), angle)[:, None]
+        x[..., at[0]], x[..., at[1]] = z.real, z.imag
+    return x
+
+
+def _exact_append(case, seed):
+    """Block by block on the host, with all values that 8 bits hold in a list."""
+    s = _prepare_append(case, seed)
+    weights = s["weights"] or (None, None)
+    held = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()  # 0 .. 448
+    middle = (held[1:] + held[:-1]) / 2
+
+    def nearest(x):
+        a = np.minimum(np.abs(x), _TOP)
+        i = np.searchsorted(middle, a)
+        tie = (i < 126) & (a == middle[np.minimum(i, 125)])
+        return np.copysign(held[i + (tie & (i % 2 == 1))], x)  # a tie goes to the even code
+
+    bs = s["heads"][3]
+    out = {}
+    slots = s["slots"].cpu().numpy()
+    runs = np.split(np.arange(len(slots)), s["first_row"].cpu().numpy()[1:])
+    copies = [] if s["copies"] is None else s["copies"].cpu().tolist()
+    for name, rows in (("k", _exact_turned(s["k"], weights[1], s)), ("v", s["v"].double())):
+        codes = s["cache"][name + "_codes"].double().cpu().numpy()
+        codes = np.ascontiguousarray(codes.swapaxes(2, 3)) if name == "v" else codes  # tokens first
+        scale = s["cache"][name + "_scale"].cpu().numpy().astype(np.int64) - 127
+        x = rows.cpu().numpy()
+        for src, dst, valid in copies:
+            codes[dst, :, :valid], scale[dst] = codes[src, :, :valid], scale[src]
+        for run in runs:
+            b, kept = slots[run[0]] // bs, slots[run[0]] % bs
+            top = np.abs(x[run]).max((0, 2))
+            least = np.array([next(e for e in range(_LEAST, _MOST_EXP + 1) if t <= _TOP * 2.0 ** e) for t in top])
+            now = np.maximum(least, scale[b]) if kept else least
+            codes[b, :, :kept] = nearest(codes[b, :, :kept] * (2.0 ** (scale[b] - now))[:, None, None])
+            codes[b][:, slots[run] % bs] = nearest(x[run] * (2.0 ** -now.astype(np.float64))[None, :, None]).swapaxes(0, 1)
+            scale[b] = now
+        out[name + "_codes"] = torch.from_numpy(np.ascontiguousarray(codes.swapaxes(2, 3)) if name == "v" else codes)
+        out[name + "_scale"] = torch.from_numpy((scale + 127).astype(np.uint8))
+    out["q"] = None if s["q"] is None else _exact_turned(s["q"], weights[0], s)
+    return out
+
+
+def _exact_attend(case, seed):
+    """Sequence by sequence and head by head."""
+    s = _prepare_attend(case, seed)
+    new, kv = _lengths(case)
+    group, bs = case["hq"] // case["hkv"], case["block_size"]
+    out, lse = s["out"].double(), s["lse"].double()
+    c = s["cache"]
+    row = 0
+    for i, (m, length) in enumerate(zip(new, kv)):
+        ids = s["table"][i, :_blocks(length, bs)].long()
+        last = length - m + torch.arange(m, device=DEVICE)
+        hidden = torch.arange(length, device=DEVICE)[None] > last[:, None]
+        for h in range(case["hkv"]):
+            ks, vs = (torch.pow(2.0, c[n][ids, h].double() - 127)[:, None, None] for n in ("k_scale", "v_scale"))
+            keys = (c["k_codes"][ids, h].double() * ks).reshape(-1, case["d"])[:length]
+            values = (c["v_codes"][ids, h].double() * vs).transpose(1, 2).reshape(-1, case["d"])[:length]
+            for head in range(h * group, (h + 1) * group):
+                x = (s["q"][row:row + m, head].double() @ keys.t().contiguous()).mul_(s["scale"])
+                x.masked_fill_(hidden, -math.inf)
+                lse[row:row + m, head] = torch.logsumexp(x, 1)
+                out[row:row + m, head] = torch.softmax(x, 1) @ values
+        row += m
+    return {"out": out, "lse": lse}
+
+
+def exact(case, seed):
+    if case["kind"] == "append":
+        return _exact_append(case, seed)
+    if case["kind"] == "attend":
+        return _exact_attend(case, seed)
+    s = _prepare_rotate(case, seed)
+    weights = s["weights"] or (None, None)
+    return {"q": _exact_turned(s["q"], weights[0], s), "k": _exact_turned(s["k"], weights[1], s)}
