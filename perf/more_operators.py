@@ -3,9 +3,9 @@
 Three kinds of call: queries and keys rotated by their positions, with or without
 their norm (``spork_qk_rope``); the new tokens of a step on their way into a cache
 of 8-bit codes with a scale for each block and head, where keys and queries are
-normed and rotated on the way (``spork_kv8_write``, behind the copies of
-copy-on-write by ``spork_kv8_copy_batch``); and the attention of prompt chunks and
-single tokens that reads that cache (``spork_kv8_attn``).
+normed and rotated on the way (``spork_kvq_write``, behind the copies of
+copy-on-write by ``spork_kvq_copy_batch``); and the attention of prompt chunks and
+single tokens that reads that cache (``spork_kvq_attn``).
 
 ``own`` chooses between the library's calls and the same in plain torch.
 ``listed()`` are sizes that a server meets, ``draw(rng)`` spreads them over
@@ -332,7 +332,7 @@ def _kept(s):
         keep["shape"] = spork.make_shape(*s["heads"], spork.SPORK_DTYPE_BF16 if s["dtype"] == "bf16" else
                                          spork.SPORK_DTYPE_F32, s.get("scale", 1.0))
         if "cache" in s:
-            keep["cache"] = spork.make_kv8(**s["cache"])
+            keep["cache"] = spork.make_kvq(**s["cache"])
         if s["kind"] == "attend":
             need = spork.spork_chunk_workspace_bytes(keep["shape"], len(s["kv_len"]), len(s["q"]))
             keep["workspace"] = torch.empty(max(need, 256), dtype=torch.uint8, device=DEVICE)
@@ -349,11 +349,11 @@ def _run_own(s):
         spork.spork_qk_rope(keep["shape"], keep["rope"], keep["norm"], s["positions"], s["q"], s["k"], s["q_out"], s["k_out"])
     elif s["kind"] == "append":
         if s["copies"] is not None:
-            spork.spork_kv8_copy_batch(keep["shape"], keep["cache"], s["copies"], s["n_copies"])
-        spork.spork_kv8_write(keep["shape"], keep["cache"], keep["rope"], keep["norm"], s["slots"], s["positions"], s["q"],
+            spork.spork_kvq_copy_batch(keep["shape"], keep["cache"], s["copies"], s["n_copies"])
+        spork.spork_kvq_write(keep["shape"], keep["cache"], keep["rope"], keep["norm"], s["slots"], s["positions"], s["q"],
                               s["k"], s["v"], s["q_out"])
     else:
-        spork.spork_kv8_attn(keep["shape"], s["q"], keep["cache"], s["table"], s["row_off"], s["kv_len"], s["out"], s["lse"],
+        spork.spork_kvq_attn(keep["shape"], s["q"], keep["cache"], s["table"], s["row_off"], s["kv_len"], s["out"], s["lse"],
                              keep["workspace"])
 
 
