@@ -518,6 +518,135 @@ int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, 
                      void* out, float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ======================================================================== *
+ *  From a projection's rows to the cache: norms and rotary positions of
+ *  queries and keys, and a cache of 8-bit codes with the attention that reads
+ *  it. Every device call below can be captured in a HIP graph and replayed.
+ * ======================================================================== */
+
+/* ---- rotary positions ---- */
+#define SPORK_ROPE_HALF 0        /* channel i turns with channel i + rotary_dim / 2 */
+#define SPORK_ROPE_INTERLEAVED 1 /* channel 2i turns with channel 2i + 1 */
+
+/* The rotation of a head's first rotary_dim channels: pair i of channels
+ * (x, y) at a position becomes
+ *   magnitude * (x cos t - y sin t, y cos t + x sin t), t = position * inv_freq[i]
+ * with angles in 64 bits. The other channels stay. */
+typedef struct spork_rope {
+  int32_t rotary_dim;     /* a multiple of 16, 16 .. head_dim */
+  int32_t layout;         /* SPORK_ROPE_* */
+  double magnitude;       /* 1, unless a scaling asks for another */
+  const double* inv_freq; /* device [rotary_dim / 2] radians per position, 16-byte aligned */
+} spork_rope;
+
+/* Norms of queries and keys, each head by itself, in front of the rotation:
+ * x w / sqrt(mean(x^2) + eps). Weights (device [head_dim], the shape's dtype,
+ * 16-byte aligned); one whose rows a call doesn't take may be NULL. */
+typedef struct spork_qk_norm {
+  const void* q_weight;
+  const void* k_weight;
+  double eps; /* finite, >= 0 */
+} spork_qk_norm;
+
+/* How frequencies are scaled for contexts longer than the one trained on.
+ * With f_i = base^(-2i / rotary_dim), their wavelengths 2 pi / f_i, and the
+ * turns trained_len / wavelength that a pair makes over the trained context: */
+#define SPORK_ROPE_SCALE_LINEAR 1 /* f_i / factor */
+#define SPORK_ROPE_SCALE_BASE 2   /* base * factor^(rotary_dim / (rotary_dim - 2)) in place of base */
+#define SPORK_ROPE_SCALE_PARTS 3  /* f_i for pairs up to the one that makes `fast` turns, f_i / factor from
+                                     the one that makes `slow` on, linear in the pair's index between (the
+                                     two indices rounded outwards); magnitude 0.1 ln(factor) + 1 (1 for
+                                     factor <= 1). YaRN, arXiv 2309.00071 */
+#define SPORK_ROPE_SCALE_BANDS 4  /* f_i for pairs of more than `fast` turns, f_i / factor for those of fewer
+                                     than `slow`, linear in the turns between */
+typedef struct spork_rope_scaling {
+  int32_t kind;        /* SPORK_ROPE_SCALE_* */
+  int32_t trained_len; /* PARTS, BANDS: > 0 */
+  double factor;       /* > 0 */
+  double fast, slow;   /* PARTS, BANDS: fast > slow > 0 */
+} spork_rope_scaling;
+
+/* Frequencies into inv_freq (host, rotary_dim / 2 doubles) and the magnitude
+ * (host) of a spork_rope; the caller copies the frequencies to the device.
+ * rotary_dim > 0 and even (BASE: above 2), base > 1; scaling NULL: none. */
+int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_scaling* scaling,
+                           double* inv_freq, double* magnitude);
+
+/* Norm and rotation of the queries and keys of n_rows tokens, in one pass
+ * (head_dim 64 or 128).
+ * rope, norm: NULL leaves that step out, not both. positions (device int32
+ * [n_rows], as spork_tables_step makes them; NULL if rope is NULL, or else
+ * required): rows at a negative position are left as they are in the outputs.
+ * q (device, n_rows rows of [Hq][D] dtype, q_stride elements apart), k (rows of
+ * [Hkv][D], k_stride), q_out, k_out likewise; k and k_out, or q and q_out, may be
+ * NULL. Rows 16-byte aligned: the parts of a fused projection's rows will do.
+ * q_out may be q, and k_out k, at the same stride; else outputs must not overlap
+ * each other or the inputs (SPORK_E_INVAL). bf16 rows: computed in float32,
+ * rounded once. One launch. */
+int spork_qk_rope(const spork_shape* shape, const spork_rope* rope, const spork_qk_norm* norm,
+                  const int32_t* positions, int32_t n_rows, const void* q, int64_t q_stride,
+                  const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
+                  int64_t k_out_stride, hipStream_t stream);
+
+/* ---- the cache of 8-bit codes ---- */
+
+/* Pools in device memory, owned by the caller, blocks and tables as for the
+ * other pools. A value is its code (8-bit floating point with 4 exponent and 3
+ * mantissa bits, e4m3 of the OCP's FP8: largest 448, no infinities) times
+ * 2^(s - 127), s being the scale byte (e8m0) of its block and KV head; keys and
+ * values have a scale each. Codes 16-byte aligned. */
+typedef struct spork_kvq {
+  int32_t num_blocks;
+  uint8_t* k_codes; /* device [num_blocks][Hkv][block_size][D] */
+  uint8_t* v_codes; /* device [num_blocks][Hkv][D][block_size] */
+  uint8_t* k_scale; /* device [num_blocks][Hkv] */
+  uint8_t* v_scale; /* device [num_blocks][Hkv] */
+} spork_kvq;
+
+/* A step's keys and values into the cache, and with q its queries, from the
+ * rows of the projection (head_dim 64 or 128, block_size 16 or 32).
+ * slots (device int64 [n_rows]): each row's slot; rows outside the pool are not
+ * written, their queries neither, and are counted into *bad_slots (device int32,
+ * nullable, not cleared by the call). k, v (device, rows of [Hkv][D] dtype,
+ * k_stride and v_stride elements apart), q (rows of [Hq][D], nullable) and q_out;
+ * rows 16-byte aligned. rope and norm (each nullable; both NULL: keys come ready,
+ * and q must be NULL): what happens to queries and keys on the way. positions
+ * (device int32 [n_rows]): required with rope. q_out may be q at the same stride;
+ * else it must not overlap what is read.
+ * The step's tokens of a block are consecutive rows in consecutive slots, as
+ * spork_tables_step makes them; tokens of the block in front of them stay, the
+ * places behind them hold what they held. (Rows that put a block's tokens in
+ * another order, or a slot twice, leave that block's contents undefined.) A
+ * block's scale is the least 2^e, -100 <= e <= 120, that brings its new tokens'
+ * largest magnitude to 448 or less; with tokens in front of them, no less than
+ * the scale these have, and where it grows their codes are rounded to it.
+ * Values are divided by the scale and rounded to the nearest code, ties to even;
+ * infinities and NaN become NaN and don't count for the scale. Keys are normed
+ * and rotated in float64 and rounded to their codes once; queries are computed in
+ * float32. Scale bytes of blocks that hold tokens must be ones that this call
+ * wrote (27 .. 247; others are taken for the nearest of these). One launch. */
+int spork_kvq_write(const spork_shape* shape, const spork_kvq* cache, const spork_rope* rope,
+                    const spork_qk_norm* norm, const int64_t* slots, const int32_t* positions,
+                    int32_t n_rows, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                    int32_t* bad_slots, hipStream_t stream);
+
+/* spork_kv_copy_batch for the cache of 8-bit codes: the codes of slots
+ * 0..n_valid-1 of block src into block dst, and the scales of all heads. */
+int spork_kvq_copy_batch(const spork_shape* shape, const spork_kvq* cache, const int32_t* copies,
+                         const int32_t* n_copies, int32_t max_copies, hipStream_t stream);
+
+/* spork_chunk_attn over the cache of 8-bit codes: the same arguments, limits,
+ * masks and empty rows, q and out of the shape's dtype, and the same workspace
+ * (spork_chunk_workspace_bytes; calls that share it must not overlap). Codes
+ * become bf16 (bf16 queries) or float32 exactly, so the result is that of
+ * spork_chunk_attn over pools of these values. NaN codes of positions below
+ * kv_len may show in rows that don't attend to them. Two launches. */
+int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, const spork_kvq* cache,
+                   const int32_t* table, int32_t max_blocks, const int32_t* row_off,
+                   const int32_t* kv_len, int32_t n_seqs, int32_t n_rows, void* out, float* lse,
+                   void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ======================================================================== *
  *  Kernel timing (benchmarks).
  * ======================================================================== */
 #define SPORK_KERNEL_ATTN 0   /* cascade / private-range partial attention (+ the verify step's argmax) */

@@ -21,9 +21,9 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
 
-HOST_SOURCES = ["block_manager.cpp", "plan.cpp", "capi.cpp", "paged.cpp", "dispatch_rules.cpp"]
+HOST_SOURCES = ["block_manager.cpp", "plan.cpp", "capi.cpp", "paged.cpp", "rows.cpp", "dispatch_rules.cpp"]
 DEVICE_SOURCES = ["attention.hip", "vocab.hip", "kv.hip", "ngram.hip", "ceiling.hip", "noalloc.hip",
-                  "tables.hip", "chunk.hip"]
+                  "tables.hip", "chunk.hip", "rope.hip", "kvq.hip", "chunk_kvq.hip"]
 DEVICE_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
                 "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                 "-Wno-unused-command-line-argument"]

@@ -43,6 +43,9 @@ struct ChunkArgs {
   int32_t* continues;   // [kChunkSlices] 1: the slice holds a piece of a tile that began before it
   float* part_ml;       // [kChunkSlices][2][kChunkTileRows][2] running max (base 2) and sum
   float* part_o;        // [kChunkSlices][2][kChunkTileRows][D] unnormalised outputs
+  // of a cache of 8-bit codes: [num_blocks][hkv]
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
 };
 
 // KV heads that a tile of a sequence with few rows may take together: a power of
@@ -52,6 +55,8 @@ bool chunk_supported(int32_t dtype, int32_t head_dim, int32_t block_size);
 size_t chunk_workspace_bytes(int32_t head_dim);
 void chunk_workspace(ChunkArgs* a, void* workspace);
 hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t stream);
+// the same over a cache of 8-bit codes (chunk_kvq.hip)
+hipError_t launch_kvq_attn(const ChunkArgs& a, hipStream_t stream);
 hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream);
 
 }  // namespace spork

@@ -1,0 +1,138 @@
+// A head's norm and rotation, as the lanes that hold it compute them. Shared by
+// the kernels that rotate rows (rope.hip) and write them into the cache of 8-bit
+// codes (kvq.hip).
+//
+//   norm      x <- x w / sqrt(mean(x^2) + eps)
+//   rotation  of each pair (x, y) of channels: (x, y) <- m (x cos t - y sin t, y cos t + x sin t),
+//             t = position * inv_freq[pair]
+//
+// D / 16 lanes hold a head, 16 channels each: two runs of 8 (kRun), so that a lane
+// has both channels of each of its 8 pairs and nothing is exchanged. Lane c of a
+// head has the pairs 8c .. 8c + 7 where these turn: half layout, channels 8c .. and
+// rotary_dim / 2 + 8c ..; interleaved, channels 16c .. 16c + 15. Lanes past the
+// pairs hold channels 16c .. 16c + 15, which only the norm changes.
+#pragma once
+#include "device_common.h"
+#include "rows_kernels.h"
+
+namespace spork {
+namespace {
+
+constexpr int kRun = 8;
+
+// Where a lane's two runs begin in a head, and whether they turn.
+struct Runs {
+  int a, b;
+  bool turns;
+  __device__ __forceinline__ Runs(const TurnArgs& t, int c) {
+    turns = 16 * c < t.rotary_dim;
+    const bool half = turns && t.interleaved == 0;
+    a = half ? 8 * c : 16 * c;
+    b = half ? t.rotary_dim / 2 + 8 * c : 16 * c + 8;
+  }
+};
+
+// Eight channels as they lie in memory.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__bf16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const __bf16* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ float get(int i) const { return vec_f<__bf16>(w, i); }
+};
+template <>
+struct Raw<float> {
+  uint4 w[2];
+  __device__ __forceinline__ void load(const float* p) {
+    w[0] = reinterpret_cast<const uint4*>(p)[0];
+    w[1] = reinterpret_cast<const uint4*>(p)[1];
+  }
+  __device__ __forceinline__ float get(int i) const { return vec_f<float>(w[i >> 2], i & 3); }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+// Eight channels, rounded to the output type once (to nearest: by at most half of its last place).
+template <typename F>
+__device__ __forceinline__ void store_run(__bf16* p, const F* x) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = bf16_pair(static_cast<float>(x[2 * i]), static_cast<float>(x[2 * i + 1]));
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename F>
+__device__ __forceinline__ void store_run(float* p, const F* x) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<float4*>(p)[i] = make_float4(static_cast<float>(x[4 * i]), static_cast<float>(x[4 * i + 1]),
+                                                  static_cast<float>(x[4 * i + 2]), static_cast<float>(x[4 * i + 3]));
+}
+
+// The value of the lane that differs in bit BY (1, 2 or 4) of its number: DPP moves.
+template <int BY>
+__device__ __forceinline__ float lane_xor(float x) {
+  if constexpr (BY == 1) return dpp_mov<0xB1>(x);
+  if constexpr (BY == 2) return dpp_mov<0x4E>(x);
+  // (within four lanes all are equal by then: the mirror of eight does for a difference of 4)
+  return dpp_mov<0x141>(x);
+}
+template <int BY>
+__device__ __forceinline__ double lane_xor(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const float lo = lane_xor<BY>(__uint_as_float(static_cast<uint32_t>(u)));
+  const float hi = lane_xor<BY>(__uint_as_float(static_cast<uint32_t>(u >> 32)));
+  return __builtin_bit_cast(double, static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo));
+}
+
+__device__ __forceinline__ float inv_sqrt(float x) { return 1.0f / sqrtf(x); }
+__device__ __forceinline__ double inv_sqrt(double x) { return 1.0 / sqrt(x); }
+
+// The head's norm, in F: w holds the lane's weights.
+template <int D, typename F>
+__device__ __forceinline__ void norm_head(F (&x)[16], const F (&w)[16], F eps) {
+  F s = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += x[i] * x[i];
+  s += lane_xor<1>(s);
+  s += lane_xor<2>(s);
+  if constexpr (D == 128) s += lane_xor<4>(s);
+  const F r = inv_sqrt(s * (F(1) / D) + eps);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+}
+
+// The lane's eight pairs, by their cosines and sines (the magnitude is in them).
+template <typename F, typename F2>
+__device__ __forceinline__ void turn_pairs(F (&x)[16], const F2 (&cs)[8], bool interleaved) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const F a = interleaved ? x[2 * j] : x[j], b = interleaved ? x[2 * j + 1] : x[8 + j];
+    const F y = a * cs[j].x - b * cs[j].y, z = b * cs[j].x + a * cs[j].y;
+    if (interleaved) {
+      x[2 * j] = y;
+      x[2 * j + 1] = z;
+    } else {
+      x[j] = y;
+      x[8 + j] = z;
+    }
+  }
+}
+
+// Cosine and sine of a pair at a position, in 64 bits: at position 131,071 a
+// rounded 32-bit angle is off by up to 0.004. The whole turns are taken off
+// before the functions, whose argument then is small.
+__device__ __forceinline__ double2 pair_turn(const TurnArgs& t, int pair, int position) {
+  constexpr double kTurns = 0.15915494309189533577;  // 1 / (2 pi)
+  double u = position * t.inv_freq[pair] * kTurns;
+  u -= rint(u);
+  double s, c;
+  sincospi(2.0 * u, &s, &c);
+  const double m = t.magnitude;
+  return make_double2(c * m, s * m);
+}
+
+}  // namespace
+}  // namespace spork

@@ -26,6 +26,12 @@ SPORK_E_CAPACITY = -4
 SPORK_E_HIP = -5
 SPORK_DTYPE_F32 = 0
 SPORK_DTYPE_BF16 = 1
+SPORK_ROPE_HALF = 0
+SPORK_ROPE_INTERLEAVED = 1
+SPORK_ROPE_SCALE_LINEAR = 1
+SPORK_ROPE_SCALE_BASE = 2
+SPORK_ROPE_SCALE_PARTS = 3
+SPORK_ROPE_SCALE_BANDS = 4
 SPORK_KERNEL_ATTN = 0
 SPORK_KERNEL_MERGE = 1
 SPORK_KERNEL_ARGMAX = 2
@@ -71,6 +77,25 @@ class spork_tables(ctypes.Structure):
     _fields_ = [("num_blocks", _c_i32), ("block_size", _c_i32), ("n_seqs", _c_i32), ("max_blocks", _c_i32),
                 ("table", _p), ("held", _p), ("refcount", _p), ("free_queue", _p), ("queue", _p)]
 
+
+class spork_rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", _c_i32), ("layout", _c_i32), ("magnitude", ctypes.c_double), ("inv_freq", _p)]
+
+
+class spork_qk_norm(ctypes.Structure):
+    _fields_ = [("q_weight", _p), ("k_weight", _p), ("eps", ctypes.c_double)]
+
+
+class spork_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", _c_i32), ("trained_len", _c_i32), ("factor", ctypes.c_double), ("fast", ctypes.c_double),
+                ("slow", ctypes.c_double)]
+
+
+class spork_kvq(ctypes.Structure):
+    _fields_ = [("num_blocks", _c_i32), ("k_codes", _p), ("v_codes", _p), ("k_scale", _p), ("v_scale", _p)]
+
+
+_shape, _rope, _norm, _kvq = (ctypes.POINTER(x) for x in (spork_shape, spork_rope, spork_qk_norm, spork_kvq))
 
 # name -> (restype, argtypes); every name is declared in include/spork.h
 _SIGNATURES = {
@@ -122,6 +147,15 @@ _SIGNATURES = {
                                                    ctypes.POINTER(ctypes.c_size_t)]),
     "spork_chunk_attn": (ctypes.c_int, [ctypes.POINTER(spork_shape), _p, _c_i64, _p, _p, _c_i32, _p, _c_i32, _p, _p,
                                         _c_i32, _c_i32, _p, _p, _p, ctypes.c_size_t, _p]),
+    "spork_rope_frequencies": (ctypes.c_int, [_c_i32, ctypes.c_double, ctypes.POINTER(spork_rope_scaling), _p,
+                                              ctypes.POINTER(ctypes.c_double)]),
+    "spork_qk_rope": (ctypes.c_int, [_shape, _rope, _norm, _p, _c_i32, _p, _c_i64, _p, _c_i64, _p, _c_i64, _p, _c_i64,
+                                     _p]),
+    "spork_kvq_write": (ctypes.c_int, [_shape, _kvq, _rope, _norm, _p, _p, _c_i32, _p, _c_i64, _p, _c_i64, _p, _c_i64, _p,
+                                       _c_i64, _p, _p]),
+    "spork_kvq_copy_batch": (ctypes.c_int, [_shape, _kvq, _p, _p, _c_i32, _p]),
+    "spork_kvq_attn": (ctypes.c_int, [_shape, _p, _c_i64, _kvq, _p, _c_i32, _p, _p, _c_i32, _c_i32, _p, _p, _p,
+                                      ctypes.c_size_t, _p]),
     "spork_read_ceiling": (ctypes.c_int, [_p, _c_i64, _c_i32, _c_i32, _p, _p]),
     "spork_timing_enable": (ctypes.c_int, [_c_i32]),
     "spork_timing_read": (ctypes.c_int, [_p, _p]),
@@ -511,6 +545,137 @@ def spork_chunk_attn(shape, q, k_cache, v_cache, table, row_off, kv_len, out, ls
             _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace))
     _on_gpu(q, k_cache, v_cache, table, row_off, kv_len, out, lse, workspace)
     _check(lib().spork_chunk_attn(ctypes.byref(shape), *args, _stream(stream)))
+
+
+# ---- from a projection's rows to the cache ------------------------------------------
+def spork_rope_frequencies(rotary_dim, base, scaling=None):
+    """(float64 array of rotary_dim / 2 frequencies, magnitude); `scaling` is a spork_rope_scaling."""
+    freq = np.zeros(max(rotary_dim // 2, 1))
+    magnitude = ctypes.c_double()
+    _check(lib().spork_rope_frequencies(rotary_dim, float(base), None if scaling is None else ctypes.byref(scaling),
+                                        _ptr(freq), ctypes.byref(magnitude)))
+    return freq, magnitude.value
+
+
+def _is_f64(x):
+    import torch
+    return x.dtype == torch.float64
+
+
+def make_rope(inv_freq, layout=SPORK_ROPE_HALF, magnitude=1.0):
+    """A spork_rope over the float64 tensor inv_freq, two channels a frequency, which it keeps alive."""
+    if inv_freq.dim() != 1 or not _is_f64(inv_freq) or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous float64 tensor of one dimension")
+    r = spork_rope(2 * inv_freq.shape[0], layout, magnitude, inv_freq.data_ptr())
+    r.tensors = (inv_freq,)
+    return r
+
+
+def make_qk_norm(q_weight, k_weight, eps):
+    """A spork_qk_norm over weights of head_dim elements (either may be None), which it keeps alive."""
+    if any(w is not None and (w.dim() != 1 or not w.is_contiguous()) for w in (q_weight, k_weight)):
+        raise ValueError("the norms' weights must be contiguous tensors of one dimension")
+    n = spork_qk_norm(_ptr(q_weight), _ptr(k_weight), eps)
+    n.tensors = (q_weight, k_weight)
+    return n
+
+
+def make_kvq(k_codes, v_codes, k_scale, v_scale):
+    """A spork_kvq over tensors of one byte an element (float8_e4m3fn or uint8 codes, uint8 or float8_e8m0fnu scales),
+    which it keeps alive: k_codes [blocks, hkv, block_size, head_dim], v_codes [blocks, hkv, head_dim, block_size],
+    k_scale and v_scale [blocks, hkv]."""
+    import torch
+    codes, scales = (torch.float8_e4m3fn, torch.uint8), (torch.uint8, torch.float8_e8m0fnu)
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be [blocks, hkv, block_size, head_dim]")
+    blocks, hkv, bs, d = k_codes.shape
+    for name, x, shape, types in (("k_codes", k_codes, (blocks, hkv, bs, d), codes), ("v_codes", v_codes, (blocks, hkv, d, bs), codes),
+                                  ("k_scale", k_scale, (blocks, hkv), scales), ("v_scale", v_scale, (blocks, hkv), scales)):
+        if tuple(x.shape) != shape or x.dtype not in types or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor of {' or '.join(map(str, types))} of shape {list(shape)}, "
+                             f"not {x.dtype} {list(x.shape)}")
+    c = spork_kvq(blocks, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+    c.tensors = (k_codes, v_codes, k_scale, v_scale)
+    return c
+
+
+def _heads(name, x, n, heads, d, dtype):
+    """(device pointer, stride) of rows [n, heads, d] that may have any stride between them; None passes."""
+    if x is None:
+        return None, 0
+    if x.shape != (n, heads, d) or not _of_dtype(dtype, x):
+        raise ValueError(f"{name} must be [{n}, {heads}, {d}] of the shape's dtype, not {x.dtype} {list(x.shape)}")
+    if n == 0:
+        return x.data_ptr(), heads * d
+    stride = x.stride()
+    if stride[2] != 1 or (stride[1] != d and heads > 1):
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return x.data_ptr(), stride[0] if n > 1 else heads * d
+
+
+def _turn(shape, rope, norm):
+    """References to rope and norm for a call (None passes), and their tensors."""
+    tensors = ()
+    if rope is not None:
+        tensors = rope.tensors
+    if norm is not None:
+        for w in norm.tensors:
+            if w is not None and (w.shape[0] != shape.head_dim or not _of_dtype(shape.dtype, w)):
+                raise ValueError("the norms' weights must have head_dim elements of the shape's dtype")
+        tensors += norm.tensors
+    return None if rope is None else ctypes.byref(rope), None if norm is None else ctypes.byref(norm), tensors
+
+
+def spork_qk_rope(shape, rope, norm, positions, q, k, q_out, k_out, stream=None):
+    """q [rows, hq, head_dim] and k [rows, hkv, head_dim] (one of them may be None) may have any stride between their
+    rows, and so may the outputs; q_out may be q, k_out k."""
+    n, d, dtype = (k if q is None else q).shape[0], shape.head_dim, shape.dtype
+    rope_ref, norm_ref, tensors = _turn(shape, rope, norm)
+    args = (_want("positions", positions, 4, n), n, *_heads("q", q, n, shape.hq, d, dtype), *_heads("k", k, n, shape.hkv, d, dtype),
+            *_heads("q_out", q_out, n, shape.hq, d, dtype), *_heads("k_out", k_out, n, shape.hkv, d, dtype))
+    _on_gpu(q, k, q_out, k_out, positions, *tensors)
+    _check(lib().spork_qk_rope(ctypes.byref(shape), rope_ref, norm_ref, *args, _stream(stream)))
+
+
+def _check_kvq(shape, cache):
+    if cache.tensors[0].shape[1:] != (shape.hkv, shape.block_size, shape.head_dim):
+        raise ValueError("the cache must be of the shape's hkv, block_size and head_dim")
+
+
+def spork_kvq_write(shape, cache, rope, norm, slots, positions, q, k, v, q_out, bad_slots=None, stream=None):
+    """q and q_out [rows, hq, head_dim] (both may be None), k and v [rows, hkv, head_dim] may have any stride between
+    their rows; q_out may be q."""
+    n, d, dtype = slots.shape[0], shape.head_dim, shape.dtype
+    _check_kvq(shape, cache)
+    rope_ref, norm_ref, tensors = _turn(shape, rope, norm)
+    args = (_want("slots", slots, 8, n), _want("positions", positions, 4, n), n, *_heads("q", q, n, shape.hq, d, dtype),
+            *_heads("k", k, n, shape.hkv, d, dtype), *_heads("v", v, n, shape.hkv, d, dtype),
+            *_heads("q_out", q_out, n, shape.hq, d, dtype), _want("bad_slots", bad_slots, 4, 1))
+    _on_gpu(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
+    _check(lib().spork_kvq_write(ctypes.byref(shape), ctypes.byref(cache), rope_ref, norm_ref, *args, _stream(stream)))
+
+
+def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
+    most = copies.shape[0]
+    _check_kvq(shape, cache)
+    _on_gpu(*cache.tensors, copies, n_copies)
+    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), ctypes.byref(cache), _want("copies", copies, 4, most, 3),
+                                      _want("n_copies", n_copies, 4, 1), most, _stream(stream)))
+
+
+def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace, stream=None):
+    """q [rows, hq, head_dim] may have any stride between its rows; the workspace is spork_chunk_attn's."""
+    n_rows, (n_seqs, max_blocks) = q.shape[0], table.shape
+    _check_kvq(shape, cache)
+    args = (*_heads("q", q, n_rows, shape.hq, shape.head_dim, shape.dtype), ctypes.byref(cache),
+            _want("table", table, 4, n_seqs, max_blocks), max_blocks, _want("row_off", row_off, 4, n_seqs + 1),
+            _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows, _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace))
+    if out.shape != q.shape or not _of_dtype(shape.dtype, out):
+        raise ValueError("out must be [rows, hq, head_dim] of the shape's dtype")
+    if lse is not None and (lse.shape != q.shape[:2] or not _of_dtype(SPORK_DTYPE_F32, lse)):
+        raise ValueError("lse must be [rows, hq] float32")
+    _on_gpu(q, *cache.tensors, table, row_off, kv_len, out, lse, workspace)
+    _check(lib().spork_kvq_attn(ctypes.byref(shape), *args, _stream(stream)))
 
 
 # ---- measurement aid --------------------------------------------------------
