@@ -172,11 +172,11 @@ int spork_qk_rope(const spork_shape* shape, const spork_rope* rope, const spork_
     if (rc != SPORK_OK) return rc;
     if (n_rows < 0) return fail(SPORK_E_INVAL, "n_rows must be >= 0");
     if (rope == nullptr && norm == nullptr) return fail(SPORK_E_INVAL, "rope and norm are both NULL");
+    if (n_rows == 0) return SPORK_OK;
     const bool with_q = q != nullptr || q_out != nullptr, with_k = k != nullptr || k_out != nullptr;
     if (!with_q && !with_k) return fail(SPORK_E_INVAL, "q and k are both NULL");
     rc = check_turn(shape, rope, norm, with_q, with_k);
     if (rc != SPORK_OK) return rc;
-    if (n_rows == 0) return SPORK_OK;
     if (rope != nullptr && positions == nullptr) return fail(SPORK_E_INVAL, "positions is NULL");
     const int elem = elem_bytes(shape->dtype);
     const int64_t qw = static_cast<int64_t>(shape->hq) * shape->head_dim, kw = static_cast<int64_t>(shape->hkv) * shape->head_dim;
@@ -224,11 +224,11 @@ int spork_kvq_write(const spork_shape* shape, const spork_kvq* cache, const spor
     if (rc == SPORK_OK) rc = check_cache(cache);
     if (rc != SPORK_OK) return rc;
     if (n_rows < 0) return fail(SPORK_E_INVAL, "n_rows must be >= 0");
+    if (n_rows == 0) return SPORK_OK;
     const bool with_q = q != nullptr || q_out != nullptr;
     if (with_q && rope == nullptr && norm == nullptr) return fail(SPORK_E_INVAL, "q needs rope or norm: without them it is ready");
     rc = check_turn(shape, rope, norm, with_q, true);
     if (rc != SPORK_OK) return rc;
-    if (n_rows == 0) return SPORK_OK;
     if (slots == nullptr || (rope != nullptr && positions == nullptr)) return fail(SPORK_E_INVAL, "slots or positions is NULL");
     const int elem = elem_bytes(shape->dtype);
     const int64_t qw = static_cast<int64_t>(shape->hq) * shape->head_dim, kw = static_cast<int64_t>(shape->hkv) * shape->head_dim;

@@ -658,9 +658,9 @@ def spork_kvq_write(shape, cache, rope, norm, slots, positions, q, k, v, q_out, 
 def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
     most = copies.shape[0]
     _check_kvq(shape, cache)
+    args = (_want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1), most)
     _on_gpu(*cache.tensors, copies, n_copies)
-    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), ctypes.byref(cache), _want("copies", copies, 4, most, 3),
-                                      _want("n_copies", n_copies, 4, 1), most, _stream(stream)))
+    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), ctypes.byref(cache), *args, _stream(stream)))
 
 
 def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace, stream=None):
