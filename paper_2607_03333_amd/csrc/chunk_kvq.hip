@@ -22,7 +22,7 @@
 // one it computes), as many bytes as they have. The blocks' entries and scales come 64 at a
 // time, a window ahead, into registers: loads beside the stages' would be counted
 // with them at every wait.
-#include "chunk_tiles.h"
+#include "chunk_wide.h"
 
 namespace spork {
 namespace {
@@ -164,6 +164,167 @@ struct DeepStages {
   }
 };
 
+// The stages that a workgroup's waves share (chunk_wide.h): codes come into a ring of
+// three pairs of stages by direct loads, and each wave turns what it has loaded itself
+// into bf16 in the ring of stages, a pair of stages ahead of those that are
+// published. So every code is converted once, not by every wave that needs it.
+// Instruction i of wave w takes stage i of a pair, its chunks 64 w .. (64 channels:
+// the lower four waves the first stage, the others the second, chunks 64 (w % 4) ..),
+// the first half of them K. A chunk of K is two of the ring's: its first and last
+// eight channels go to chunks 4 (c / 2) + c % 2 and 2 further, the order in which
+// load_q has the queries.
+template <int D, int BS>
+struct CodeLoader {
+  using E = StageLayout<D, BS>;
+  static constexpr bool kCoded = true;
+  static constexpr int kRing = 6;         // stages of bf16
+  static constexpr int kPairs = 3;        // pairs of stages of codes
+  static constexpr int kStageLoads = 1;   // (of a stage's place in the period)
+  static constexpr int kPairLoads = D / 64;
+  static constexpr int kPerStage = 32 / BS, kWindow = 64 / kPerStage;  // entries of a stage, stages of a window
+  static constexpr int kPairChunks = 8 * D;
+  static constexpr int kWords = kRing * 8 * D + kPairs * kPairChunks;  // LDS, in 16-byte chunks
+  static constexpr int kSteps = 4;
+  const char* pool;
+  const uint8_t* scales;
+  Pages pages;
+  int first;  // the tile's first entry
+  int head, hkv;
+  int wave, lane;
+  int stage, half;  // D = 64: the stage of a pair that the wave loads; which block of a stage
+  uint32_t off, dst, other;  // of the lane: in a block of codes, in a stage of the ring; bit in which its second chunk there differs
+  uint4* raw;            // codes of the wave in pair 0
+  uint32_t ring;
+  int now, next;         // lane i: block of entry i of the window that is loaded; entry of the next one
+  uint32_t scale_now, scale_next;
+  // of a period
+  const char* from[kPairLoads];
+  float scale[kPairLoads];
+  uint32_t to[kPairLoads];  // stages of the ring
+  int conv_pair, load_pair;
+  u32x4 w;
+
+  __device__ __forceinline__ int blocks(int st) const { return pages.block(pages.entry(first + st * kPerStage + lane)); }
+  __device__ __forceinline__ uint32_t scales_of(int block) const { return scales[static_cast<size_t>(block) * hkv + head]; }
+  __device__ __forceinline__ void init(const ChunkArgs& a, const Pages& pg, int kv_head, int tb0, int wave_, int lane_, uint4* smem) {
+    wave = wave_;
+    lane = lane_;
+    pages = pg;
+    first = tb0 / BS;
+    head = kv_head;
+    hkv = a.hkv;
+    const int part = D == 128 ? wave : wave & 3;  // of a stage, 64 chunks each
+    constexpr int kParts = D / 32;                // of K, and of V
+    stage = D == 128 ? 0 : wave >> 2;
+    const bool values = part >= kParts;
+    const int chunk = (values ? part - kParts : part) * 64 + lane;
+    pool = static_cast<const char*>(values ? a.v_cache : a.k_cache);
+    scales = values ? a.v_scale : a.k_scale;
+    if (!values) {
+      constexpr int kPerToken = D / 16;
+      const int t = chunk / kPerToken, c = chunk % kPerToken;
+      half = uniform(BS == 16 ? t / 16 : 0);
+      off = (t % BS) * D + 16 * c;
+      dst = 16u * (t * E::kChunksPerToken + ((4 * (c >> 1) + (c & 1)) ^ E::kswz(t)));
+      other = 32;
+    } else {
+      const int d = BS == 16 ? chunk % D : chunk >> 1, h = BS == 16 ? chunk / D : chunk & 1;
+      half = uniform(BS == 16 ? h : 0);
+      off = d * BS + (BS == 16 ? 0 : 16 * h);
+      dst = 16u * (E::kHalf + (BS == 16 ? E::kHalf / 2 * h + 2 * d + E::vswz(d) : 4 * d + ((2 * h) ^ E::vswz(d))));
+      other = 16;
+    }
+    raw = smem + kRing * 8 * D + wave * 64;
+    ring = lds_addr(smem);
+    now = blocks(0);
+    next = blocks(kWindow);
+    scale_now = scales_of(now);
+    scale_next = 0;
+  }
+  // What a period needs to know: the pair of stages from st on is loaded, that from `conv` on is converted.
+  __device__ __forceinline__ void look_up(int st, int conv) {
+#pragma unroll
+    for (int i = 0; i < kPairLoads; ++i) {
+      const int s = D == 128 ? i : stage;
+      const int block = __builtin_amdgcn_readlane(now, (st + s) % kWindow * kPerStage + half);
+      from[i] = pool + (static_cast<size_t>(block) * hkv + head) * (BS * D);
+      scale[i] = scale_of(__builtin_amdgcn_readlane(scale_now, (conv + s) % kWindow * kPerStage + half));
+      to[i] = ring + static_cast<uint32_t>((conv + s) % kRing) * (8 * D * 16);
+    }
+    load_pair = st / 2 % kPairs;
+    conv_pair = conv / 2 % kPairs;
+  }
+  __device__ __forceinline__ void load(int i) const {
+    load_lds<kKeep>(from[i], BS * D, off, 0, raw + load_pair * kPairChunks + i * (4 * D));
+  }
+  __device__ __forceinline__ void read(int i) {
+    w = lds_read_b128(lds_addr(raw) + 16u * lane + static_cast<uint32_t>(conv_pair * kPairChunks + i * (4 * D)) * 16u, 0);
+  }
+  __device__ __forceinline__ void convert(int i, int b) const {
+    const bf16x8 x = widen(w[2 * b], w[2 * b + 1], scale[i]);
+    asm volatile("ds_write_b128 %0, %1" : : "v"(to[i] + (b == 0 ? dst : dst ^ other)), "v"(x) : "memory");
+  }
+  // The first pairs: 0 to 2 loaded; then 0 and 1 converted and 3 loaded.
+  __device__ __forceinline__ void begin() {
+    asm volatile("" : "+v"(scale_now));  // here: no wait for it is left for the stages
+#pragma unroll
+    for (int p = 0; p < kPairs; ++p) {
+      look_up(2 * p, 0);
+#pragma unroll
+      for (int i = 0; i < kPairLoads; ++i) load(i);
+    }
+  }
+  __device__ __forceinline__ void first_pairs() {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      look_up(6, 2 * p);
+      wait_vmcnt<2 * kPairLoads>();
+#pragma unroll
+      for (int i = 0; i < kPairLoads; ++i) {
+        read(i);
+        lds_wait(w, 0);
+        convert(i, 0);
+        convert(i, 1);
+      }
+      if (p == 0) {
+#pragma unroll
+        for (int i = 0; i < kPairLoads; ++i) load(i);
+      }
+    }
+  }
+  // Stage st begins a period: stages st + 4 and st + 5 are converted, st + 8 and st + 9 loaded.
+  __device__ __forceinline__ void publish(int st) {
+    if ((st + 8) % kWindow == 0) {
+      now = next;
+      asm volatile("" : "+v"(now));
+      next = blocks(st + 8 + kWindow);
+      scale_next = scales_of(now);
+    }
+    if ((st + 4) % kWindow == 0) {
+      scale_now = scale_next;
+      asm volatile("" : "+v"(scale_now));
+    }
+    look_up(st + 8, st + 4);
+  }
+  // Step t of the period's stage I.
+  template <int I>
+  __device__ __forceinline__ void step(int t) {
+    if (I >= kPairLoads) return;
+    if (t == 0) {
+      // (behind the awaited pair the next one is in flight)
+      if (I == 0) wait_vmcnt<kPairLoads>();
+      read(I);
+    } else if (t == 1) {
+      load(I);
+    } else if (t == 2) {
+      lds_wait(w, 0);
+      convert(I, 0);
+    } else {
+      convert(I, 1);
+    }
+  }
+};
+
 struct Scale2 {
   float k, v;
 };
@@ -175,8 +336,8 @@ template <int D, int BS>
 struct CodeEngine<__bf16, D, BS> {
   using Elem = __bf16;
   using Stages = DeepStages<CodeEngine>;
-  static constexpr bool kWide = false;
-  static constexpr int kNarrowTiles = kWaves;
+  static constexpr bool kWide = true;
+  static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
   static constexpr int kD = D, kBlock = BS;
   static constexpr int kTokens = 32;             // of a stage
   static constexpr int kUnits = 1;               // rows of a lane
@@ -184,7 +345,9 @@ struct CodeEngine<__bf16, D, BS> {
   static constexpr int kPerToken = D / 16;       // 16-byte chunks
   static constexpr int kHalf = kTokens * D / 16; // chunks of K, and of V
   static constexpr int kLoads = kHalf / 64;
-  static constexpr int kStage = 2 * kHalf, kDepth = 2, kSlot = kDepth * kStage;
+  static constexpr int kStage = 2 * kHalf, kDepth = 2;
+  static constexpr int kSlot = CodeLoader<D, BS>::kWords / kWaves;
+  static_assert(kSlot >= kDepth * kStage, "a wave's slot holds its stages");
   static constexpr int kSteps = D / 16, kCt = D / 32;
   bf16x8 q[kSteps];
   f32x16 o[kCt];
@@ -342,7 +505,10 @@ struct CodeEngine<__bf16, D, BS> {
             widen(vop[ct][2 * i], vop[ct][2 * i + 1], scale.v),
             __builtin_bit_cast(bf16x8, u32x4{pw[4 * i], pw[4 * i + 1], pw[4 * i + 2], pw[4 * i + 3]}), o[ct], 0, 0, 0);
   }
-  static __device__ __forceinline__ void wide_tile(const ChunkArgs&, const Tile&, const Pages&, uint4 (*)[kSlot], int, int, CodeEngine&) {}
+  static __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[kSlot], int lane,
+                                                   int wave, CodeEngine& e) {
+    spork::wide_tile<D, BS, CodeLoader<D, BS>>(a, w, pg, reinterpret_cast<uint4(*)[D * 8]>(smem), lane, wave, e);
+  }
 };
 
 template <int D, int BS>
