@@ -29,6 +29,15 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// A value in scalar registers of its own: kept in those of the kernel's arguments it
+// would be stored and fetched with all sixteen of them. (A pointer is generic then:
+// only for those of direct loads, which take it as an integer.)
+template <typename T>
+__device__ __forceinline__ T alone_in_scalars(T x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
 // The scale of a byte: its power of two.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -68,49 +77,64 @@ struct DeepStages {
   static constexpr int kWindow = 64 / kB;     // stages of a window
   static constexpr int L = E::kLoads, N = E::kDepth;
   static_assert(N >= 2 && N < kWindow && (2 * N - 1) * L < 64, "waits and windows");
-  int first, stride, count, head;
-  bool alone;
-  int now, next;          // lane i: entry i of the window that is loaded, and of the next one
-  uint32_t scales, scales_next;  // lane i: its K scale, and its V scale 16 bits up; of the window that is computed
+  int first, stride, count;
+  const char *k_head, *v_head;  // the head's part of block 0
+  uint32_t block_bytes;         // of all heads
+  const uint8_t *k_scales, *v_scales;
+  int hkv;
+  int now, next;  // lane i: block of entry i of the window that is loaded; entry i of the next one, as it is loaded
+  // lane i: K and V scale of entry i of the window that is computed (as one: V 16 bits
+  // up), and of the next one, as they are loaded: combined there, they would be waited for
+  uint32_t scales;
+  uint8_t k_first, v_first, k_next, v_next;
 
   __device__ __forceinline__ int entries(const Pages& pg, int window, int lane) const {
     const int k = min(window * kWindow + lane / kB, count - 1);
-    return pg.block(pg.entry((first + k * stride) / E::kBlock + lane % kB));
+    return pg.entry((first + k * stride) / E::kBlock + lane % kB);
   }
-  __device__ __forceinline__ uint32_t scales_of(const ChunkArgs& a, int block) const {
-    const size_t at = static_cast<size_t>(block) * a.hkv + head;
-    return a.k_scale[at] | static_cast<uint32_t>(a.v_scale[at]) << 16;
+  __device__ __forceinline__ void load_scales(uint8_t& k, uint8_t& v) const {
+    const size_t at = static_cast<size_t>(now) * hkv;
+    k = k_scales[at];
+    v = v_scales[at];
   }
-  template <bool kValues>
-  __device__ __forceinline__ void issue(const ChunkArgs& a, const Bases& at, int k, uint4* slot) const {
-    constexpr size_t kBytes = E::kBlock * E::kD;
+  static __device__ __forceinline__ uint32_t both(uint8_t k, uint8_t v) {
+    uint32_t x = k | static_cast<uint32_t>(v) << 16;
+    asm volatile("" : "+v"(x));  // here: no wait for it is left for the loop
+    return x;
+  }
+  template <int POLICY, bool kValues>
+  __device__ __forceinline__ void issue(const Bases& at, int k, uint4* slot) const {
     const char* from[kB];
 #pragma unroll
     for (int b = 0; b < kB; ++b) {
       const int block = __builtin_amdgcn_readlane(now, k % kWindow * kB + b);
-      from[b] = static_cast<const char*>(kValues ? a.v_cache : a.k_cache) + (static_cast<size_t>(block) * a.hkv + head) * kBytes;
+      from[b] = (kValues ? v_head : k_head) + static_cast<uint64_t>(static_cast<uint32_t>(block)) * block_bytes;
     }
     uint4* to = slot + k % N * E::kStage;
     const int off = (first + k * stride) % E::kBlock;  // (bf16: 0)
-    if (alone) E::template load<kStream, kValues>(from, at, off, to);
-    else E::template load<kKeep, kValues>(from, at, off, to);
+    E::template load<POLICY, kValues>(from, at, off, to);
   }
-  __device__ __forceinline__ void begin(const ChunkArgs& a, const Pages& pg, const Bases& at, int head_, int first_, int stride_, int seen,
-                                        bool alone_, int lane, uint4* slot) {
-    head = head_;
+  template <int POLICY>
+  __device__ __forceinline__ void begin(const ChunkArgs& a, const Pages& pg, const Bases& at, int head, int first_, int stride_, int seen,
+                                        int lane, uint4* slot) {
+    constexpr int kBytes = E::kBlock * E::kD;
+    hkv = a.hkv;
+    block_bytes = alone_in_scalars(static_cast<uint32_t>(hkv) * kBytes);
+    k_head = alone_in_scalars(static_cast<const char*>(a.k_cache) + static_cast<size_t>(head) * kBytes);
+    v_head = alone_in_scalars(static_cast<const char*>(a.v_cache) + static_cast<size_t>(head) * kBytes);
+    k_scales = a.k_scale + head;
+    v_scales = a.v_scale + head;
     first = first_;
     stride = stride_;
-    alone = alone_;
     count = (seen - first - 1) / stride + 1;
-    now = entries(pg, 0, lane);
+    now = pg.block(entries(pg, 0, lane));
     next = entries(pg, 1, lane);
-    scales = scales_of(a, now);
-    scales_next = 0;
+    load_scales(k_first, v_first);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       if (k < count) {
-        issue<false>(a, at, k, slot);
-        issue<true>(a, at, k, slot);
+        issue<POLICY, false>(at, k, slot);
+        issue<POLICY, true>(at, k, slot);
       }
     }
   }
@@ -130,35 +154,34 @@ struct DeepStages {
     }
     wait_vmcnt<2 * LEFT * L>();
   }
+  template <int POLICY>
   __device__ __forceinline__ void run(E& e, const ChunkArgs& a, const Pages& pg, const Bases& at, int tok_hi, int least, float c, int lane,
                                       bool second, uint4* places) {
     const uint32_t slot = lds_addr(places);
-    asm volatile("" : "+v"(scales));  // here: no wait for it is left for the loop
+    scales = both(k_first, v_first);
+    k_next = v_next = 0;
     for (int k = 0; k < count; ++k) {
       const int tb = first + k * stride, ahead = k + N, left = min(N - 1, count - 1 - k);
       const bool more = ahead < count;
       const uint32_t place = slot + k % N * (E::kStage * 16);
-      if (k > 0 && k % kWindow == 0) {
-        scales = scales_next;
-        asm volatile("" : "+v"(scales));
-      }
+      if (k > 0 && k % kWindow == 0) scales = both(k_next, v_next);
       const auto scale = E::scales_at(scales, k % kWindow * kB, lane);
       wait_k<N - 1>(left);
       e.read_k(place, at);  // (waited for: the half may be written again)
       if (more) {
         if (ahead % kWindow == 0) {
-          now = next;
+          now = pg.block(next);
           asm volatile("" : "+v"(now));
           next = entries(pg, ahead / kWindow + 1, lane);
-          scales_next = scales_of(a, now);
+          load_scales(k_next, v_next);
         }
-        issue<false>(a, at, ahead, places);
+        issue<POLICY, false>(at, ahead, places);
       }
       e.softmax(tb, tok_hi, tb + E::kTokens > tok_hi || tb + E::kTokens - 1 > least, c, lane, second, scale);
       if (more) wait_vmcnt<(2 * N - 1) * L>();
       else wait_v<N - 1>(left);
       e.read_v(place, at);
-      if (more) issue<true>(a, at, ahead, places);
+      if (more) issue<POLICY, true>(at, ahead, places);
       e.values(tb, tok_hi, lane, second, scale);
     }
   }
@@ -189,7 +212,8 @@ struct CodeLoader {
   const uint8_t* scales;
   Pages pages;
   int first;  // the tile's first entry
-  int head, hkv;
+  uint32_t block_bytes;  // of all heads
+  int hkv;
   int wave, lane;
   int stage, half;  // D = 64: the stage of a pair that the wave loads; which block of a stage
   uint32_t off, dst, other;  // of the lane: in a block of codes, in a stage of the ring; bit in which its second chunk there differs
@@ -204,22 +228,22 @@ struct CodeLoader {
   int conv_pair, load_pair;
   u32x4 w;
 
-  __device__ __forceinline__ int blocks(int st) const { return pages.block(pages.entry(first + st * kPerStage + lane)); }
-  __device__ __forceinline__ uint32_t scales_of(int block) const { return scales[static_cast<size_t>(block) * hkv + head]; }
+  __device__ __forceinline__ int entries(int st) const { return pages.entry(first + st * kPerStage + lane); }
+  __device__ __forceinline__ uint32_t scales_of(int block) const { return scales[static_cast<size_t>(block) * hkv]; }
   __device__ __forceinline__ void init(const ChunkArgs& a, const Pages& pg, int kv_head, int tb0, int wave_, int lane_, uint4* smem) {
     wave = wave_;
     lane = lane_;
     pages = pg;
     first = tb0 / BS;
-    head = kv_head;
     hkv = a.hkv;
+    block_bytes = alone_in_scalars(static_cast<uint32_t>(hkv) * (BS * D));
     const int part = D == 128 ? wave : wave & 3;  // of a stage, 64 chunks each
     constexpr int kParts = D / 32;                // of K, and of V
     stage = D == 128 ? 0 : wave >> 2;
     const bool values = part >= kParts;
     const int chunk = (values ? part - kParts : part) * 64 + lane;
-    pool = static_cast<const char*>(values ? a.v_cache : a.k_cache);
-    scales = values ? a.v_scale : a.k_scale;
+    pool = alone_in_scalars(static_cast<const char*>(values ? a.v_cache : a.k_cache) + static_cast<size_t>(kv_head) * (BS * D));
+    scales = (values ? a.v_scale : a.k_scale) + kv_head;
     if (!values) {
       constexpr int kPerToken = D / 16;
       const int t = chunk / kPerToken, c = chunk % kPerToken;
@@ -236,22 +260,28 @@ struct CodeLoader {
     }
     raw = smem + kRing * 8 * D + wave * 64;
     ring = lds_addr(smem);
-    now = blocks(0);
-    next = blocks(kWindow);
+    now = pages.block(entries(0));
+    next = entries(kWindow);
     scale_now = scales_of(now);
     scale_next = 0;
   }
-  // What a period needs to know: the pair of stages from st on is loaded, that from `conv` on is converted.
-  __device__ __forceinline__ void look_up(int st, int conv) {
+  // What a period needs to know: the pair of stages from st on is loaded, that from st on converted.
+  __device__ __forceinline__ void will_load(int st) {
 #pragma unroll
     for (int i = 0; i < kPairLoads; ++i) {
       const int s = D == 128 ? i : stage;
       const int block = __builtin_amdgcn_readlane(now, (st + s) % kWindow * kPerStage + half);
-      from[i] = pool + (static_cast<size_t>(block) * hkv + head) * (BS * D);
+      from[i] = pool + static_cast<uint64_t>(static_cast<uint32_t>(block)) * block_bytes;
+    }
+    load_pair = st / 2 % kPairs;
+  }
+  __device__ __forceinline__ void will_convert(int conv) {
+#pragma unroll
+    for (int i = 0; i < kPairLoads; ++i) {
+      const int s = D == 128 ? i : stage;
       scale[i] = scale_of(__builtin_amdgcn_readlane(scale_now, (conv + s) % kWindow * kPerStage + half));
       to[i] = ring + static_cast<uint32_t>((conv + s) % kRing) * (8 * D * 16);
     }
-    load_pair = st / 2 % kPairs;
     conv_pair = conv / 2 % kPairs;
   }
   __device__ __forceinline__ void load(int i) const {
@@ -266,18 +296,19 @@ struct CodeLoader {
   }
   // The first pairs: 0 to 2 loaded; then 0 and 1 converted and 3 loaded.
   __device__ __forceinline__ void begin() {
-    asm volatile("" : "+v"(scale_now));  // here: no wait for it is left for the stages
 #pragma unroll
     for (int p = 0; p < kPairs; ++p) {
-      look_up(2 * p, 0);
+      will_load(2 * p);
 #pragma unroll
       for (int i = 0; i < kPairLoads; ++i) load(i);
     }
   }
   __device__ __forceinline__ void first_pairs() {
+    asm volatile("" : "+v"(scale_now));  // here: no wait for it is left for the stages
+    will_load(6);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      look_up(6, 2 * p);
+      will_convert(2 * p);
       wait_vmcnt<2 * kPairLoads>();
 #pragma unroll
       for (int i = 0; i < kPairLoads; ++i) {
@@ -295,16 +326,17 @@ struct CodeLoader {
   // Stage st begins a period: stages st + 4 and st + 5 are converted, st + 8 and st + 9 loaded.
   __device__ __forceinline__ void publish(int st) {
     if ((st + 8) % kWindow == 0) {
-      now = next;
+      now = pages.block(next);
       asm volatile("" : "+v"(now));
-      next = blocks(st + 8 + kWindow);
+      next = entries(st + 8 + kWindow);
       scale_next = scales_of(now);
     }
     if ((st + 4) % kWindow == 0) {
       scale_now = scale_next;
       asm volatile("" : "+v"(scale_now));
     }
-    look_up(st + 8, st + 4);
+    will_load(st + 8);
+    will_convert(st + 4);
   }
   // Step t of the period's stage I.
   template <int I>

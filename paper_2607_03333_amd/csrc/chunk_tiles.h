@@ -414,8 +414,6 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
           look_up(ahead, first + stride);
           issue_k(first % BS);
           issue_v(first % BS);
-        } else {
-          stages.begin(a, pg, at, head, first, stride, seen, alone, lane, smem[wave]);
         }
       }
       int least = INT_MAX;
@@ -429,6 +427,12 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
         least = min(least, e.hz[u]);
         e.load_q(static_cast<const T*>(a.q) + static_cast<int64_t>(sq.row0 + row) * a.q_stride +
                      (head * group + pp % group) * D, lane, u);
+      }
+      if constexpr (E::kDepth > 1) {  // behind the queries: a wait for these is none for the stages
+        if (!wide && first < seen) {
+          if (alone) stages.template begin<kStream>(a, pg, at, head, first, stride, seen, lane, smem[wave]);
+          else stages.template begin<kKeep>(a, pg, at, head, first, stride, seen, lane, smem[wave]);
+        }
       }
       least = uniform(wave_min_int(least));
       const float c = a.scale_log2;
@@ -461,7 +465,10 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
             e.values(tb, tok_hi, lane, second);
           }
         } else {
-          if (first < seen) stages.run(e, a, pg, at, tok_hi, least, c, lane, second, smem[wave]);
+          if (first < seen) {
+            if (alone) stages.template run<kStream>(e, a, pg, at, tok_hi, least, c, lane, second, smem[wave]);
+            else stages.template run<kKeep>(e, a, pg, at, tok_hi, least, c, lane, second, smem[wave]);
+          }
         }
       }
       // ---- join the ways, and write the outputs or the piece for the merge ----

@@ -102,6 +102,8 @@ int check_kvq_shape(const spork_shape* shape) {
   if (rc != SPORK_OK) return rc;
   if (!spork::kvq_supported(shape->dtype, shape->head_dim, shape->block_size))
     return fail(SPORK_E_UNSUPPORTED, "the cache of 8-bit codes takes head_dim 64 or 128 and block_size 16 or 32");
+  if (static_cast<int64_t>(shape->hkv) * shape->head_dim * shape->block_size > INT_MAX)
+    return fail(SPORK_E_UNSUPPORTED, "hkv * head_dim * block_size must be below 2^31");
   return SPORK_OK;
 }
 
