@@ -113,6 +113,7 @@ struct Engine<__bf16, D, BS> : StageLayout<D, BS> {
   using Elem = __bf16;
   using Stages = int;
   static constexpr int kDepth = 1;
+  static constexpr bool kShifts = false;
   static constexpr bool kWide = true;
   static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
   static constexpr int kD = D, kBlock = BS;
@@ -296,6 +297,7 @@ struct Engine<float, D, BS> {
   using Elem = float;
   using Stages = int;
   static constexpr int kDepth = 1;
+  static constexpr bool kShifts = false;
   static constexpr bool kWide = false;
   static constexpr int kNarrowTiles = kWaves;
   static constexpr int kD = D, kBlock = BS;

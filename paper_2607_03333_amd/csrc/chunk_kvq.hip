@@ -368,6 +368,7 @@ template <int D, int BS>
 struct CodeEngine<__bf16, D, BS> {
   using Elem = __bf16;
   using Stages = DeepStages<CodeEngine>;
+  static constexpr bool kShifts = true;
   static constexpr bool kWide = true;
   static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
   static constexpr int kD = D, kBlock = BS;
@@ -547,6 +548,7 @@ template <int D, int BS>
 struct CodeEngine<float, D, BS> {
   using Elem = float;
   using Stages = DeepStages<CodeEngine>;
+  static constexpr bool kShifts = true;
   static constexpr bool kWide = false;
   static constexpr int kNarrowTiles = kWaves;
   static constexpr int kD = D, kBlock = BS;
@@ -564,7 +566,7 @@ struct CodeEngine<float, D, BS> {
   int hz[2];
 
   static __device__ __forceinline__ int token_cost(const ChunkArgs&, int row_tiles, int heads) {
-    return 2 * (D == 128 ? 2 : 1) * row_tiles * heads;
+    return (D == 128 ? 4 : 2) * heads << (row_tiles > 4 ? 3 : row_tiles > 2 ? 2 : row_tiles - 1);
   }
   static __device__ __forceinline__ int row(int lane, int u) { return 16 * u + (lane & 15); }
   static __device__ __forceinline__ int out_row(int lane, int i) { return 16 * (i / kDt) + (lane & 15); }

@@ -53,6 +53,8 @@ constexpr int kTileCost = 1000;
 // Least length of a slice: three fp32 prompts took 47.4 us at 2,048, 33.2 at 1,024,
 // 31.3 at 512, 27.8 at 320; one token over 1,000 positions 25.5, 17.8, 16.9, 16.5.
 constexpr int kMinSlice = 320;
+constexpr int kShortSlice = 256;  // with kShifts
+static_assert(kChunkSlices == 256, "slices of a long line by shifts");
 // Least cost of a piece: a cut closer to a tile's end moves to it. At 64, 256, 512 and
 // 1,024: eight fp32 tokens over up to 1,500 positions 16.9, 18.2, 19.1, 26.5 us, one
 // bf16 token over 1,000 17.0, 16.6, 17.5, 20.4; pieces of many rows, which cost more
@@ -127,15 +129,28 @@ __device__ __forceinline__ Seq seq_uniform(const ChunkArgs& a, int i) {
 
 // Where the line of length `total` is cut in front of slice i of n. (Fewer slices
 // than workgroups: the line is short.)
+// Engines with kShifts have costs that are powers of two and short lines in slices
+// of kShortSlice: no division of 64 bits is left on the way to a tile, which took 1.6
+// us from the slice's place to the tile's queries.
+template <typename E>
 __device__ __forceinline__ int64_t line_cut(int64_t total, int i, int n) {
+  if constexpr (E::kShifts)
+    return n == kChunkSlices ? (total >> 8) * i + ((total & 255) * i >> 8) : min(total, static_cast<int64_t>(i) * kShortSlice);
   return n == kChunkSlices ? total / kChunkSlices * i + total % kChunkSlices * i / kChunkSlices
                            : static_cast<int64_t>(static_cast<uint64_t>(total) * i / n);
 }
 
 // Token at which a cut at `y` of a tile's cost goes through its `end` tokens.
+template <typename E>
 __device__ __forceinline__ int cut(int64_t y, int64_t tile_cost, int cost, int end) {
   if (y <= 0) return 0;
   if (y >= tile_cost) return end;
+  if constexpr (E::kShifts) {
+    const int by = 31 - __builtin_clz(cost);
+    const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) >> by) & ~31;
+    const int least = max(32, kMinPiece >> by & ~31);
+    return t < least ? 0 : t > end - least ? end : t;
+  }
   const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) / cost) & ~31;
   const int least = max(32, kMinPiece / cost & ~31);
   return t < least ? 0 : t > end - least ? end : t;
@@ -277,13 +292,14 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     total += wave_sum[w];
   }
   total = uniform(total);
-  const int n = static_cast<int>(min(max(total / kMinSlice, static_cast<int64_t>(1)), static_cast<int64_t>(kChunkSlices)));
+  const int64_t wanted = E::kShifts ? (total + kShortSlice - 1) / kShortSlice : max(total / kMinSlice, static_cast<int64_t>(1));
+  const int n = static_cast<int>(min(wanted, static_cast<int64_t>(kChunkSlices)));
   *n_slices = n;
   *total_out = total;
   if (slice >= n || total == 0) return false;
-  const int64_t pos = line_cut(total, slice, n);
+  const int64_t pos = line_cut<E>(total, slice, n);
   *pos_out = pos;
-  *stop_out = line_cut(total, slice + 1, n);
+  *stop_out = line_cut<E>(total, slice + 1, n);
   int64_t at = upto - sum;
   if (pos >= at && pos < upto) {
     int i = i0;
@@ -366,7 +382,7 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
     const int tile = sq.at(nth), end = uniform(sq.end(tile));
     const int64_t tile_cost = uniform(sq.tile_cost(tile));
     const int64_t y1 = uniform(min(tile_cost, y0 + stop - pos));
-    const int tok_lo = uniform(cut(y0, tile_cost, sq.cost, end)), tok_hi = uniform(cut(y1, tile_cost, sq.cost, end));
+    const int tok_lo = uniform(cut<E>(y0, tile_cost, sq.cost, end)), tok_hi = uniform(cut<E>(y1, tile_cost, sq.cost, end));
     if (tok_hi > tok_lo || (end == 0 && y0 == 0)) {
       const int r0 = tile * sq.per;  // first query row of the tile, in the sequence
       const int n_packed = min(sq.per, sq.rows - r0) * group;
@@ -551,8 +567,8 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
           // the last slice that begins inside the tile
           const int64_t tile_end = pos - y0 + tile_cost;
           int last = min(static_cast<int>(static_cast<double>(tile_end) / static_cast<double>(total) * n_slices), n_slices - 1);
-          while (line_cut(total, last, n_slices) >= tile_end) --last;
-          while (last + 1 < n_slices && line_cut(total, last + 1, n_slices) < tile_end) ++last;
+          while (line_cut<E>(total, last, n_slices) >= tile_end) --last;
+          while (last + 1 < n_slices && line_cut<E>(total, last + 1, n_slices) < tile_end) ++last;
           a.splits[slice] = ChunkSplit{sq.row0 + r0, head0, n_packed, row_tiles, heads, last};
         }
       }
