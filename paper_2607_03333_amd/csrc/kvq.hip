@@ -8,10 +8,9 @@
 // where they need it; the codes of the tokens in front of them are then written
 // anew (again exact, but for those that fall below 2^-6 of the scale).
 //
-// A run is the step's consecutive tokens of a block. A workgroup takes the runs
-// that begin in its window of rows, one after the other; `parts` workgroups share
-// a window and deal its tasks among their waves: a KV head's keys, a KV head's
-// values, a token's query heads. Nothing is left to atomics.
+// A run is the step's consecutive tokens of a block. Three kinds of workgroups share
+// the launch: keys and values of four KV heads, a head a wave, of the runs that begin
+// in a window of rows; and query heads. Nothing is left to atomics.
 //   keys     16 bytes a lane and load, D / 16 lanes a token (turn.h). Norm and
 //            rotation are in 64 bits: 32 would put values that lie near the middle
 //            of two codes on the wrong side. What is kept of the result is 32 bits
@@ -76,90 +75,16 @@ __device__ __forceinline__ uint4 recode16(uint4 w, float by) {
   return make_uint4(recode4(w.x, by), recode4(w.y, by), recode4(w.z, by), recode4(w.w, by));
 }
 
-// A run: its first row and slot, the tokens of its block in front of it, and its length.
-struct Run {
-  int row, tokens, kept;
-  int64_t block;
-};
-
 // The lane's run of 8 codes.
 __device__ __forceinline__ uint2 codes8(const float* x, float by) {
   return make_uint2(codes4(x[0] * by, x[1] * by, x[2] * by, x[3] * by), codes4(x[4] * by, x[5] * by, x[6] * by, x[7] * by));
 }
 
-// A KV head's keys of a run.
-template <typename T, int D, int BS, bool kTurn>
-__device__ __forceinline__ void write_keys(const KvqWriteArgs& a, const Run& run, int head, const double2* table, int lane) {
-  constexpr int kLanes = D / 16, kTokens = 64 / kLanes, kPasses = (BS + kTokens - 1) / kTokens;
-  const int c = lane % kLanes;
-  const Runs at(a.turn, c);
-  const size_t bh = static_cast<size_t>(run.block) * a.hkv + head;
-  const int before = run.kept > 0 ? a.pools.k_scale[bh] - kBias : kLeastExp;
-  Raw<T> raw[kPasses][2];
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int t = p * kTokens + lane / kLanes;
-    if (t < run.tokens) {
-      const T* src = static_cast<const T*>(a.k) + (run.row + t) * a.k_stride + head * D;
-      raw[p][0].load(src + at.a);
-      raw[p][1].load(src + at.b);
-    }
-  }
-  float x[kPasses][16];
-  uint32_t top = 0;
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int t = p * kTokens + lane / kLanes;
-    if (t >= run.tokens) continue;
-    if constexpr (!kTurn) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[p][i] = raw[p][i / 8].get(i % 8);
-    } else {
-      double y[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = raw[p][i / 8].get(i % 8);
-      if (a.turn.k_weight != nullptr) {
-        Raw<T> wr[2];
-        wr[0].load(static_cast<const T*>(a.turn.k_weight) + at.a);
-        wr[1].load(static_cast<const T*>(a.turn.k_weight) + at.b);
-        double w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = wr[i / 8].get(i % 8);
-        norm_head<D>(y, w, a.turn.eps);
-      }
-      if (at.turns) {
-        double2 cs[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) cs[j] = table[t * (D / 2) + 8 * c + j];
-        if (a.turn.interleaved) turn_pairs(y, cs, true);
-        else turn_pairs(y, cs, false);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[p][i] = round_odd(y[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, top_bits(x[p][i]));
-  }
-  const int e = max(before, scale_exp(wave_max(top)));
-  uint8_t* codes = a.pools.k_codes + bh * (BS * D);
-  const float by = exp2_int(-e);
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int t = p * kTokens + lane / kLanes;
-    if (t >= run.tokens) continue;
-    uint8_t* dst = codes + (run.kept + t) * D;
-    *reinterpret_cast<uint2*>(dst + at.a) = codes8(x[p], by);
-    *reinterpret_cast<uint2*>(dst + at.b) = codes8(x[p] + 8, by);
-  }
-  if (run.kept > 0 && e > before) {
-    const float again = exp2_int(max(before - e, -126));
-    for (int i = lane; i < run.kept * (D / 16); i += 64) {
-      uint4* p = reinterpret_cast<uint4*>(codes) + i;
-      *p = recode16(*p, again);
-    }
-  }
-  if (lane == 0) a.pools.k_scale[bh] = static_cast<uint8_t>(e + kBias);
-}
+// A run: its first row, its block, the tokens of the block in front of it, and its length.
+struct Run {
+  int row, tokens, kept;
+  int64_t block;
+};
 
 // Bytes [lo, hi) of a dword that holds bytes first .. first + 3.
 __device__ __forceinline__ uint32_t byte_mask(int first, int lo, int hi) {
@@ -174,162 +99,315 @@ __device__ __forceinline__ uint32_t byte_mask(int first, int lo, int hi) {
 template <int D, int BS>
 constexpr int kTileWords = D * BS / 4 + (D / 8) * (BS / 4);
 
-// A KV head's values of a run.
-template <typename T, int D, int BS>
-__device__ __forceinline__ void write_values(const KvqWriteArgs& a, const Run& run, int head, uint32_t* tile, int lane) {
-  constexpr int kChunks = D / 8;                        // runs of 8 channels
-  constexpr int kQuads = 64 / kChunks;                  // groups of four tokens that a wave holds at once
-  constexpr int kPasses = (BS / 4 + kQuads - 1) / kQuads;
-  constexpr int W = BS / 4;
-  const int chunk = lane % kChunks;
-  const size_t bh = static_cast<size_t>(run.block) * a.hkv + head;
-  const int before = run.kept > 0 ? a.pools.v_scale[bh] - kBias : kLeastExp;
-  Raw<T> raw[kPasses][4];
-  bool there[kPasses][4];
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = 4 * (p * kQuads + lane / kChunks) + i - run.kept;
-      there[p][i] = t >= 0 && t < run.tokens;
-      if (there[p][i]) raw[p][i].load(static_cast<const T*>(a.v) + (run.row + t) * a.v_stride + head * D + 8 * chunk);
-    }
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = there[p][i] ? max(top, top_bits(raw[p][i].get(j))) : top;
-  const int e = max(before, scale_exp(wave_max(top)));
-  const float by = exp2_int(-e);
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int quad = p * kQuads + lane / kChunks;
-    if (quad >= W) continue;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = there[p][i] ? raw[p][i].get(j) * by : 0.0f;
-      const int d = 8 * chunk + j;
-      tile[d * W + chunk * W + quad] = codes4(x[0], x[1], x[2], x[3]);
-    }
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  uint4* dst = reinterpret_cast<uint4*>(a.pools.v_codes + bh * (BS * D));
-  const bool whole = run.tokens == BS;
-  const float again = exp2_int(max(before - e, -126));
-#pragma unroll
-  for (int i = 0; i < D * W / 4 / 64; ++i) {
-    const int at = i * 64 + lane, d = at / (W / 4), part = at % (W / 4);
-    uint4 w = *reinterpret_cast<const uint4*>(tile + d * W + d / 8 * W + 4 * part);
-    if (!whole) {
-      const uint4 old = dst[at];
-      uint32_t n[4] = {w.x, w.y, w.z, w.w}, o[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int first = 16 * part + 4 * k;
-        const uint32_t mine = byte_mask(first, run.kept, run.kept + run.tokens), front = byte_mask(first, 0, run.kept);
-        uint32_t rest = o[k];
-        if (e > before && front != 0) rest = (recode4(o[k], again) & front) | (o[k] & ~front);
-        n[k] = (n[k] & mine) | (rest & ~mine);
-      }
-      w = make_uint4(n[0], n[1], n[2], n[3]);
-    }
-    dst[at] = w;
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();  // the tile is read: the wave's next task may write it
-  if (lane == 0) a.pools.v_scale[bh] = static_cast<uint8_t>(e + kBias);
-}
+// What a wave makes of a head of a run, D / 16 lanes a token (keys) or four tokens of
+// eight channels a lane (values).
+template <typename T, int D, int BS, bool kTurn>
+struct Heads {
+  static constexpr int kLanes = D / 16, kRows = 64 / kLanes;  // lanes of a token, tokens that a wave holds in two runs
+  static constexpr int kKeyPasses = (BS + kRows - 1) / kRows;
+  static constexpr int kChunks = D / 8, kQuads = 64 / kChunks, W = BS / 4;
+  static constexpr int kValuePasses = (W + kQuads - 1) / kQuads;
+  static constexpr int kOld = D * W / 4 / 64;  // 16-byte pieces of a head's block of values, of a lane
 
-// A token's query heads.
-template <typename T, int D, bool kTurn>
-__device__ __forceinline__ void write_queries(const KvqWriteArgs& a, int row, const double2* table, int lane) {
+  static __device__ __forceinline__ int exponent(uint8_t byte) { return min(max(byte - kBias, kLeastExp), kMostExp); }
+
+  // The run's keys, as they are loaded, and the scale of the tokens in front of them.
+  struct Keys {
+    Raw<T> raw[kKeyPasses][2];
+    uint8_t before;
+    __device__ __forceinline__ void load(const KvqWriteArgs& a, const Run& run, int head, const Runs& at, int lane) {
+      const T* src = static_cast<const T*>(a.k) + run.row * a.k_stride + head * D;
+#pragma unroll
+      for (int p = 0; p < kKeyPasses; ++p) {
+        const int t = p * kRows + lane / kLanes;
+        if (t < run.tokens) {
+          raw[p][0].load(src + t * a.k_stride + at.a);
+          raw[p][1].load(src + t * a.k_stride + at.b);
+        }
+      }
+      before = a.pools.k_scale[run.block * a.hkv + head];
+    }
+  };
+
+  static __device__ __forceinline__ void write_keys(const KvqWriteArgs& a, const Run& run, int head, const Runs& at, const Keys& k,
+                                                    const Raw<T> (&weight)[2], const double2* table, int lane) {
+    const int c = lane % kLanes;
+    float x[kKeyPasses][16];
+    uint32_t top = 0;
+#pragma unroll
+    for (int p = 0; p < kKeyPasses; ++p) {
+      const int t = p * kRows + lane / kLanes;
+      if (t >= run.tokens) continue;
+      if constexpr (!kTurn) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[p][i] = k.raw[p][i / 8].get(i % 8);
+      } else {
+        // One pair at a time, from what was loaded to 32 bits: kept in 64, a run's would
+        // fill the registers.
+        __builtin_amdgcn_sched_barrier(0);
+        double r = 1.0;
+        if (a.turn.k_weight != nullptr) {
+          double s = 0.0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const double v = k.raw[p][i / 8].get(i % 8);
+            s += v * v;
+          }
+          r = norm_factor<D>(s, a.turn.eps);
+        }
+        const auto value = [&](int i) __attribute__((always_inline)) {
+          const double v = k.raw[p][i / 8].get(i % 8);
+          return a.turn.k_weight != nullptr ? v * (r * weight[i / 8].get(i % 8)) : v;
+        };
+        const auto pairs = [&](auto interleaved) __attribute__((always_inline)) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int lo = interleaved ? 2 * j : j, hi = interleaved ? 2 * j + 1 : 8 + j;
+            double u = value(lo), v = value(hi);
+            if (at.turns) {
+              const double2 cs = table[t * (D / 2) + 8 * c + j];
+              const double y = u * cs.x - v * cs.y;
+              v = v * cs.x + u * cs.y;
+              u = y;
+            }
+            x[p][lo] = round_odd(u);
+            x[p][hi] = round_odd(v);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        if (a.turn.interleaved) pairs(std::true_type{});
+        else pairs(std::false_type{});
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = max(top, top_bits(x[p][i]));
+    }
+    const int before = run.kept > 0 ? exponent(k.before) : kLeastExp;
+    const int e = max(before, scale_exp(wave_max(top)));
+    const int64_t bh = run.block * a.hkv + head;
+    uint8_t* codes = a.pools.k_codes + bh * (BS * D);
+    const float by = exp2_int(-e);
+#pragma unroll
+    for (int p = 0; p < kKeyPasses; ++p) {
+      const int t = p * kRows + lane / kLanes;
+      if (t >= run.tokens) continue;
+      uint8_t* dst = codes + (run.kept + t) * D;
+      *reinterpret_cast<uint2*>(dst + at.a) = codes8(x[p], by);
+      *reinterpret_cast<uint2*>(dst + at.b) = codes8(x[p] + 8, by);
+    }
+    if (run.kept > 0 && e > before) {
+      const float again = exp2_int(max(before - e, -126));
+      for (int i = lane; i < run.kept * (D / 16); i += 64) {
+        uint4* p = reinterpret_cast<uint4*>(codes) + i;
+        *p = recode16(*p, again);
+      }
+    }
+    if (lane == 0) a.pools.k_scale[bh] = static_cast<uint8_t>(e + kBias);
+  }
+
+  static __device__ __forceinline__ void write_values(const KvqWriteArgs& a, const Run& run, int head, uint32_t* tile, int lane) {
+    const int chunk = lane % kChunks;
+    const int64_t bh = run.block * a.hkv + head;
+    uint4* dst = reinterpret_cast<uint4*>(a.pools.v_codes + bh * (BS * D));
+    const T* src = static_cast<const T*>(a.v) + run.row * a.v_stride + head * D + 8 * chunk;
+    const auto there = [&](int p, int i) {
+      const int t = 4 * (p * kQuads + lane / kChunks) + i - run.kept;
+      return t >= 0 && t < run.tokens;
+    };
+    Raw<T> raw[kValuePasses][4];
+#pragma unroll
+    for (int p = 0; p < kValuePasses; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (there(p, i)) raw[p][i].load(src + (4 * (p * kQuads + lane / kChunks) + i - run.kept) * a.v_stride);
+    uint4 old[kOld];
+    if (run.tokens < BS) {
+#pragma unroll
+      for (int i = 0; i < kOld; ++i) old[i] = dst[i * 64 + lane];
+    }
+    const int before = run.kept > 0 ? exponent(a.pools.v_scale[bh]) : kLeastExp;
+    uint32_t top = 0;
+#pragma unroll
+    for (int p = 0; p < kValuePasses; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = there(p, i) ? max(top, top_bits(raw[p][i].get(j))) : top;
+    const int e = max(before, scale_exp(wave_max(top)));
+    const float by = exp2_int(-e);
+#pragma unroll
+    for (int p = 0; p < kValuePasses; ++p) {
+      const int quad = p * kQuads + lane / kChunks;
+      if (quad >= W) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = there(p, i) ? raw[p][i].get(j) * by : 0.0f;
+        tile[(8 * chunk + j) * W + chunk * W + quad] = codes4(x[0], x[1], x[2], x[3]);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const float again = exp2_int(max(before - e, -126));
+#pragma unroll
+    for (int i = 0; i < kOld; ++i) {
+      const int at = i * 64 + lane, d = at / (W / 4), part = at % (W / 4);
+      uint4 w = *reinterpret_cast<const uint4*>(tile + d * W + d / 8 * W + 4 * part);
+      if (run.tokens < BS) {
+        uint32_t n[4] = {w.x, w.y, w.z, w.w}, o[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int first = 16 * part + 4 * k;
+          const uint32_t mine = byte_mask(first, run.kept, run.kept + run.tokens), front = byte_mask(first, 0, run.kept);
+          uint32_t rest = o[k];
+          if (e > before && front != 0) rest = (recode4(o[k], again) & front) | (o[k] & ~front);
+          n[k] = (n[k] & mine) | (rest & ~mine);
+        }
+        w = make_uint4(n[0], n[1], n[2], n[3]);
+      }
+      dst[at] = w;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();  // the tile is read: the wave's next run may write it
+    if (lane == 0) a.pools.v_scale[bh] = static_cast<uint8_t>(e + kBias);
+  }
+};
+
+// Rows of a window, at most: with the row in front of it and the longest run that
+// begins in it they fit the lanes of a wave.
+constexpr int kMostWindow = 16;
+
+// The runs that begin in a window of rows, found by all lanes at once: lane i has the
+// slot of row row0 - 1 + i.
+template <int BS>
+struct Window {
+  int64_t slot;
+  uint64_t ends, leaders;
+  int row0, bad;
+  __device__ __forceinline__ Window(const KvqWriteArgs& a, int first_row, int lane) {
+    static_assert(1 + kMostWindow + BS <= 64, "a window's rows in a wave's lanes");
+    row0 = first_row;
+    const int mine = row0 - 1 + lane;
+    slot = mine >= 0 && mine < a.n_rows ? a.slots[mine] : -1;
+    const bool sound = slot >= 0 && slot < static_cast<int64_t>(a.pools.num_blocks) * BS;
+    const int64_t before = __shfl_up(slot, 1);  // (of all lanes: not behind a condition)
+    const bool begins = !sound || slot % BS == 0 || before != slot - 1;
+    const uint64_t rows = ((uint64_t{1} << min(a.window, a.n_rows - row0)) - 1) << 1, good = __ballot(sound);
+    ends = __ballot(begins);
+    leaders = ends & good & rows;
+    bad = static_cast<int>(__popcll(rows & ~good));
+  }
+  __device__ __forceinline__ Run next() {
+    const int l = __builtin_ctzll(leaders);
+    leaders &= leaders - 1;
+    const int64_t begin = __shfl(slot, l);
+    return Run{row0 - 1 + l, __builtin_ctzll(ends >> (l + 1)) + 1, static_cast<int>(begin % BS), begin / BS};  // (a run ends within BS rows)
+  }
+};
+
+// A wave's query heads of one token: as qk_rope_kernel's (rope.hip).
+constexpr int kQueryGroups = 2;
+
+template <typename T, int D>
+__device__ __forceinline__ void write_queries(const KvqWriteArgs& a, int64_t num_slots, int64_t unit, float2* table, int lane) {
   constexpr int kLanes = D / 16, kHeads = 64 / kLanes;
+  const int parts = (a.hq + kQueryGroups * kHeads - 1) / (kQueryGroups * kHeads);
+  if (unit >= static_cast<int64_t>(a.n_rows) * parts) return;
+  const int row = static_cast<int>(unit / parts), first = static_cast<int>(unit % parts) * (kQueryGroups * kHeads) + lane / kLanes;
+  const int64_t slot = a.slots[row];
+  const int position = a.turn.rotary_dim > 0 ? a.positions[row] : 0;
   const int c = lane % kLanes;
   const Runs at(a.turn, c);
-  float2 cs[8];
-  if (at.turns) {
+  const T* src = static_cast<const T*>(a.q) + row * a.q_stride;
+  Raw<T> raw[kQueryGroups][2], weight[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const double2 t = table[8 * c + j];
-      cs[j] = make_float2(static_cast<float>(t.x), static_cast<float>(t.y));
+  for (int u = 0; u < kQueryGroups; ++u) {
+    const int head = first + u * kHeads;
+    if (head < a.hq) {
+      raw[u][0].load(src + head * D + at.a);
+      raw[u][1].load(src + head * D + at.b);
     }
   }
-  float w[16];
-  if (kTurn && a.turn.q_weight != nullptr) {
-    Raw<T> wr[2];
-    wr[0].load(static_cast<const T*>(a.turn.q_weight) + at.a);
-    wr[1].load(static_cast<const T*>(a.turn.q_weight) + at.b);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = wr[i / 8].get(i % 8);
+  if (a.turn.q_weight != nullptr) {
+    weight[0].load(static_cast<const T*>(a.turn.q_weight) + at.a);
+    weight[1].load(static_cast<const T*>(a.turn.q_weight) + at.b);
   }
-  for (int head = lane / kLanes; head < a.hq; head += kHeads) {
-    const T* src = static_cast<const T*>(a.q) + row * a.q_stride + head * D;
-    Raw<T> raw[2];
-    raw[0].load(src + at.a);
-    raw[1].load(src + at.b);
+  if (slot < 0 || slot >= num_slots) return;
+  float2 cs[8];
+  if (a.turn.rotary_dim > 0) lane_turns(a.turn, position, table, lane, c, cs);
+  T* dst = static_cast<T*>(a.q_out) + row * a.q_out_stride;
+#pragma unroll
+  for (int u = 0; u < kQueryGroups; ++u) {
+    const int head = first + u * kHeads;
+    if (head >= a.hq) continue;  // (whole heads: the lanes that reduce together stay together)
     float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = raw[i / 8].get(i % 8);
-    if constexpr (kTurn) {
-      if (a.turn.q_weight != nullptr) norm_head<D>(x, w, static_cast<float>(a.turn.eps));
-      if (at.turns) {
-        if (a.turn.interleaved) turn_pairs(x, cs, true);
-        else turn_pairs(x, cs, false);
-      }
+    for (int i = 0; i < 16; ++i) x[i] = raw[u][i / 8].get(i % 8);
+    if (a.turn.q_weight != nullptr) {
+      float w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = weight[i / 8].get(i % 8);
+      norm_head<D>(x, w, static_cast<float>(a.turn.eps));
     }
-    T* dst = static_cast<T*>(a.q_out) + row * a.q_out_stride + head * D;
-    store_run(dst + at.a, x);
-    store_run(dst + at.b, x + 8);
+    if (at.turns) {
+      if (a.turn.interleaved) turn_pairs(x, cs, true);
+      else turn_pairs(x, cs, false);
+    }
+    store_run(dst + head * D + at.a, x);
+    store_run(dst + head * D + at.b, x + 8);
   }
 }
 
 template <typename T, int D, int BS, bool kTurn>
 __global__ void __launch_bounds__(64 * kWriteWaves) kvq_write_kernel(KvqWriteArgs a) {
-  __shared__ double2 table[kTurn ? BS * (D / 2) : 1];
-  __shared__ __align__(16) uint32_t tile[kWriteWaves][kTileWords<D, BS>];
+  using H = Heads<T, D, BS, kTurn>;
+  constexpr int kTableBytes = kTurn ? BS * (D / 2) * sizeof(double2) : 0, kTilesBytes = kWriteWaves * kTileWords<D, BS> * 4;
+  __shared__ __align__(16) char memory[kTableBytes > kTilesBytes ? kTableBytes : kTilesBytes];  // of keys, values or queries
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int part = blockIdx.x % static_cast<unsigned>(a.parts);
-  const int row0 = static_cast<int>(blockIdx.x / static_cast<unsigned>(a.parts)) * a.window;
-  const int64_t num_slots = static_cast<int64_t>(a.pools.num_blocks) * BS;
-  const int row1 = min(a.n_rows, row0 + a.window);
-  for (int row = row0; row < row1; ++row) {
-    const int64_t slot = a.slots[row];
-    if (slot < 0 || slot >= num_slots) {
-      if (part == 0 && tid == 0 && a.bad_slots != nullptr) atomicAdd(a.bad_slots, 1);
-      continue;
+  const int head_groups = (a.hkv + kWriteWaves - 1) / kWriteWaves, windows = (a.n_rows + a.window - 1) / a.window;
+  const int64_t groups = static_cast<int64_t>(windows) * head_groups;  // of keys, and of values
+  const int64_t group = blockIdx.x;
+  if (group >= 2 * groups) {
+    write_queries<T, D>(a, static_cast<int64_t>(a.pools.num_blocks) * BS, (group - 2 * groups) * kWriteWaves + wave,
+                        reinterpret_cast<float2*>(memory) + 64 * wave, lane);
+    return;
+  }
+  const bool values = group >= groups;
+  const int at_group = static_cast<int>(values ? group - groups : group);
+  const int row0 = at_group / head_groups * a.window, head = at_group % head_groups * kWriteWaves + wave;
+  Window<BS> window(a, row0, lane);
+  if (values) {
+    uint32_t* tile = reinterpret_cast<uint32_t*>(memory) + wave * kTileWords<D, BS>;
+    if (head >= a.hkv) return;
+    while (window.leaders != 0) H::write_values(a, window.next(), head, tile, lane);
+    return;
+  }
+  if (head == 0 && lane == 0 && a.bad_slots != nullptr && window.bad > 0) atomicAdd(a.bad_slots, window.bad);
+  const Runs at(a.turn, lane % H::kLanes);
+  Raw<T> weight[2];
+  if constexpr (kTurn) {
+    if (a.turn.k_weight != nullptr) {
+      weight[0].load(static_cast<const T*>(a.turn.k_weight) + at.a);
+      weight[1].load(static_cast<const T*>(a.turn.k_weight) + at.b);
     }
-    Run run;
-    run.row = row;
-    run.block = slot / BS;
-    run.kept = static_cast<int>(slot % BS);
-    if (run.kept > 0 && row > 0 && a.slots[row - 1] == slot - 1) continue;  // inside a run
-    const int most = min(BS - run.kept, a.n_rows - row);
-    const bool goes_on = lane < most && a.slots[row + lane] == slot + lane;
-    const uint64_t ends = ~__ballot(goes_on);
-    run.tokens = __builtin_ctzll(ends);  // (most <= BS < 64: a bit is set)
+  }
+  double2* table = reinterpret_cast<double2*>(memory);
+  while (window.leaders != 0) {
+    const Run run = window.next();
+    typename H::Keys keys;
+    if (head < a.hkv) keys.load(a, run, head, at, lane);
     if constexpr (kTurn) {
       const int half = a.turn.rotary_dim / 2;
       if (half > 0) {
         __syncthreads();  // the last run's are read
         for (int i = tid; i < run.tokens * half; i += 64 * kWriteWaves) {
           const int t = i / half, pair = i - t * half;
-          table[t * (D / 2) + pair] = pair_turn(a.turn, pair, a.positions[row + t]);
+          table[t * (D / 2) + pair] = pair_turn(a.turn, pair, a.positions[run.row + t]);
         }
         __syncthreads();
       }
     }
-    const int tasks = 2 * a.hkv + (a.q != nullptr ? run.tokens : 0);
-    for (int task = part * kWriteWaves + wave; task < tasks; task += a.parts * kWriteWaves) {
-      if (task < a.hkv) write_keys<T, D, BS, kTurn>(a, run, task, table, lane);
-      else if (task < 2 * a.hkv) write_values<T, D, BS>(a, run, task - a.hkv, tile[wave], lane);
-      else write_queries<T, D, kTurn>(a, row + task - 2 * a.hkv, table + (kTurn ? (task - 2 * a.hkv) * (D / 2) : 0), lane);
-    }
+    if (head < a.hkv) H::write_keys(a, run, head, at, keys, weight, table, lane);
   }
 }
 
@@ -337,8 +415,11 @@ template <typename T, int D, int BS>
 hipError_t launch_write(const KvqWriteArgs& a, hipStream_t stream) {
   const bool turn = a.turn.rotary_dim > 0 || a.turn.q_weight != nullptr || a.turn.k_weight != nullptr;
   const auto k = turn ? kvq_write_kernel<T, D, BS, true> : kvq_write_kernel<T, D, BS, false>;
+  constexpr int kTaskHeads = kQueryGroups * 64 / (D / 16);
   const int64_t windows = (static_cast<int64_t>(a.n_rows) + a.window - 1) / a.window;
-  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(windows * a.parts)), dim3(64 * kWriteWaves), 0, stream, a);
+  const int64_t queries = a.q == nullptr ? 0 : static_cast<int64_t>(a.n_rows) * ((a.hq + kTaskHeads - 1) / kTaskHeads);
+  const int64_t groups = 2 * windows * ((a.hkv + kWriteWaves - 1) / kWriteWaves) + (queries + kWriteWaves - 1) / kWriteWaves;
+  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(groups)), dim3(64 * kWriteWaves), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -384,8 +465,8 @@ bool kvq_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
 
 hipError_t launch_kvq_write(const KvqWriteArgs& given, hipStream_t stream) {
   KvqWriteArgs a = given;
-  a.window = a.n_rows <= 512 ? 1 : 8;
-  a.parts = 4;
+  a.window = 1;
+  while (a.window < kMostWindow && a.window * 512 < a.n_rows) a.window *= 2;
   if (a.dtype == 1) {
     if (a.head_dim == 128) return a.block_size == 16 ? launch_write<__bf16, 128, 16>(a, stream) : launch_write<__bf16, 128, 32>(a, stream);
     return a.block_size == 16 ? launch_write<__bf16, 64, 16>(a, stream) : launch_write<__bf16, 64, 32>(a, stream);

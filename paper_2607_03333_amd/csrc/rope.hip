@@ -37,16 +37,7 @@ __global__ void __launch_bounds__(64 * kRopeWaves) qk_rope_kernel(RopeArgs a, in
     }
   }
   float2 cs[8];
-  if (a.turn.rotary_dim > 0) {
-    if (2 * lane < a.turn.rotary_dim) {
-      const double2 t = pair_turn(a.turn, lane, position);
-      table[wave][lane] = make_float2(static_cast<float>(t.x), static_cast<float>(t.y));
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) cs[j] = table[wave][(8 * c + j) & 63];
-  }
+  if (a.turn.rotary_dim > 0) lane_turns(a.turn, position, table[wave], lane, c, cs);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     if (head[u] >= heads) continue;  // (whole heads: the lanes that reduce together stay together)

@@ -52,8 +52,7 @@ struct KvqWriteArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   int32_t* bad_slots;  // nullable
   int32_t n_rows, hq, hkv, head_dim, block_size, dtype;
-  // the launch's split (launch_kvq_write)
-  int32_t window, parts;
+  int32_t window;  // rows whose runs a workgroup takes (launch_kvq_write)
 };
 
 // Head and block sizes that there are kernels for.

@@ -90,16 +90,22 @@ __device__ __forceinline__ double lane_xor(double x) {
 __device__ __forceinline__ float inv_sqrt(float x) { return 1.0f / sqrtf(x); }
 __device__ __forceinline__ double inv_sqrt(double x) { return 1.0 / sqrt(x); }
 
+// 1 / sqrt(mean(x^2) + eps) of a head, from the lane's sum of squares.
+template <int D, typename F>
+__device__ __forceinline__ F norm_factor(F s, F eps) {
+  s += lane_xor<1>(s);
+  s += lane_xor<2>(s);
+  if constexpr (D == 128) s += lane_xor<4>(s);
+  return inv_sqrt(s * (F(1) / D) + eps);
+}
+
 // The head's norm, in F: w holds the lane's weights.
 template <int D, typename F>
 __device__ __forceinline__ void norm_head(F (&x)[16], const F (&w)[16], F eps) {
   F s = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s += x[i] * x[i];
-  s += lane_xor<1>(s);
-  s += lane_xor<2>(s);
-  if constexpr (D == 128) s += lane_xor<4>(s);
-  const F r = inv_sqrt(s * (F(1) / D) + eps);
+  const F r = norm_factor<D>(s, eps);
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
 }
@@ -132,6 +138,20 @@ __device__ __forceinline__ double2 pair_turn(const TurnArgs& t, int pair, int po
   sincospi(2.0 * u, &s, &c);
   const double m = t.magnitude;
   return make_double2(c * m, s * m);
+}
+
+// The turns of a lane's eight pairs at a position, in 32 bits: each lane of the wave
+// computes one pair, and they are exchanged through the wave's table in LDS (64
+// entries). Lanes whose channels don't turn get anything.
+__device__ __forceinline__ void lane_turns(const TurnArgs& t, int position, float2* table, int lane, int c, float2 (&cs)[8]) {
+  if (2 * lane < t.rotary_dim) {
+    const double2 x = pair_turn(t, lane, position);
+    table[lane] = make_float2(static_cast<float>(x.x), static_cast<float>(x.y));
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cs[j] = table[(8 * c + j) & 63];
 }
 
 }  // namespace

@@ -440,6 +440,7 @@ def _want(name, x, size, *shape):
 
 
 _element_types = {}
+_torch = None
 
 
 def _of_dtype(dtype, *tensors):
@@ -568,6 +569,7 @@ def make_rope(inv_freq, layout=SPORK_ROPE_HALF, magnitude=1.0):
         raise ValueError("inv_freq must be a contiguous float64 tensor of one dimension")
     r = spork_rope(2 * inv_freq.shape[0], layout, magnitude, inv_freq.data_ptr())
     r.tensors = (inv_freq,)
+    r.ref = ctypes.byref(r)
     return r
 
 
@@ -576,7 +578,8 @@ def make_qk_norm(q_weight, k_weight, eps):
     if any(w is not None and (w.dim() != 1 or not w.is_contiguous()) for w in (q_weight, k_weight)):
         raise ValueError("the norms' weights must be contiguous tensors of one dimension")
     n = spork_qk_norm(_ptr(q_weight), _ptr(k_weight), eps)
-    n.tensors = (q_weight, k_weight)
+    n.tensors = tuple(w for w in (q_weight, k_weight) if w is not None)
+    n.ref = ctypes.byref(n)
     return n
 
 
@@ -596,86 +599,110 @@ def make_kvq(k_codes, v_codes, k_scale, v_scale):
                              f"not {x.dtype} {list(x.shape)}")
     c = spork_kvq(blocks, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
     c.tensors = (k_codes, v_codes, k_scale, v_scale)
+    c.blocks_of = (hkv, bs, d)
+    c.ref = ctypes.byref(c)
     return c
 
 
-def _heads(name, x, n, heads, d, dtype):
-    """(device pointer, stride) of rows [n, heads, d] that may have any stride between them; None passes."""
+def _types(dtype):
+    """The types that tensors of the library's dtype may have, () for one it doesn't know."""
+    if not _element_types:
+        _of_dtype(dtype)
+    return _element_types.get(dtype, ())
+
+
+def _heads(name, x, shape, types):
+    """(device pointer, stride) of rows [n, heads, head_dim] that may have any stride between them; None passes."""
     if x is None:
         return None, 0
-    if x.shape != (n, heads, d) or not _of_dtype(dtype, x):
-        raise ValueError(f"{name} must be [{n}, {heads}, {d}] of the shape's dtype, not {x.dtype} {list(x.shape)}")
-    if n == 0:
-        return x.data_ptr(), heads * d
+    if x.shape != shape or x.dtype not in types:
+        raise ValueError(f"{name} must be {list(shape)} of the shape's dtype, not {x.dtype} {list(x.shape)}")
+    n, heads, d = shape
     stride = x.stride()
-    if stride[2] != 1 or (stride[1] != d and heads > 1):
+    if n > 0 and (stride[2] != 1 or (stride[1] != d and heads > 1)):
         raise ValueError(f"the rows of {name} must be contiguous")
     return x.data_ptr(), stride[0] if n > 1 else heads * d
 
 
-def _turn(shape, rope, norm):
+def _here(first, *tensors):
+    """_on_gpu for tensors alone (None passes, but for the first), without a branch for each kind."""
+    global _torch
+    here = first.get_device()
+    if here < 0:
+        _on_gpu(first)
+    if _torch is None:
+        import torch
+        _torch = torch
+    if here != _torch.cuda.current_device():
+        _on_gpu(first)
+    for x in tensors:
+        if x is not None and x.get_device() != here:
+            _on_gpu(x)
+
+
+def _turn(shape, rope, norm, types):
     """References to rope and norm for a call (None passes), and their tensors."""
-    tensors = ()
-    if rope is not None:
-        tensors = rope.tensors
-    if norm is not None:
-        for w in norm.tensors:
-            if w is not None and (w.shape[0] != shape.head_dim or not _of_dtype(shape.dtype, w)):
-                raise ValueError("the norms' weights must have head_dim elements of the shape's dtype")
-        tensors += norm.tensors
-    return None if rope is None else ctypes.byref(rope), None if norm is None else ctypes.byref(norm), tensors
+    if norm is None:
+        return (None, None, ()) if rope is None else (rope.ref, None, rope.tensors)
+    for w in norm.tensors:
+        if w.shape[0] != shape.head_dim or w.dtype not in types:
+            raise ValueError("the norms' weights must have head_dim elements of the shape's dtype")
+    return (None, norm.ref, norm.tensors) if rope is None else (rope.ref, norm.ref, rope.tensors + norm.tensors)
 
 
 def spork_qk_rope(shape, rope, norm, positions, q, k, q_out, k_out, stream=None):
     """q [rows, hq, head_dim] and k [rows, hkv, head_dim] (one of them may be None) may have any stride between their
     rows, and so may the outputs; q_out may be q, k_out k."""
-    n, d, dtype = (k if q is None else q).shape[0], shape.head_dim, shape.dtype
-    rope_ref, norm_ref, tensors = _turn(shape, rope, norm)
-    args = (_want("positions", positions, 4, n), n, *_heads("q", q, n, shape.hq, d, dtype), *_heads("k", k, n, shape.hkv, d, dtype),
-            *_heads("q_out", q_out, n, shape.hq, d, dtype), *_heads("k_out", k_out, n, shape.hkv, d, dtype))
-    _on_gpu(q, k, q_out, k_out, positions, *tensors)
+    n, d, types = (k if q is None else q).shape[0], shape.head_dim, _types(shape.dtype)
+    of_q, of_k = (n, shape.hq, d), (n, shape.hkv, d)
+    rope_ref, norm_ref, tensors = _turn(shape, rope, norm, types)
+    args = (_want("positions", positions, 4, n), n, *_heads("q", q, of_q, types), *_heads("k", k, of_k, types),
+            *_heads("q_out", q_out, of_q, types), *_heads("k_out", k_out, of_k, types))
+    _here(k if q is None else q, k, q_out, k_out, positions, *tensors)
     _check(lib().spork_qk_rope(ctypes.byref(shape), rope_ref, norm_ref, *args, _stream(stream)))
 
 
 def _check_kvq(shape, cache):
-    if cache.tensors[0].shape[1:] != (shape.hkv, shape.block_size, shape.head_dim):
+    if cache.blocks_of != (shape.hkv, shape.block_size, shape.head_dim):
         raise ValueError("the cache must be of the shape's hkv, block_size and head_dim")
 
 
 def spork_kvq_write(shape, cache, rope, norm, slots, positions, q, k, v, q_out, bad_slots=None, stream=None):
     """q and q_out [rows, hq, head_dim] (both may be None), k and v [rows, hkv, head_dim] may have any stride between
     their rows; q_out may be q."""
-    n, d, dtype = slots.shape[0], shape.head_dim, shape.dtype
+    n, d, types = slots.shape[0], shape.head_dim, _types(shape.dtype)
+    of_q, of_k = (n, shape.hq, d), (n, shape.hkv, d)
     _check_kvq(shape, cache)
-    rope_ref, norm_ref, tensors = _turn(shape, rope, norm)
-    args = (_want("slots", slots, 8, n), _want("positions", positions, 4, n), n, *_heads("q", q, n, shape.hq, d, dtype),
-            *_heads("k", k, n, shape.hkv, d, dtype), *_heads("v", v, n, shape.hkv, d, dtype),
-            *_heads("q_out", q_out, n, shape.hq, d, dtype), _want("bad_slots", bad_slots, 4, 1))
-    _on_gpu(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
-    _check(lib().spork_kvq_write(ctypes.byref(shape), ctypes.byref(cache), rope_ref, norm_ref, *args, _stream(stream)))
+    rope_ref, norm_ref, tensors = _turn(shape, rope, norm, types)
+    args = (_want("slots", slots, 8, n), _want("positions", positions, 4, n), n, *_heads("q", q, of_q, types),
+            *_heads("k", k, of_k, types), *_heads("v", v, of_k, types), *_heads("q_out", q_out, of_q, types),
+            _want("bad_slots", bad_slots, 4, 1))
+    _here(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
+    _check(lib().spork_kvq_write(ctypes.byref(shape), cache.ref, rope_ref, norm_ref, *args, _stream(stream)))
 
 
 def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
     most = copies.shape[0]
     _check_kvq(shape, cache)
     args = (_want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1), most)
-    _on_gpu(*cache.tensors, copies, n_copies)
-    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), ctypes.byref(cache), *args, _stream(stream)))
+    _here(*cache.tensors, copies, n_copies)
+    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), cache.ref, *args, _stream(stream)))
 
 
 def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace, stream=None):
     """q [rows, hq, head_dim] may have any stride between its rows; the workspace is spork_chunk_attn's."""
     n_rows, (n_seqs, max_blocks) = q.shape[0], table.shape
     _check_kvq(shape, cache)
-    args = (*_heads("q", q, n_rows, shape.hq, shape.head_dim, shape.dtype), ctypes.byref(cache),
-            _want("table", table, 4, n_seqs, max_blocks), max_blocks, _want("row_off", row_off, 4, n_seqs + 1),
-            _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows, _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace))
-    if out.shape != q.shape or not _of_dtype(shape.dtype, out):
+    types, of_q = _types(shape.dtype), (n_rows, shape.hq, shape.head_dim)
+    args = (*_heads("q", q, of_q, types), cache.ref, _want("table", table, 4, n_seqs, max_blocks), max_blocks,
+            _want("row_off", row_off, 4, n_seqs + 1), _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows)
+    if out.shape != of_q or out.dtype not in types:
         raise ValueError("out must be [rows, hq, head_dim] of the shape's dtype")
-    if lse is not None and (lse.shape != q.shape[:2] or not _of_dtype(SPORK_DTYPE_F32, lse)):
+    if lse is not None and (lse.shape != of_q[:2] or lse.dtype not in _types(SPORK_DTYPE_F32)):
         raise ValueError("lse must be [rows, hq] float32")
-    _on_gpu(q, *cache.tensors, table, row_off, kv_len, out, lse, workspace)
-    _check(lib().spork_kvq_attn(ctypes.byref(shape), *args, _stream(stream)))
+    _here(*cache.tensors, q, table, row_off, kv_len, out, lse, workspace)
+    _check(lib().spork_kvq_attn(ctypes.byref(shape), *args, _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace),
+                                _stream(stream)))
 
 
 # ---- measurement aid --------------------------------------------------------
