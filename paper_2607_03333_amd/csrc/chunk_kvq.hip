@@ -187,10 +187,12 @@ struct DeepStages {
   }
 };
 
-// The stages that a workgroup's waves share (chunk_wide.h): codes come into a ring of
-// three pairs of stages by direct loads, and each wave turns what it has loaded itself
-// into bf16 in the ring of stages, a pair of stages ahead of those that are
-// published. So every code is converted once, not by every wave that needs it.
+// The stages that a workgroup's waves share (chunk_wide.h): each wave loads its part of
+// a pair of stages as codes into registers, a period of two stages ahead, and writes
+// it as bf16 into a ring of three pairs, a pair ahead of the one that is published. So
+// every code is converted once, not by every wave that needs it. (LDS is nearly as
+// busy as the matrix cores here: codes that came into LDS first, by direct loads, cost
+// 2,048 rows behind 30,000 positions 1.86 ms.)
 // Instruction i of wave w takes stage i of a pair, its chunks 64 w .. (64 channels:
 // the lower four waves the first stage, the others the second, chunks 64 (w % 4) ..),
 // the first half of them K. A chunk of K is two of the ring's: its first and last
@@ -201,13 +203,10 @@ struct CodeLoader {
   using E = StageLayout<D, BS>;
   static constexpr bool kCoded = true;
   static constexpr int kRing = 6;         // stages of bf16
-  static constexpr int kPairs = 3;        // pairs of stages of codes
   static constexpr int kStageLoads = 1;   // (of a stage's place in the period)
   static constexpr int kPairLoads = D / 64;
   static constexpr int kPerStage = 32 / BS, kWindow = 64 / kPerStage;  // entries of a stage, stages of a window
-  static constexpr int kPairChunks = 8 * D;
-  static constexpr int kWords = kRing * 8 * D + kPairs * kPairChunks;  // LDS, in 16-byte chunks
-  static constexpr int kSteps = 4;
+  static constexpr int kSteps = 3;
   const char* pool;
   const uint8_t* scales;
   Pages pages;
@@ -217,7 +216,6 @@ struct CodeLoader {
   int wave, lane;
   int stage, half;  // D = 64: the stage of a pair that the wave loads; which block of a stage
   uint32_t off, dst, other;  // of the lane: in a block of codes, in a stage of the ring; bit in which its second chunk there differs
-  uint4* raw;            // codes of the wave in pair 0
   uint32_t ring;
   int now, next;         // lane i: block of entry i of the window that is loaded; entry of the next one
   uint32_t scale_now, scale_next;
@@ -225,8 +223,7 @@ struct CodeLoader {
   const char* from[kPairLoads];
   float scale[kPairLoads];
   uint32_t to[kPairLoads];  // stages of the ring
-  int conv_pair, load_pair;
-  u32x4 w;
+  u32x4 w[kPairLoads];  // the codes
 
   __device__ __forceinline__ int entries(int st) const { return pages.entry(first + st * kPerStage + lane); }
   __device__ __forceinline__ uint32_t scales_of(int block) const { return scales[static_cast<size_t>(block) * hkv]; }
@@ -258,7 +255,6 @@ struct CodeLoader {
       dst = 16u * (E::kHalf + (BS == 16 ? E::kHalf / 2 * h + 2 * d + E::vswz(d) : 4 * d + ((2 * h) ^ E::vswz(d))));
       other = 16;
     }
-    raw = smem + kRing * 8 * D + wave * 64;
     ring = lds_addr(smem);
     now = pages.block(entries(0));
     next = entries(kWindow);
@@ -273,7 +269,6 @@ struct CodeLoader {
       const int block = __builtin_amdgcn_readlane(now, (st + s) % kWindow * kPerStage + half);
       from[i] = pool + static_cast<uint64_t>(static_cast<uint32_t>(block)) * block_bytes;
     }
-    load_pair = st / 2 % kPairs;
   }
   __device__ __forceinline__ void will_convert(int conv) {
 #pragma unroll
@@ -282,78 +277,67 @@ struct CodeLoader {
       scale[i] = scale_of(__builtin_amdgcn_readlane(scale_now, (conv + s) % kWindow * kPerStage + half));
       to[i] = ring + static_cast<uint32_t>((conv + s) % kRing) * (8 * D * 16);
     }
-    conv_pair = conv / 2 % kPairs;
   }
-  __device__ __forceinline__ void load(int i) const {
-    load_lds<kKeep>(from[i], BS * D, off, 0, raw + load_pair * kPairChunks + i * (4 * D));
-  }
-  __device__ __forceinline__ void read(int i) {
-    w = lds_read_b128(lds_addr(raw) + 16u * lane + static_cast<uint32_t>(conv_pair * kPairChunks + i * (4 * D)) * 16u, 0);
+  __device__ __forceinline__ void load(int i) {
+    typedef const __attribute__((address_space(1))) char* global;
+    typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+    w[i] = *(global_u32x4)((global)from[i] + off);
   }
   __device__ __forceinline__ void convert(int i, int b) const {
-    const bf16x8 x = widen(w[2 * b], w[2 * b + 1], scale[i]);
+    const bf16x8 x = widen(w[i][2 * b], w[i][2 * b + 1], scale[i]);
     asm volatile("ds_write_b128 %0, %1" : : "v"(to[i] + (b == 0 ? dst : dst ^ other)), "v"(x) : "memory");
   }
-  // The first pairs: 0 to 2 loaded; then 0 and 1 converted and 3 loaded.
+  // Pairs 0 and 1 loaded; then converted, and pair 2 loaded.
+  u32x4 second[kPairLoads];
   __device__ __forceinline__ void begin() {
 #pragma unroll
-    for (int p = 0; p < kPairs; ++p) {
+    for (int p = 0; p < 2; ++p) {
       will_load(2 * p);
 #pragma unroll
-      for (int i = 0; i < kPairLoads; ++i) load(i);
+      for (int i = 0; i < kPairLoads; ++i) {
+        load(i);
+        if (p == 0) second[i] = w[i];
+      }
     }
   }
   __device__ __forceinline__ void first_pairs() {
-    asm volatile("" : "+v"(scale_now));  // here: no wait for it is left for the stages
-    will_load(6);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       will_convert(2 * p);
-      wait_vmcnt<2 * kPairLoads>();
 #pragma unroll
       for (int i = 0; i < kPairLoads; ++i) {
-        read(i);
-        lds_wait(w, 0);
+        const u32x4 later = w[i];
+        if (p == 0) w[i] = second[i];
         convert(i, 0);
         convert(i, 1);
-      }
-      if (p == 0) {
-#pragma unroll
-        for (int i = 0; i < kPairLoads; ++i) load(i);
+        if (p == 0) w[i] = later;
       }
     }
+    will_load(4);
+#pragma unroll
+    for (int i = 0; i < kPairLoads; ++i) load(i);
   }
-  // Stage st begins a period: stages st + 4 and st + 5 are converted, st + 8 and st + 9 loaded.
+  // Stage st begins a period: stages st + 4 and st + 5 are converted, st + 6 and st + 7 loaded.
   __device__ __forceinline__ void publish(int st) {
-    if ((st + 8) % kWindow == 0) {
+    if ((st + 6) % kWindow == 0) {
       now = pages.block(next);
       asm volatile("" : "+v"(now));
-      next = entries(st + 8 + kWindow);
+      next = entries(st + 6 + kWindow);
       scale_next = scales_of(now);
     }
     if ((st + 4) % kWindow == 0) {
       scale_now = scale_next;
       asm volatile("" : "+v"(scale_now));
     }
-    will_load(st + 8);
+    will_load(st + 6);
     will_convert(st + 4);
   }
   // Step t of the period's stage I.
   template <int I>
   __device__ __forceinline__ void step(int t) {
     if (I >= kPairLoads) return;
-    if (t == 0) {
-      // (behind the awaited pair the next one is in flight)
-      if (I == 0) wait_vmcnt<kPairLoads>();
-      read(I);
-    } else if (t == 1) {
-      load(I);
-    } else if (t == 2) {
-      lds_wait(w, 0);
-      convert(I, 0);
-    } else {
-      convert(I, 1);
-    }
+    if (t < 2) convert(I, t);
+    else load(I);
   }
 };
 
@@ -379,8 +363,8 @@ struct CodeEngine<__bf16, D, BS> {
   static constexpr int kHalf = kTokens * D / 16; // chunks of K, and of V
   static constexpr int kLoads = kHalf / 64;
   static constexpr int kStage = 2 * kHalf, kDepth = 2;
-  static constexpr int kSlot = CodeLoader<D, BS>::kWords / kWaves;
-  static_assert(kSlot >= kDepth * kStage, "a wave's slot holds its stages");
+  static constexpr int kSlot = kDepth * kStage;
+  static_assert(kWaves * kSlot >= CodeLoader<D, BS>::kRing * 8 * D, "the slots hold the ring");
   static constexpr int kSteps = D / 16, kCt = D / 32;
   bf16x8 q[kSteps];
   f32x16 o[kCt];

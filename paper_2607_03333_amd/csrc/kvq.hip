@@ -145,6 +145,9 @@ struct Heads {
         // One pair at a time, from what was loaded to 32 bits: kept in 64, a run's would
         // fill the registers.
         __builtin_amdgcn_sched_barrier(0);
+        Raw<T> w[2] = {weight[0], weight[1]};
+        w[0].anew();  // (or all of them would be kept in 64 bits over the passes)
+        w[1].anew();
         double r = 1.0;
         if (a.turn.k_weight != nullptr) {
           double s = 0.0;
@@ -157,7 +160,7 @@ struct Heads {
         }
         const auto value = [&](int i) __attribute__((always_inline)) {
           const double v = k.raw[p][i / 8].get(i % 8);
-          return a.turn.k_weight != nullptr ? v * (r * weight[i / 8].get(i % 8)) : v;
+          return a.turn.k_weight != nullptr ? v * (r * w[i / 8].get(i % 8)) : v;
         };
         const auto pairs = [&](auto interleaved) __attribute__((always_inline)) {
 #pragma unroll
@@ -466,7 +469,7 @@ bool kvq_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
 hipError_t launch_kvq_write(const KvqWriteArgs& given, hipStream_t stream) {
   KvqWriteArgs a = given;
   a.window = 1;
-  while (a.window < kMostWindow && a.window * 512 < a.n_rows) a.window *= 2;
+  while (a.window < kMostWindow && a.window * 256 < a.n_rows) a.window *= 2;
   if (a.dtype == 1) {
     if (a.head_dim == 128) return a.block_size == 16 ? launch_write<__bf16, 128, 16>(a, stream) : launch_write<__bf16, 128, 32>(a, stream);
     return a.block_size == 16 ? launch_write<__bf16, 64, 16>(a, stream) : launch_write<__bf16, 64, 32>(a, stream);

@@ -40,6 +40,8 @@ struct Raw<__bf16> {
   uint4 w;
   __device__ __forceinline__ void load(const __bf16* p) { w = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ float get(int i) const { return vec_f<__bf16>(w, i); }
+  // Values that the compiler takes for new ones.
+  __device__ __forceinline__ void anew() { asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w)); }
 };
 template <>
 struct Raw<float> {
@@ -49,6 +51,10 @@ struct Raw<float> {
     w[1] = reinterpret_cast<const uint4*>(p)[1];
   }
   __device__ __forceinline__ float get(int i) const { return vec_f<float>(w[i >> 2], i & 3); }
+  __device__ __forceinline__ void anew() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(w[i].x), "+v"(w[i].y), "+v"(w[i].z), "+v"(w[i].w));
+  }
 };
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
