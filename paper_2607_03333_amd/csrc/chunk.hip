@@ -23,6 +23,8 @@
 // and accumulators are fp32.
 #include "chunk_wide.h"
 
+#include <algorithm>
+
 namespace spork {
 namespace {
 
@@ -454,11 +456,6 @@ struct Engine<float, D, BS> {
   }
 };
 
-template <typename T, int D, int BS>
-__global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
-  attend_slice<Engine<T, D, BS>>(a);
-}
-
 // Log-sum-exp merge of a split tile: D / 4 lanes per packed row, four channels a
 // lane. What bounds it is the way of a load, so many are in flight: with up to
 // four pieces (most tiles that a cut goes through have two) a wave takes its next
@@ -468,7 +465,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
 // chunks beside 29 tokens, nearly every tile in two pieces: 19 us when a wave took
 // its rows one after the other, 12 so; one token over 1,000 positions in 8 pieces:
 // 16.5 us of both launches when the rows came behind the weights, 15.6 so.)
-constexpr int kMergeWaves = 4, kMergeGroups = 16;  // of a workgroup; workgroups of a slice
+constexpr int kMergeWaves = 4, kMergeGroups = 16;  // of a workgroup; workgroups of a slice, at most
 
 // A packed row of a split tile, as the merge reads and writes it.
 struct MergeRow {
@@ -541,7 +538,7 @@ __global__ void __launch_bounds__(64 * kMergeWaves) chunk_merge_kernel(ChunkArgs
   const ChunkSplit s = a.splits[slice];
   if (s.n_rows == 0) return;
   const int pieces = s.last - slice + 1, rows = s.n_rows * s.heads;
-  const int first = blockIdx.y * kMergeWaves + static_cast<int>(threadIdx.x >> 6), step = kMergeGroups * kMergeWaves;
+  const int first = blockIdx.y * kMergeWaves + static_cast<int>(threadIdx.x >> 6), step = static_cast<int>(gridDim.y) * kMergeWaves;
   if (pieces <= 2) {
     merge_few<T, D, 2, 4>(a, s, slice, pieces, lane, first, step);
     return;
@@ -604,8 +601,8 @@ using ChunkKernel = void (*)(ChunkArgs);
 template <typename T>
 ChunkKernel pick_attn(int d, int bs) {
   if (bs != 16 && bs != 32) return nullptr;
-  if (d == 64) return bs == 16 ? chunk_attn_kernel<T, 64, 16> : chunk_attn_kernel<T, 64, 32>;
-  if (d == 128) return bs == 16 ? chunk_attn_kernel<T, 128, 16> : chunk_attn_kernel<T, 128, 32>;
+  if (d == 64) return bs == 16 ? chunk_attn_kernel<Engine<T, 64, 16>> : chunk_attn_kernel<Engine<T, 64, 32>>;
+  if (d == 128) return bs == 16 ? chunk_attn_kernel<Engine<T, 128, 16>> : chunk_attn_kernel<Engine<T, 128, 32>>;
   return nullptr;
 }
 
@@ -656,7 +653,12 @@ hipError_t launch_chunk_attn(const ChunkArgs& a, hipStream_t stream) {
 hipError_t launch_chunk_merge(const ChunkArgs& a, hipStream_t stream) {
   const ChunkKernel k = a.dtype == 1 ? pick_merge<__bf16>(a.head_dim) : pick_merge<float>(a.head_dim);
   if (k == nullptr) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k, dim3(kChunkSlices, kMergeGroups), dim3(64 * kMergeWaves), 0, stream, a);
+  // No more workgroups of a slice than a tile can have rows for (one token over 1,000
+  // positions of 8-bit codes 14.3 us with all 16, 13.95 with one).
+  const int64_t rows = std::min(static_cast<int64_t>(a.n_rows) * a.group * a.most_heads, static_cast<int64_t>(kChunkTileRows));
+  const int per_group = kMergeWaves * 64 / (a.head_dim / 4);
+  const int groups = static_cast<int>(std::min((rows + per_group - 1) / per_group, static_cast<int64_t>(kMergeGroups)));
+  hipLaunchKernelGGL(k, dim3(kChunkSlices, groups), dim3(64 * kMergeWaves), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -345,15 +345,17 @@ struct Scale2 {
   float k, v;
 };
 
-template <typename T, int D, int BS>
+// WIDE: tiles of many row tiles share their stages. A call whose rows cannot make such a
+// tile runs the engine without: its registers need not hold both.
+template <typename T, int D, int BS, bool WIDE>
 struct CodeEngine;
 
-template <int D, int BS>
-struct CodeEngine<__bf16, D, BS> {
+template <int D, int BS, bool WIDE>
+struct CodeEngine<__bf16, D, BS, WIDE> {
   using Elem = __bf16;
   using Stages = DeepStages<CodeEngine>;
   static constexpr bool kShifts = true;
-  static constexpr bool kWide = true;
+  static constexpr bool kWide = WIDE;
   static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
   static constexpr int kD = D, kBlock = BS;
   static constexpr int kTokens = 32;             // of a stage
@@ -529,7 +531,7 @@ struct CodeEngine<__bf16, D, BS> {
 };
 
 template <int D, int BS>
-struct CodeEngine<float, D, BS> {
+struct CodeEngine<float, D, BS, false> {
   using Elem = float;
   using Stages = DeepStages<CodeEngine>;
   static constexpr bool kShifts = true;
@@ -691,15 +693,10 @@ struct CodeEngine<float, D, BS> {
   static __device__ __forceinline__ void wide_tile(const ChunkArgs&, const Tile&, const Pages&, uint4 (*)[kSlot], int, int, CodeEngine&) {}
 };
 
-template <typename T, int D, int BS>
-__global__ void __launch_bounds__(64 * kWaves, 1) kvq_attn_kernel(ChunkArgs a) {
-  attend_slice<CodeEngine<T, D, BS>>(a);
-}
-
-template <typename T>
+template <typename T, bool WIDE>
 hipError_t launch(const ChunkArgs& a, hipStream_t stream) {
-  const auto k = a.head_dim == 128 ? (a.block_size == 16 ? kvq_attn_kernel<T, 128, 16> : kvq_attn_kernel<T, 128, 32>)
-                                   : (a.block_size == 16 ? kvq_attn_kernel<T, 64, 16> : kvq_attn_kernel<T, 64, 32>);
+  const auto k = a.head_dim == 128 ? (a.block_size == 16 ? chunk_attn_kernel<CodeEngine<T, 128, 16, WIDE>> : chunk_attn_kernel<CodeEngine<T, 128, 32, WIDE>>)
+                                   : (a.block_size == 16 ? chunk_attn_kernel<CodeEngine<T, 64, 16, WIDE>> : chunk_attn_kernel<CodeEngine<T, 64, 32, WIDE>>);
   hipLaunchKernelGGL(k, dim3(kChunkSlices), dim3(64 * kWaves), 0, stream, a);
   return hipGetLastError();
 }
@@ -707,7 +704,10 @@ hipError_t launch(const ChunkArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_kvq_attn(const ChunkArgs& a, hipStream_t stream) {
-  return a.dtype == 1 ? launch<__bf16>(a, stream) : launch<float>(a, stream);
+  if (a.dtype == 0) return launch<float, false>(a, stream);
+  // (all rows in one sequence would make at most this many packed rows)
+  const bool wide = static_cast<int64_t>(a.n_rows) * a.group > 32 * (kWaves / 2);
+  return wide ? launch<__bf16, true>(a, stream) : launch<__bf16, false>(a, stream);
 }
 
 }  // namespace spork

@@ -274,8 +274,10 @@ template <typename E>
 __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int tid, int64_t* wave_sum, Start* start, int* n_slices,
                                            int64_t* total_out, int64_t* pos_out, int64_t* stop_out) {
   const int lane = tid & 63, wave = tid >> 6;
-  const int per_thread = (a.n_seqs + 64 * kWaves - 1) / (64 * kWaves);
-  const int i0 = min(tid * per_thread, a.n_seqs), i1 = min(i0 + per_thread, a.n_seqs);
+  // Up to 64 sequences: every wave finds the place by itself, without a barrier.
+  const bool few = E::kShifts && a.n_seqs <= 64;
+  const int per_thread = few ? 1 : (a.n_seqs + 64 * kWaves - 1) / (64 * kWaves), me = few ? lane : tid;
+  const int i0 = min(me * per_thread, a.n_seqs), i1 = min(i0 + per_thread, a.n_seqs);
   int64_t sum = 0;
   Seq s;
   for (int i = i0; i < i1; ++i) {
@@ -283,13 +285,17 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     sum += s.group_cost * s.groups;
   }
   int64_t upto = wave_scan(sum);
-  if (lane == 63) wave_sum[wave] = upto;
-  __syncthreads();
   int64_t total = 0;
+  if (few) {
+    total = __shfl(upto, 63);
+  } else {
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) upto += wave_sum[w];
-    total += wave_sum[w];
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) upto += wave_sum[w];
+      total += wave_sum[w];
+    }
   }
   total = uniform(total);
   const int64_t wanted = E::kShifts ? (total + kShortSlice - 1) / kShortSlice : max(total / kMinSlice, static_cast<int64_t>(1));
@@ -328,15 +334,22 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
     if (nth > 0) y0 -= s.before(nth);
     *start = Start{i, s.row0, s.rows, s.kv, group, nth, y0};
   }
-  __syncthreads();
+  if (few) {  // (every wave has written the same)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  } else {
+    __syncthreads();
+  }
   return true;
 }
 
 // A workgroup's slice, with the stage engine E: types and sizes (Elem, kD, kBlock,
-// kTokens, kUnits, kSlot), prices (token_cost), a wave's own stages (stream) and,
-// with kWide, tiles of many row tiles whose stages the waves share (wide_tile).
+// kTokens, kUnits, kSlot), prices (token_cost, kShifts), a wave's own stages (kDepth 1:
+// the loop below; more: Stages) and, with kWide, tiles of more than kNarrowTiles row
+// tiles whose stages the waves share (wide_tile). The kernel itself, and no function
+// that kernels call: with one, the bf16 engine took one token 0.3 us more.
 template <typename E>
-__device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
+__global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a) {
   using T = typename E::Elem;
   constexpr int D = E::kD, BS = E::kBlock;
   constexpr int kFloat4s = D / 8;  // of a lane's accumulator
@@ -501,7 +514,10 @@ __device__ __forceinline__ void attend_slice(const ChunkArgs& a) {
           if (lane < 32 / E::kUnits) ml[wave][E::row(lane, u)] = make_float2(e.m[u], sum);
         }
 #pragma unroll
-        for (int i = 0; i < kFloat4s; ++i) *chunk_at(wave, E::out_row(lane, i), E::out_channel(lane, i) / 4) = e.get(i);
+        for (int i = 0; i < kFloat4s; ++i) {
+          if (!E::kShifts || 32 * rt + E::out_row(lane, i) < n_packed)  // (rows that are none have no place to go)
+            *chunk_at(wave, E::out_row(lane, i), E::out_channel(lane, i) / 4) = e.get(i);
+        }
       }
       if (ways > 1) __syncthreads();
       const bool whole = tok_lo == 0 && tok_hi == end;

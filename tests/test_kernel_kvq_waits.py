@@ -21,11 +21,11 @@ def test_kvq_kernels_wait_before_using_lds_reads(tmp_path):
            "-o", str(out), os.path.join(build.CSRC, "chunk_kvq.hip")]
     subprocess.run(cmd, check=True, capture_output=True, timeout=600)
     asm = out.read_text()
-    assert lds_wait_hazards(asm, r"kvq_attn") == []
+    assert lds_wait_hazards(asm, r"chunk_attn") == []
     kernels, name = {}, None
     for line in asm.splitlines():
         t = line.strip()
-        m = re.match(r"^(_Z\S*kvq_attn\S*):", t)
+        m = re.match(r"^(_Z\S*CodeEngine\S*):", t)
         if m:
             name = m.group(1)
             kernels[name] = []
@@ -33,7 +33,7 @@ def test_kvq_kernels_wait_before_using_lds_reads(tmp_path):
             name = None
         elif name:
             kernels[name].append(t)
-    assert len(kernels) == 8  # two types, two head sizes, two block sizes
+    assert len(kernels) == 12  # bf16 with and without shared stages, fp32; two head sizes, two block sizes
     for name, lines in kernels.items():
         assert sum("ds_read" in t for t in lines), name
         assert pending_read_uses(lines) == [], name
