@@ -116,6 +116,7 @@ struct Engine<__bf16, D, BS> : StageLayout<D, BS> {
   using Stages = int;
   static constexpr int kDepth = 1;
   static constexpr bool kShifts = false;
+  static constexpr int kTile = kTileCost;
   static constexpr bool kWide = true;
   static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
   static constexpr int kD = D, kBlock = BS;
@@ -300,6 +301,7 @@ struct Engine<float, D, BS> {
   using Stages = int;
   static constexpr int kDepth = 1;
   static constexpr bool kShifts = false;
+  static constexpr int kTile = kTileCost;
   static constexpr bool kWide = false;
   static constexpr int kNarrowTiles = kWaves;
   static constexpr int kD = D, kBlock = BS;

@@ -114,9 +114,8 @@ struct DeepStages {
     const int off = (first + k * stride) % E::kBlock;  // (bf16: 0)
     E::template load<POLICY, kValues>(from, at, off, to);
   }
-  template <int POLICY>
-  __device__ __forceinline__ void begin(const ChunkArgs& a, const Pages& pg, const Bases& at, int head, int first_, int stride_, int seen,
-                                        int lane, uint4* slot) {
+  // Entries of the first windows are asked for, in front of all else of the tile.
+  __device__ __forceinline__ void look_up(const ChunkArgs& a, const Pages& pg, int head, int first_, int stride_, int seen, int lane) {
     constexpr int kBytes = E::kBlock * E::kD;
     hkv = a.hkv;
     block_bytes = alone_in_scalars(static_cast<uint32_t>(hkv) * kBytes);
@@ -127,8 +126,12 @@ struct DeepStages {
     first = first_;
     stride = stride_;
     count = (seen - first - 1) / stride + 1;
-    now = pg.block(entries(pg, 0, lane));
+    now = entries(pg, 0, lane);
     next = entries(pg, 1, lane);
+  }
+  template <int POLICY>
+  __device__ __forceinline__ void begin(const Pages& pg, const Bases& at, uint4* slot) {
+    now = pg.block(now);
     load_scales(k_first, v_first);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -355,8 +358,15 @@ struct CodeEngine<__bf16, D, BS, WIDE> {
   using Elem = __bf16;
   using Stages = DeepStages<CodeEngine>;
   static constexpr bool kShifts = true;
+  // A tile's start-up: chunks beside 60 tokens, 64 heads, 292 us at 600, 281 at 1,000,
+  // 271 at 1,600; 24 prompts of up to 777 tokens with 16 heads of 64 61, 54, 52.5; 96
+  // single tokens 152.5, 148, 148.5.
+  static constexpr int kTile = 1600;
   static constexpr bool kWide = WIDE;
-  static constexpr int kNarrowTiles = kWaves / 2;  // row tiles of a tile that isn't wide
+  // Row tiles of a tile that isn't wide: 16 sequences of 9 rows over 8,000 positions, 64
+  // heads in groups of 8 (three row tiles) 111 us with stages of each wave's own, 98 with
+  // shared ones; in groups of 4 (two) 74 and 88.
+  static constexpr int kNarrowTiles = 2;
   static constexpr int kD = D, kBlock = BS;
   static constexpr int kTokens = 32;             // of a stage
   static constexpr int kUnits = 1;               // rows of a lane
@@ -373,10 +383,12 @@ struct CodeEngine<__bf16, D, BS, WIDE> {
   float m[1], l[1];
   int hz[1];  // last visible position of the lane's row
 
-  // The line's unit is chunk.hip's: a token of 128 channels costs half of what it
-  // costs in bf16 until the products weigh more.
+  // The line's unit is what a token of 128 channels takes where HBM bounds it, about 6
+  // ns on one compute unit, until the products weigh more. (Three chunks beside 29
+  // tokens 190 us at a price of 2 for more than one row tile, 182 at 4, 222 at 8 from
+  // five row tiles on.)
   static __device__ __forceinline__ int token_cost(const ChunkArgs&, int row_tiles, int heads) {
-    return max(D == 128 ? heads : (heads + 1) / 2, row_tiles <= 2 ? 1 : 2);
+    return max(D == 128 ? heads : (heads + 1) / 2, row_tiles <= 1 ? 1 : 4);
   }
   static __device__ __forceinline__ int row(int lane, int) { return lane & 31; }
   static __device__ __forceinline__ int out_row(int lane, int) { return lane & 31; }
@@ -535,6 +547,7 @@ struct CodeEngine<float, D, BS, false> {
   using Elem = float;
   using Stages = DeepStages<CodeEngine>;
   static constexpr bool kShifts = true;
+  static constexpr int kTile = kTileCost;
   static constexpr bool kWide = false;
   static constexpr int kNarrowTiles = kWaves;
   static constexpr int kD = D, kBlock = BS;
@@ -706,7 +719,8 @@ hipError_t launch(const ChunkArgs& a, hipStream_t stream) {
 hipError_t launch_kvq_attn(const ChunkArgs& a, hipStream_t stream) {
   if (a.dtype == 0) return launch<float, false>(a, stream);
   // (all rows in one sequence would make at most this many packed rows)
-  const bool wide = static_cast<int64_t>(a.n_rows) * a.group > 32 * (kWaves / 2);
+  constexpr int kNarrow = CodeEngine<__bf16, 128, 16, true>::kNarrowTiles;
+  const bool wide = static_cast<int64_t>(a.n_rows) * a.group > 32 * kNarrow;
   return wide ? launch<__bf16, true>(a, stream) : launch<__bf16, false>(a, stream);
 }
 

@@ -72,7 +72,8 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 // more it sees, and so every two neighbours cost the same and slices end where
 // tiles do (in the order of the tiles a 4,096-token prompt's first slices held
 // eleven start-ups each).
-struct Seq {
+template <int TILE>
+struct SeqOf {
   int row0, rows, kv;
   int per;    // query rows of a tile
   int tiles;  // per group of KV heads
@@ -81,7 +82,7 @@ struct Seq {
   int64_t group_cost;
   // positions that tile j sees
   __device__ __forceinline__ int end(int j) const { return max(0, kv - rows + min(rows, (j + 1) * per)); }
-  __device__ __forceinline__ int64_t tile_cost(int j) const { return kTileCost + static_cast<int64_t>(end(j)) * cost; }
+  __device__ __forceinline__ int64_t tile_cost(int j) const { return TILE + static_cast<int64_t>(end(j)) * cost; }
   // cost of the tiles 0 .. j - 1
   __device__ __forceinline__ int64_t first(int j) const {
     const int64_t base = kv - rows;
@@ -92,7 +93,7 @@ struct Seq {
       tokens = (whole - blind) * base +
                per * (static_cast<int64_t>(whole) * (whole + 1) / 2 - static_cast<int64_t>(blind) * (blind + 1) / 2);
     if (j == tiles) tokens += max(0, kv);
-    return static_cast<int64_t>(j) * kTileCost + tokens * cost;
+    return static_cast<int64_t>(j) * TILE + tokens * cost;
   }
   // the k-th tile on the line, and the cost of those before it
   __device__ __forceinline__ int at(int k) const { return k & 1 ? tiles - 1 - (k >> 1) : k >> 1; }
@@ -103,8 +104,8 @@ struct Seq {
 
 // Offsets and lengths are clamped to what the buffers hold.
 template <typename E>
-__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off, int kv) {
-  Seq s;
+__device__ __forceinline__ SeqOf<E::kTile> seq_of(const ChunkArgs& a, int off, int next_off, int kv) {
+  SeqOf<E::kTile> s;
   s.row0 = min(max(off, 0), a.n_rows);
   s.rows = max(0, min(max(next_off, 0), a.n_rows) - s.row0);
   s.kv = min(max(kv, 0), a.max_blocks * a.block_size);
@@ -118,12 +119,12 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int off, int next_off,
   return s;
 }
 template <typename E>
-__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int i) {
+__device__ __forceinline__ SeqOf<E::kTile> seq_of(const ChunkArgs& a, int i) {
   return seq_of<E>(a, a.row_off[i], a.row_off[i + 1], a.kv_len[i]);
 }
 // The same for an i that all lanes share, in scalar registers.
 template <typename E>
-__device__ __forceinline__ Seq seq_uniform(const ChunkArgs& a, int i) {
+__device__ __forceinline__ SeqOf<E::kTile> seq_uniform(const ChunkArgs& a, int i) {
   return seq_of<E>(a, uniform(a.row_off[i]), uniform(a.row_off[i + 1]), uniform(a.kv_len[i]));
 }
 
@@ -147,11 +148,11 @@ __device__ __forceinline__ int cut(int64_t y, int64_t tile_cost, int cost, int e
   if (y >= tile_cost) return end;
   if constexpr (E::kShifts) {
     const int by = 31 - __builtin_clz(cost);
-    const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) >> by) & ~31;
+    const int t = static_cast<int>(max(static_cast<int64_t>(0), y - E::kTile) >> by) & ~31;
     const int least = max(32, kMinPiece >> by & ~31);
     return t < least ? 0 : t > end - least ? end : t;
   }
-  const int t = static_cast<int>(max(static_cast<int64_t>(0), y - kTileCost) / cost) & ~31;
+  const int t = static_cast<int>(max(static_cast<int64_t>(0), y - E::kTile) / cost) & ~31;
   const int least = max(32, kMinPiece / cost & ~31);
   return t < least ? 0 : t > end - least ? end : t;
 }
@@ -279,7 +280,7 @@ __device__ __forceinline__ bool find_slice(const ChunkArgs& a, int slice, int ti
   const int per_thread = few ? 1 : (a.n_seqs + 64 * kWaves - 1) / (64 * kWaves), me = few ? lane : tid;
   const int i0 = min(me * per_thread, a.n_seqs), i1 = min(i0 + per_thread, a.n_seqs);
   int64_t sum = 0;
-  Seq s;
+  SeqOf<E::kTile> s;
   for (int i = i0; i < i1; ++i) {
     s = seq_of<E>(a, i);
     sum += s.group_cost * s.groups;
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   if (!find_slice<E>(a, slice, tid, wave_sum, &start, &n_slices, &total, &pos, &stop)) return;
   int seq = start.seq, head_group = start.group, nth = start.nth;
   int64_t y0 = start.y0;
-  Seq sq;
+  SeqOf<E::kTile> sq;
   sq.row0 = start.row0;
   sq.rows = start.rows;
   sq.kv = start.kv;
@@ -443,6 +444,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
           look_up(ahead, first + stride);
           issue_k(first % BS);
           issue_v(first % BS);
+        } else {
+          stages.look_up(a, pg, head, first, stride, seen, lane);
         }
       }
       int least = INT_MAX;
@@ -459,8 +462,8 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
       }
       if constexpr (E::kDepth > 1) {  // behind the queries: a wait for these is none for the stages
         if (!wide && first < seen) {
-          if (alone) stages.template begin<kStream>(a, pg, at, head, first, stride, seen, lane, smem[wave]);
-          else stages.template begin<kKeep>(a, pg, at, head, first, stride, seen, lane, smem[wave]);
+          if (alone) stages.template begin<kStream>(pg, at, smem[wave]);
+          else stages.template begin<kKeep>(pg, at, smem[wave]);
         }
       }
       least = uniform(wave_min_int(least));
