@@ -27,6 +27,11 @@
  *   - spork_ngram_propose: the n-gram (prompt-lookup) draft proposer of the
  *     engine's n-gram speculative decoding (Sections 4.3 and 6.1), a second
  *     source of the drafts spork_verify_accept checks.
+ *   - spork_qk_rope: norms and rotary positions of a projection's queries and
+ *     keys.
+ *   - spork_kvq_write, spork_kvq_copy_batch, spork_kvq_attn: a KV cache of 8-bit
+ *     codes with a scale for each block and head; the writes norm and rotate on
+ *     the way, and the attention of prompt chunks and single tokens reads it.
  *
  * Conventions
  *   - Every entry point returns SPORK_OK (0) or a negative status and never
@@ -581,7 +586,8 @@ int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_sca
  * NULL. Rows 16-byte aligned: the parts of a fused projection's rows will do.
  * q_out may be q, and k_out k, at the same stride; else outputs must not overlap
  * each other or the inputs (SPORK_E_INVAL). bf16 rows: computed in float32,
- * rounded once. One launch. */
+ * rounded once. Hq * D must be below 2^30 and n_rows * ((Hq + Hkv + 7) / 8) below
+ * 2^26 - 4 (SPORK_E_UNSUPPORTED). One launch. */
 int spork_qk_rope(const spork_shape* shape, const spork_rope* rope, const spork_qk_norm* norm,
                   const int32_t* positions, int32_t n_rows, const void* q, int64_t q_stride,
                   const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
@@ -623,7 +629,9 @@ typedef struct spork_kvq {
  * infinities and NaN become NaN and don't count for the scale. Keys are normed
  * and rotated in float64 and rounded to their codes once; queries are computed in
  * float32. Scale bytes of blocks that hold tokens must be ones that this call
- * wrote (27 .. 247; others are taken for the nearest of these). One launch. */
+ * wrote (27 .. 247; others are taken for the nearest of these). For this and the
+ * next two Hq * D must be below 2^30 and Hkv * D * block_size below 2^31, here also
+ * n_rows * (Hq + Hkv) below 2^25 (SPORK_E_UNSUPPORTED). One launch. */
 int spork_kvq_write(const spork_shape* shape, const spork_kvq* cache, const spork_rope* rope,
                     const spork_qk_norm* norm, const int64_t* slots, const int32_t* positions,
                     int32_t n_rows, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
@@ -631,7 +639,8 @@ int spork_kvq_write(const spork_shape* shape, const spork_kvq* cache, const spor
                     int32_t* bad_slots, hipStream_t stream);
 
 /* spork_kv_copy_batch for the cache of 8-bit codes: the codes of slots
- * 0..n_valid-1 of block src into block dst, and the scales of all heads. */
+ * 0..n_valid-1 of block src into block dst, and the scales of all heads.
+ * max_copies * Hkv must be below 2^24 (SPORK_E_UNSUPPORTED). One launch. */
 int spork_kvq_copy_batch(const spork_shape* shape, const spork_kvq* cache, const int32_t* copies,
                          const int32_t* n_copies, int32_t max_copies, hipStream_t stream);
 

@@ -19,6 +19,11 @@
 //            through LDS: the pool is channel-major. A run that doesn't fill its
 //            block is put into the 16 bytes of each channel that the block holds.
 //   queries  in 32 bits, as in rope.hip.
+// Rows read once and codes written once bound it: a prompt of 4,096 tokens with 32
+// query and 8 KV heads of 128, normed and turned, 92 MB, takes 24.2 us (3.8 TB/s; a
+// large copy has 5.1, which would be 18). What is left is the keys' arithmetic in 64
+// bits, behind two barriers a run. A step of few tokens costs a launch and the
+// waits for slots, rows and old codes: 96 tokens 9.9 us.
 #include "turn.h"
 
 namespace spork {
@@ -308,7 +313,7 @@ struct Window {
   }
 };
 
-// A wave's query heads of one token: as qk_rope_kernel's (rope.hip).
+// A wave's query heads of one token, twice qk_rope_kernel's (rope.hip).
 constexpr int kQueryGroups = 2;
 
 template <typename T, int D>
@@ -468,6 +473,11 @@ bool kvq_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
 
 hipError_t launch_kvq_write(const KvqWriteArgs& given, hipStream_t stream) {
   KvqWriteArgs a = given;
+  // A workgroup takes a window of n / 256 rows or more, a power of two. Narrower windows
+  // have more workgroups for steps of single tokens, of which each starts a run; wider ones
+  // leave a prompt's runs fewer workgroups that find none. With n / 512 (n / 256), us:
+  // a prompt of 300 tokens 13.7 (11.6), of 1,024 22.4 (15.4), of 4,096 32.3 (24.2); 300
+  // single tokens 11.5 (12.2), 600 18.8 (22.2), 1,024 27.8 (28.2).
   a.window = 1;
   while (a.window < kMostWindow && a.window * 256 < a.n_rows) a.window *= 2;
   if (a.dtype == 1) {

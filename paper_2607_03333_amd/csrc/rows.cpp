@@ -18,6 +18,10 @@ using namespace spork::capi;
 
 // A launch has fewer than 2^32 threads: so many workgroups of 256.
 constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
+// Rows of heads that a write takes, so that its workgroups (kvq.hip) are fewer than these:
+// for keys and values at most n_rows (hkv + 3) / 2, of which a window of 16 rows leaves a
+// sixteenth from 2,049 rows on, and n_rows (hq + 15) / 64 + 1 for queries.
+constexpr int64_t kMostHeadRows = int64_t{1} << 25;
 // Positions run a few stages past a context's end, in 32 bits.
 constexpr int64_t kHeadroom = 4096;
 
@@ -242,7 +246,8 @@ int spork_kvq_write(const spork_shape* shape, const spork_kvq* cache, const spor
     if (rc != SPORK_OK) return rc;
     if ((!in_place(qr, qo) && rows_meet(qo, qr, n_rows, elem)) || rows_meet(qo, kr, n_rows, elem) || rows_meet(qo, vr, n_rows, elem))
       return fail(SPORK_E_INVAL, "q_out must not overlap what is read, unless in place of q");
-    if (n_rows > kMostGroups / 16) return fail(SPORK_E_UNSUPPORTED, "n_rows must be below 2^20");
+    if (static_cast<int64_t>(n_rows) * (static_cast<int64_t>(shape->hq) + shape->hkv) >= kMostHeadRows)
+      return fail(SPORK_E_UNSUPPORTED, "n_rows * (hq + hkv) must be below 2^25");
     spork::KvqWriteArgs a{};
     a.turn = turn_args(rope, norm);
     a.pools = pools_of(cache);

@@ -137,6 +137,18 @@ def test_rows_of_a_write():
     for bad in (dict(q_out=at(0) + 256), dict(q_out=at(1)), dict(q_out=at(2) + 512), dict(q_out=at(0), q_out_stride=8192)):
         assert write(**bad) == INVAL and b"overlap" in spork.lib().spork_last_error(), bad
     assert write(n_rows=1 << 20, q=None, q_out=None, norm=None) == UNSUPPORTED
+    for heads in (dict(hq=1, hkv=1, d=64), dict(hq=1 << 15, hkv=1 << 15, d=64, bs=32)):  # the fewest and the most KV heads
+        wide, most = heads["hq"] * 64, (1 << 25) // (heads["hq"] + heads["hkv"])
+        f = dict(rope=None, norm=None, q=None, q_out=None, q_stride=0, q_out_stride=0, k_stride=wide, v=1 << 50, v_stride=wide)
+        assert write(shape(**heads), n_rows=most, **f) == UNSUPPORTED and b"2^25" in spork.lib().spork_last_error()
+
+
+def test_blocks_of_many_heads():
+    """A block's codes of all heads are placed by 31 bits."""
+    for d, bs, hkv in ((64, 16, 1 << 21), (128, 32, 1 << 19)):
+        for call in (write, attn, copy):
+            assert call(shape(hq=hkv, hkv=hkv, d=d, bs=bs)) == UNSUPPORTED, (call, d)
+            assert b"2^31" in spork.lib().spork_last_error()
 
 
 def test_copies():
