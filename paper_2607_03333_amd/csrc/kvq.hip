@@ -13,17 +13,20 @@
 // in a window of rows; and query heads. Nothing is left to atomics.
 //   keys     16 bytes a lane and load, D / 16 lanes a token (turn.h). Norm and
 //            rotation are in 64 bits: 32 would put values that lie near the middle
-//            of two codes on the wrong side. What is kept of the result is 32 bits
+//            of two codes on the wrong side. What is kept of the result is 16 bits
 //            rounded to odd, from which the 8 bits come out as from the 64.
 //   values   four tokens of eight channels a lane, packed by channel and turned
 //            through LDS: the pool is channel-major. A run that doesn't fill its
 //            block is put into the 16 bytes of each channel that the block holds.
 //   queries  in 32 bits, as in rope.hip.
 // Rows read once and codes written once bound it: a prompt of 4,096 tokens with 32
-// query and 8 KV heads of 128, normed and turned, 92 MB, takes 24.2 us (3.8 TB/s; a
-// large copy has 5.1, which would be 18). What is left is the keys' arithmetic in 64
-// bits, behind two barriers a run. A step of few tokens costs a launch and the
-// waits for slots, rows and old codes: 96 tokens 9.9 us.
+// query and 8 KV heads of 128, normed and turned, 92 MB, takes 22.8 us (4.05 TB/s; a
+// large copy has 5.1, which would be 18). The keys' arithmetic in 64 bits and their two
+// barriers a run go beside the queries' rows, two thirds of the bytes; registers
+// decide how many workgroups do (166 of them 24.4 us, 125 22.8). A step of few tokens
+// costs a launch and the waits for slots, rows and old codes: 96 tokens 9.9 us.
+#include <algorithm>
+
 #include "turn.h"
 
 namespace spork {
@@ -46,23 +49,34 @@ __device__ __forceinline__ uint32_t top_bits(float x) {
   return u < 0x7F800000u ? u : 0u;
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int by = 32; by >= 1; by >>= 1) x = max(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), by)));
-  return x;
+  const auto with = [&](float y) __attribute__((always_inline)) { x = max(x, __float_as_uint(y)); };
+  with(dpp_mov<0xB1>(__uint_as_float(x)));  // of two, four, eight, and all 16 lanes of a row
+  with(dpp_mov<0x4E>(__uint_as_float(x)));
+  with(dpp_mov<0x141>(__uint_as_float(x)));
+  with(dpp_mov<0x140>(__uint_as_float(x)));
+  const auto row = [&](int r) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), 16 * r)); };
+  return max(max(row(0), row(1)), max(row(2), row(3)));
 }
 
-// 64 bits to 32, rounded to odd: the last place is set where anything was cut off,
-// so that a later rounding to fewer places (22 or less) sees on which side of a
-// middle the value lies. (Below 2^-126, far under the least code: zero.)
-__device__ __forceinline__ float round_odd(double x) {
+// 64 bits to bf16's 16, rounded to odd: the last of the 8 places is set where anything
+// was cut off, so that a later rounding to 6 places or fewer sees on which side of a
+// middle the value lies: a code has 4, and so has the largest code's multiple that a
+// scale is found by. (Below 2^-126, far under the least code: zero.)
+__device__ __forceinline__ uint32_t round_odd(double x) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const uint32_t sign = static_cast<uint32_t>(u >> 32) & 0x80000000u;
-  const int e = static_cast<int>(u >> 52 & 0x7FF) - 1023;
-  if (e >= 128) return static_cast<float>(x);  // infinities and NaN, and what 32 bits don't hold
-  if (e < -126) return __uint_as_float(sign);
-  const uint32_t m = static_cast<uint32_t>(u >> 29) & 0x7FFFFFu;
-  return __uint_as_float(sign | static_cast<uint32_t>(e + 127) << 23 | m | ((u & 0x1FFFFFFFu) != 0 ? 1u : 0u));
+  const uint32_t hi = static_cast<uint32_t>(u >> 32), sign = hi >> 16 & 0x8000u;
+  const int e = static_cast<int>(hi >> 20 & 0x7FF) - 1023;
+  if (e >= 128) return sign | 0x7F80u | (x == x ? 0u : 0x40u);  // infinities and NaN, and what bf16 doesn't hold
+  if (e < -126) return sign;
+  return sign | static_cast<uint32_t>(e + 127) << 7 | (hi >> 13 & 0x7Fu) | (((hi & 0x1FFFu) | static_cast<uint32_t>(u)) != 0 ? 1u : 0u);
 }
+
+// Eight values as bf16's 16 bits.
+struct Odd8 {
+  uint32_t w[4];
+  __device__ __forceinline__ void set(int i, uint32_t bits) { w[i / 2] = i % 2 == 0 ? bits : w[i / 2] | bits << 16; }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xFFFF0000u); }
+};
 
 // Four codes. (Infinities are coded as NaN: the codes have none.)
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
@@ -81,8 +95,10 @@ __device__ __forceinline__ uint4 recode16(uint4 w, float by) {
 }
 
 // The lane's run of 8 codes.
-__device__ __forceinline__ uint2 codes8(const float* x, float by) {
-  return make_uint2(codes4(x[0] * by, x[1] * by, x[2] * by, x[3] * by), codes4(x[4] * by, x[5] * by, x[6] * by, x[7] * by));
+template <typename X>
+__device__ __forceinline__ uint2 codes8(const X& x, float by) {
+  return make_uint2(codes4(x.get(0) * by, x.get(1) * by, x.get(2) * by, x.get(3) * by),
+                    codes4(x.get(4) * by, x.get(5) * by, x.get(6) * by, x.get(7) * by));
 }
 
 // A run: its first row, its block, the tokens of the block in front of it, and its length.
@@ -116,7 +132,8 @@ struct Heads {
 
   static __device__ __forceinline__ int exponent(uint8_t byte) { return min(max(byte - kBias, kLeastExp), kMostExp); }
 
-  // The run's keys, as they are loaded, and the scale of the tokens in front of them.
+  // The run's keys, as they are loaded, and the scale of the tokens in front of them. (Lanes
+  // without a token have the last one's: it changes no largest magnitude.)
   struct Keys {
     Raw<T> raw[kKeyPasses][2];
     uint8_t before;
@@ -124,11 +141,10 @@ struct Heads {
       const T* src = static_cast<const T*>(a.k) + run.row * a.k_stride + head * D;
 #pragma unroll
       for (int p = 0; p < kKeyPasses; ++p) {
-        const int t = p * kRows + lane / kLanes;
-        if (t < run.tokens) {
-          raw[p][0].load(src + t * a.k_stride + at.a);
-          raw[p][1].load(src + t * a.k_stride + at.b);
-        }
+        if (p * kRows >= run.tokens) break;
+        const int t = min(p * kRows + lane / kLanes, run.tokens - 1);
+        raw[p][0].load(src + t * a.k_stride + at.a);
+        raw[p][1].load(src + t * a.k_stride + at.b);
       }
       before = a.pools.k_scale[run.block * a.hkv + head];
     }
@@ -137,17 +153,17 @@ struct Heads {
   static __device__ __forceinline__ void write_keys(const KvqWriteArgs& a, const Run& run, int head, const Runs& at, const Keys& k,
                                                     const Raw<T> (&weight)[2], const double2* table, int lane) {
     const int c = lane % kLanes;
-    float x[kKeyPasses][16];
+    std::conditional_t<kTurn, Odd8, Raw<T>> x[kKeyPasses][2];
     uint32_t top = 0;
 #pragma unroll
     for (int p = 0; p < kKeyPasses; ++p) {
-      const int t = p * kRows + lane / kLanes;
-      if (t >= run.tokens) continue;
+      if (p * kRows >= run.tokens) break;
+      const int t = min(p * kRows + lane / kLanes, run.tokens - 1);
       if constexpr (!kTurn) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[p][i] = k.raw[p][i / 8].get(i % 8);
+        x[p][0] = k.raw[p][0];
+        x[p][1] = k.raw[p][1];
       } else {
-        // One pair at a time, from what was loaded to 32 bits: kept in 64, a run's would
+        // One pair at a time, from what was loaded to 16 bits: kept in 64, a run's would
         // fill the registers.
         __builtin_amdgcn_sched_barrier(0);
         Raw<T> w[2] = {weight[0], weight[1]};
@@ -163,8 +179,11 @@ struct Heads {
           }
           r = norm_factor<D>(s, a.turn.eps);
         }
+        Raw<T> raw[2] = {k.raw[p][0], k.raw[p][1]};
+        raw[0].anew();  // (as above)
+        raw[1].anew();
         const auto value = [&](int i) __attribute__((always_inline)) {
-          const double v = k.raw[p][i / 8].get(i % 8);
+          const double v = raw[i / 8].get(i % 8);
           return a.turn.k_weight != nullptr ? v * (r * w[i / 8].get(i % 8)) : v;
         };
         const auto pairs = [&](auto interleaved) __attribute__((always_inline)) {
@@ -178,8 +197,8 @@ struct Heads {
               v = v * cs.x + u * cs.y;
               u = y;
             }
-            x[p][lo] = round_odd(u);
-            x[p][hi] = round_odd(v);
+            x[p][lo / 8].set(lo % 8, round_odd(u));
+            x[p][hi / 8].set(hi % 8, round_odd(v));
             __builtin_amdgcn_sched_barrier(0);
           }
         };
@@ -187,7 +206,7 @@ struct Heads {
         else pairs(std::false_type{});
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = max(top, top_bits(x[p][i]));
+      for (int i = 0; i < 16; ++i) top = max(top, top_bits(x[p][i / 8].get(i % 8)));
     }
     const int before = run.kept > 0 ? exponent(k.before) : kLeastExp;
     const int e = max(before, scale_exp(wave_max(top)));
@@ -199,8 +218,8 @@ struct Heads {
       const int t = p * kRows + lane / kLanes;
       if (t >= run.tokens) continue;
       uint8_t* dst = codes + (run.kept + t) * D;
-      *reinterpret_cast<uint2*>(dst + at.a) = codes8(x[p], by);
-      *reinterpret_cast<uint2*>(dst + at.b) = codes8(x[p] + 8, by);
+      *reinterpret_cast<uint2*>(dst + at.a) = codes8(x[p][0], by);
+      *reinterpret_cast<uint2*>(dst + at.b) = codes8(x[p][1], by);
     }
     if (run.kept > 0 && e > before) {
       const float again = exp2_int(max(before - e, -126));
@@ -313,7 +332,10 @@ struct Window {
   }
 };
 
-// A wave's query heads of one token, twice qk_rope_kernel's (rope.hip).
+constexpr int64_t kMostRunGroups = 1536;  // of keys and values, as far as windows can (launch_kvq_write)
+
+// A wave's query heads of one token, twice qk_rope_kernel's (rope.hip): a prompt of 4,096
+// tokens 24.1 us with as many, 22.8 with twice, 23.2 with four times as many.
 constexpr int kQueryGroups = 2;
 
 template <typename T, int D>
@@ -372,8 +394,8 @@ __global__ void __launch_bounds__(64 * kWriteWaves) kvq_write_kernel(KvqWriteArg
   constexpr int kTableBytes = kTurn ? BS * (D / 2) * sizeof(double2) : 0, kTilesBytes = kWriteWaves * kTileWords<D, BS> * 4;
   __shared__ __align__(16) char memory[kTableBytes > kTilesBytes ? kTableBytes : kTilesBytes];  // of keys, values or queries
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int head_groups = (a.hkv + kWriteWaves - 1) / kWriteWaves, windows = (a.n_rows + a.window - 1) / a.window;
-  const int64_t groups = static_cast<int64_t>(windows) * head_groups;  // of keys, and of values
+  const int head_groups = (a.hkv + kWriteWaves - 1) / kWriteWaves;
+  const int64_t groups = static_cast<int64_t>(a.phases) * a.stretch * head_groups;  // of keys, and of values
   const int64_t group = blockIdx.x;
   if (group >= 2 * groups) {
     write_queries<T, D>(a, static_cast<int64_t>(a.pools.num_blocks) * BS, (group - 2 * groups) * kWriteWaves + wave,
@@ -382,7 +404,10 @@ __global__ void __launch_bounds__(64 * kWriteWaves) kvq_write_kernel(KvqWriteArg
   }
   const bool values = group >= groups;
   const int at_group = static_cast<int>(values ? group - groups : group);
-  const int row0 = at_group / head_groups * a.window, head = at_group % head_groups * kWriteWaves + wave;
+  const int head = at_group % head_groups * kWriteWaves + wave, place = at_group / head_groups;
+  const int64_t row = (static_cast<int64_t>(place % a.stretch) * a.phases + place / a.stretch) * a.window;
+  if (row >= a.n_rows) return;
+  const int row0 = static_cast<int>(row);
   Window<BS> window(a, row0, lane);
   if (values) {
     uint32_t* tile = reinterpret_cast<uint32_t*>(memory) + wave * kTileWords<D, BS>;
@@ -424,7 +449,7 @@ hipError_t launch_write(const KvqWriteArgs& a, hipStream_t stream) {
   const bool turn = a.turn.rotary_dim > 0 || a.turn.q_weight != nullptr || a.turn.k_weight != nullptr;
   const auto k = turn ? kvq_write_kernel<T, D, BS, true> : kvq_write_kernel<T, D, BS, false>;
   constexpr int kTaskHeads = kQueryGroups * 64 / (D / 16);
-  const int64_t windows = (static_cast<int64_t>(a.n_rows) + a.window - 1) / a.window;
+  const int64_t windows = static_cast<int64_t>(a.phases) * a.stretch;
   const int64_t queries = a.q == nullptr ? 0 : static_cast<int64_t>(a.n_rows) * ((a.hq + kTaskHeads - 1) / kTaskHeads);
   const int64_t groups = 2 * windows * ((a.hkv + kWriteWaves - 1) / kWriteWaves) + (queries + kWriteWaves - 1) / kWriteWaves;
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(groups)), dim3(64 * kWriteWaves), 0, stream, a);
@@ -473,13 +498,21 @@ bool kvq_supported(int32_t dtype, int32_t head_dim, int32_t block_size) {
 
 hipError_t launch_kvq_write(const KvqWriteArgs& given, hipStream_t stream) {
   KvqWriteArgs a = given;
-  // A workgroup takes a window of n / 256 rows or more, a power of two. Narrower windows
-  // have more workgroups for steps of single tokens, of which each starts a run; wider ones
-  // leave a prompt's runs fewer workgroups that find none. With n / 512 (n / 256), us:
-  // a prompt of 300 tokens 13.7 (11.6), of 1,024 22.4 (15.4), of 4,096 32.3 (24.2); 300
-  // single tokens 11.5 (12.2), 600 18.8 (22.2), 1,024 27.8 (28.2).
+  // Windows are as narrow as leaves the workgroups of keys and values at most kMostRunGroups:
+  // fewer would wait for each other's runs, more find none where runs are long. A workgroup's
+  // rows and the time with 8 KV heads of 128, us: 300 single tokens one 10.4, two 10.7, four
+  // 14.7; 1,000 one 25.7, four 22.3, eight 28.4; a prompt of 4,096 four 29.2, eight 26.5, 16
+  // 25.4. With 4 KV heads: 1,000 single tokens one 15.8, two 14.4, four 16.7; 192 forks' 8 to
+  // 50 tokens two 12.7, four 10.7, eight 10.8, 16 11.7.
+  const int64_t head_groups = (a.hkv + kWriteWaves - 1) / kWriteWaves;
   a.window = 1;
-  while (a.window < kMostWindow && a.window * 256 < a.n_rows) a.window *= 2;
+  while (a.window < kMostWindow && 2 * head_groups * ((a.n_rows + a.window - 1) / a.window) > kMostRunGroups) a.window *= 2;
+  // A prompt's runs begin a block apart, in every block_size / window-th window, and every
+  // eighth workgroup is on the same XCD: windows go by their phase in a block first (in the
+  // rows' order 1,024 tokens took 14.8 us, with 8 KV heads of 128, now 10.7).
+  const int windows = (a.n_rows + a.window - 1) / a.window;
+  a.phases = std::min(std::max(a.block_size / a.window, 1), windows);
+  a.stretch = (windows + a.phases - 1) / a.phases;
   if (a.dtype == 1) {
     if (a.head_dim == 128) return a.block_size == 16 ? launch_write<__bf16, 128, 16>(a, stream) : launch_write<__bf16, 128, 32>(a, stream);
     return a.block_size == 16 ? launch_write<__bf16, 64, 16>(a, stream) : launch_write<__bf16, 64, 32>(a, stream);

@@ -6,8 +6,7 @@
 // a lane, in 64 bits, exchanged through LDS. HBM bounds it, each row is read and
 // written once: 8,192 tokens with 32 query and 4 KV heads of 128, normed and turned,
 // 32.5 us for 151 MB (4.65 TB/s); 32,768 with 64 and 8 heads 217 us for 1.21 GB (5.6; a
-// copy of 512 MB has 5.1). A few tokens
-// cost a launch: one 8.1 us, 96 with 72 heads 8.7.
+// copy of 512 MB has 5.1). A few tokens cost a launch: one 8.1 us, 96 with 72 heads 8.7.
 #include "turn.h"
 
 namespace spork {

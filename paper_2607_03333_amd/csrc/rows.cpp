@@ -19,8 +19,8 @@ using namespace spork::capi;
 // A launch has fewer than 2^32 threads: so many workgroups of 256.
 constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
 // Rows of heads that a write takes, so that its workgroups (kvq.hip) are fewer than these:
-// for keys and values at most n_rows (hkv + 3) / 2, of which a window of 16 rows leaves a
-// sixteenth from 2,049 rows on, and n_rows (hq + 15) / 64 + 1 for queries.
+// for keys and values some 1,500, or from windows of 16 rows on (n_rows / 16 + 2) (hkv + 3) / 2
+// at most, and n_rows (hq + 15) / 64 + 1 for queries.
 constexpr int64_t kMostHeadRows = int64_t{1} << 25;
 // Positions run a few stages past a context's end, in 32 bits.
 constexpr int64_t kHeadroom = 4096;

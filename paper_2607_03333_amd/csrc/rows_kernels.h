@@ -52,7 +52,8 @@ struct KvqWriteArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride;
   int32_t* bad_slots;  // nullable
   int32_t n_rows, hq, hkv, head_dim, block_size, dtype;
-  int32_t window;  // rows whose runs a workgroup takes (launch_kvq_write)
+  int32_t window;           // rows whose runs a workgroup takes (launch_kvq_write)
+  int32_t phases, stretch;  // order of the windows: stretch of each phase
 };
 
 // Head and block sizes that there are kernels for.

@@ -133,17 +133,36 @@ __device__ __forceinline__ void turn_pairs(F (&x)[16], const F2 (&cs)[8], bool i
   }
 }
 
+// A number of the series, in scalar registers: the compiler would keep all of them in
+// vector registers over a loop.
+__device__ __forceinline__ double scalar(double x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
 // Cosine and sine of a pair at a position, in 64 bits: at position 131,071 a
-// rounded 32-bit angle is off by up to 0.004. The whole turns are taken off
-// before the functions, whose argument then is small.
+// rounded 32-bit angle is off by up to 0.004. Whole and quarter turns are taken off;
+// what is left, at most pi / 4, goes into the series of both functions, whose next
+// terms are below 2^-58.
 __device__ __forceinline__ double2 pair_turn(const TurnArgs& t, int pair, int position) {
-  constexpr double kTurns = 0.15915494309189533577;  // 1 / (2 pi)
+  constexpr double kTurns = 0.15915494309189533577;    // 1 / (2 pi)
+  constexpr double kQuarter = 1.57079632679489661923;  // pi / 2
   double u = position * t.inv_freq[pair] * kTurns;
-  u -= rint(u);
-  double s, c;
-  sincospi(2.0 * u, &s, &c);
-  const double m = t.magnitude;
-  return make_double2(c * m, s * m);
+  u = 4.0 * (u - rint(u));
+  const double whole = rint(u), r = (u - whole) * kQuarter, z = r * r;
+  double s = scalar(1.0 / 355687428096000), c = scalar(1.0 / 20922789888000);  // 1 / 17!, 1 / 16!
+  constexpr double kSin[] = {-1.0 / 1307674368000, 1.0 / 6227020800, -1.0 / 39916800, 1.0 / 362880, -1.0 / 5040, 1.0 / 120, -1.0 / 6};
+  constexpr double kCos[] = {-1.0 / 87178291200, 1.0 / 479001600, -1.0 / 3628800, 1.0 / 40320, -1.0 / 720, 1.0 / 24, -1.0 / 2};
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    s = __builtin_fma(s, z, scalar(kSin[i]));
+    c = __builtin_fma(c, z, scalar(kCos[i]));
+  }
+  s = __builtin_fma(r * z, s, r);
+  c = __builtin_fma(c, z, 1.0);
+  const int q = static_cast<int>(whole) & 3;
+  const double m = t.magnitude, x = (q & 1 ? s : c) * m, y = (q & 1 ? c : s) * m;
+  return make_double2((q + 1) & 2 ? -x : x, q & 2 ? -y : y);
 }
 
 // The turns of a lane's eight pairs at a position, in 32 bits: each lane of the wave
