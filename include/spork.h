@@ -626,8 +626,9 @@ typedef struct spork_kvq {
  * largest magnitude to 448 or less; with tokens in front of them, no less than
  * the scale these have, and where it grows their codes are rounded to it.
  * Values are divided by the scale and rounded to the nearest code, ties to even;
- * infinities and NaN become NaN and don't count for the scale. Keys are normed
- * and rotated in float64 and rounded to their codes once; queries are computed in
+ * infinities and NaN become NaN and don't count for the scale, and so does a key
+ * whose rotation passes 2^128. Keys are normed and rotated in float64 and rounded
+ * to their codes once; queries are computed in
  * float32. Scale bytes of blocks that hold tokens must be ones that this call
  * wrote (27 .. 247; others are taken for the nearest of these). For this and the
  * next two Hq * D must be below 2^30 and Hkv * D * block_size below 2^31, here also
@@ -649,7 +650,8 @@ int spork_kvq_copy_batch(const spork_shape* shape, const spork_kvq* cache, const
  * (spork_chunk_workspace_bytes; calls that share it must not overlap). Codes
  * become bf16 (bf16 queries) or float32 exactly, so the result is that of
  * spork_chunk_attn over pools of these values. NaN codes of positions below
- * kv_len may show in rows that don't attend to them. Two launches. */
+ * kv_len may show in rows that don't attend to them. out must not overlap q
+ * (SPORK_E_INVAL). Two launches. */
 int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, const spork_kvq* cache,
                    const int32_t* table, int32_t max_blocks, const int32_t* row_off,
                    const int32_t* kv_len, int32_t n_seqs, int32_t n_rows, void* out, float* lse,

@@ -303,7 +303,8 @@ int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, co
       return fail(SPORK_E_INVAL, "n_seqs and n_rows must be >= 0, max_blocks positive");
     if (n_seqs == 0 || n_rows == 0) return SPORK_OK;
     if (!table || !row_off || !kv_len || !out) return fail(SPORK_E_INVAL, "NULL pointer");
-    rc = check_rows(Rows{q, q_stride, static_cast<int64_t>(shape->hq) * shape->head_dim}, n_rows, elem_bytes(shape->dtype), "q");
+    const int64_t width = static_cast<int64_t>(shape->hq) * shape->head_dim;
+    rc = check_rows(Rows{q, q_stride, width}, n_rows, elem_bytes(shape->dtype), "q");
     if (rc != SPORK_OK) return rc;
     if (!aligned16(out)) return fail(SPORK_E_INVAL, "out must be 16-byte aligned");
     if (static_cast<int64_t>(max_blocks) * shape->block_size > INT_MAX - kHeadroom)
@@ -314,6 +315,8 @@ int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, co
       return fail(SPORK_E_INVAL, "workspace must be non-NULL and 256-byte aligned");
     if (ws_bytes < spork::chunk_workspace_bytes(shape->head_dim))
       return fail(SPORK_E_CAPACITY, "workspace is smaller than spork_chunk_workspace_bytes");
+    if (rows_meet(Rows{q, q_stride, width}, Rows{out, width, width}, n_rows, elem_bytes(shape->dtype)))
+      return fail(SPORK_E_INVAL, "out must not overlap q");
     spork::ChunkArgs a{};
     a.q = q;
     a.q_stride = q_stride;

@@ -168,6 +168,20 @@ def test_many_rows(dtype, hq, hkv, d, bs, rows):
     do(dtype, hq, hkv, d, bs, [(i, i % bs, 1) for i in range(rows)], "single tokens")
 
 
+@pytest.mark.parametrize("rows", (768, 769, 1600, 6200, 12300))
+@pytest.mark.parametrize("dtype,hq,hkv,d,bs", [(BF16, 2, 1, 64, 16), (F32, 1, 1, 64, 32), (BF16, 9, 9, 64, 16)])
+def test_windows_of_every_width(dtype, hq, hkv, d, bs, rows):
+    """Runs of all lengths one behind the other, in launches whose workgroups take one to sixteen rows."""
+    rng = np.random.default_rng(rows)
+    runs, n = [], 0
+    while n < rows:
+        kept = int(rng.choice((0, 0, 1, bs - 1, rng.integers(0, bs))))
+        m = min(int(rng.choice((1, 2, bs, bs))), bs - kept, rows - n)
+        runs.append((len(runs), kept, m))
+        n += m
+    do(dtype, hq, hkv, d, bs, runs, f"{rows} rows", behind=3)
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,d,bs", SHAPES)
 def test_token_by_token(dtype, hq, hkv, d, bs):
     """A block filled one token at a time, scales growing at some of them, and then begun again."""

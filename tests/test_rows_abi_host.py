@@ -172,6 +172,9 @@ def test_attention_arguments():
         assert spork.lib().spork_chunk_workspace_bytes(shape(), 3, 7, ctypes.byref(b)) == 0
         assert attn(size=b.value - 1) == CAPACITY
     assert attn(size=1000) == CAPACITY
+    row = 32 * 128 * 2
+    for bad in (dict(out=at(0)), dict(out=at(0) + 6 * row), dict(out=at(0) - 6 * row), dict(q_stride=48 * 128, out=at(0) + 32 * 128 * 2)):
+        assert attn(**{**dict(q=at(0)), **bad}) == INVAL and b"overlap" in spork.lib().spork_last_error(), bad
 
 
 def test_plain_frequencies():
