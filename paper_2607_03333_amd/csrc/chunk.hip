@@ -51,7 +51,7 @@ struct Engine;
 // loads are in, and of the next one.
 template <int D, int BS>
 struct RingLoader {
-  using E = StageLayout<D, BS>;
+  using E = StageLayout<D, BS, false>;
   static constexpr bool kCoded = false;
   static constexpr int kRing = 8;  // stages
   static constexpr int kStageLoads = D / 64;
@@ -105,8 +105,8 @@ struct RingLoader {
 };
 
 template <int D, int BS>
-struct Engine<__bf16, D, BS> : StageLayout<D, BS> {
-  using Layout = StageLayout<D, BS>;
+struct Engine<__bf16, D, BS> : StageLayout<D, BS, false> {
+  using Layout = StageLayout<D, BS, false>;
   using Layout::kChunksPerToken;
   using Layout::kHalf;
   using Layout::kswz;

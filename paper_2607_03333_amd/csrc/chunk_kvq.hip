@@ -200,10 +200,10 @@ struct DeepStages {
 // the lower four waves the first stage, the others the second, chunks 64 (w % 4) ..),
 // the first half of them K. A chunk of K is two of the ring's: its first and last
 // eight channels go to chunks 4 (c / 2) + c % 2 and 2 further, the order in which
-// load_q has the queries.
+// load_q has the queries, or the other way round (StageLayout::step).
 template <int D, int BS>
 struct CodeLoader {
-  using E = StageLayout<D, BS>;
+  using E = StageLayout<D, BS, true>;
   static constexpr bool kCoded = true;
   static constexpr int kRing = 6;         // stages of bf16
   static constexpr int kStageLoads = 1;   // (of a stage's place in the period)
@@ -249,7 +249,7 @@ struct CodeLoader {
       const int t = chunk / kPerToken, c = chunk % kPerToken;
       half = uniform(BS == 16 ? t / 16 : 0);
       off = (t % BS) * D + 16 * c;
-      dst = 16u * (t * E::kChunksPerToken + ((4 * (c >> 1) + (c & 1)) ^ E::kswz(t)));
+      dst = 16u * (t * E::kChunksPerToken + ((4 * (c >> 1) + 2 * (D == 128 ? c >> 2 : 0) + (c & 1)) ^ E::kswz(t)));
       other = 32;
     } else {
       const int d = BS == 16 ? chunk % D : chunk >> 1, h = BS == 16 ? chunk / D : chunk & 1;

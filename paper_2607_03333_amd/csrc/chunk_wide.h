@@ -28,15 +28,24 @@ constexpr int kPer = 2;  // stages that a barrier publishes
 // How a stage lies in the ring, in 16-byte chunks. K: chunk t * kChunksPerToken + (c ^
 // kswz(t)) of token t. V: chunk 2d + q of half h (16-token blocks) or 4d + (q ^
 // vswz(d)), tokens 8q .. of channel d. The swizzles spread the lanes of an operand
-// read over the banks.
-template <int D, int BS>
+// read over the banks. CODED: also those of a write of converted codes, which serves
+// eight lanes at a time (lane bit 2 is what would bring two of them together: it
+// decides which of its two chunks a lane writes first).
+template <int D, int BS, bool CODED>
 struct StageLayout {
   static constexpr int kChunksPerToken = D / 8;
   static constexpr int kHalf = 32 * D / 8;  // chunks of K, and of V
   static __device__ __forceinline__ int kswz(int t) {
+    if constexpr (CODED && D == 64) return (t & 1) << 1 | (t >> 1 & 1) | (t & 4);
     return ((t & 7) | ((t >> 1) & 8)) & (kChunksPerToken - 1);
   }
-  static __device__ __forceinline__ int vswz(int d) { return BS == 16 ? (d >> 3) & 1 : (d >> 3) & 3; }
+  static __device__ __forceinline__ int vswz(int d) {
+    const int x = BS == 16 ? (d >> 3) & 1 : (d >> 3) & 3;
+    return CODED ? x ^ (BS == 16 ? (d >> 2) & 1 : (d >> 1) & 1) : x;
+  }
+  // Product of the queries that the scores' product s takes: with codes of 128 channels
+  // the two halves of a 16-channel piece change places from channel 64 on.
+  static constexpr int step(int s) { return CODED && D == 128 && s >= 4 ? s ^ 1 : s; }
   // Zero the elements of an 8-token chunk from position `first` on that lie at or
   // past `end`.
   static __device__ __forceinline__ u32x4 zero_past(u32x4 w, int first, int end) {
@@ -53,7 +62,7 @@ struct StageLayout {
 template <int D, int BS, typename Loader, typename Rows>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, const Pages& pg, uint4 (*smem)[D * 8], int lane,
                                           int wave, Rows& e) {
-  using E = StageLayout<D, BS>;
+  using E = StageLayout<D, BS, Loader::kCoded>;
   constexpr int kRing = Loader::kRing, kAhead = kRing - kPer, kStageLoads = Loader::kStageLoads;
   constexpr int NP = D / 16;     // products of the scores, and of P.V: a slot each
   constexpr int NCt = D / 32;
@@ -108,7 +117,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& w, con
       } else {
         acc = sc;
       }
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[s]), e.q[s], acc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[s]), e.q[E::step(s)], acc, 0, 0, 0);
     };
     auto pv_product = [&](int i, const State& x) __attribute__((always_inline)) {
       const int h = 4 * (i / NCt), ct = i % NCt;
