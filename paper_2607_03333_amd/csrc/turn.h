@@ -176,7 +176,7 @@ __device__ __forceinline__ void lane_turns(const TurnArgs& t, int position, floa
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) cs[j] = table[(8 * c + j) & 63];
+  for (int j = 0; j < 8; ++j) cs[j] = table[8 * c + j];
 }
 
 }  // namespace
