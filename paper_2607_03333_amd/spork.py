@@ -204,11 +204,11 @@ def _ptr(x):
     return x.data_ptr()
 
 
-_raw_stream = None
+_raw_stream = _raw_stream_at = None
 
 
 def _stream(stream):
-    global _raw_stream
+    global _raw_stream, _raw_stream_at
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     if _raw_stream is None:
@@ -216,7 +216,13 @@ def _stream(stream):
         torch.cuda.current_stream()  # (initialises the GPU, or says why it can't)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object: 0.5 us against 2.9
         _raw_stream = (lambda: raw(torch.cuda.current_device())) if raw else lambda: torch.cuda.current_stream().cuda_stream
+        _raw_stream_at = raw
     return _raw_stream()
+
+
+def _stream_at(stream, here):
+    """_stream where the current device is known."""
+    return _raw_stream_at(here) if stream is None and _raw_stream_at is not None else _stream(stream)
 
 
 def _i32(a):
@@ -625,7 +631,7 @@ def _heads(name, x, shape, types):
 
 
 def _here(first, *tensors):
-    """_on_gpu for tensors alone (None passes, but for the first), without a branch for each kind."""
+    """_on_gpu for tensors alone (None passes, but for the first), without a branch for each kind: the current device."""
     global _torch
     here = first.get_device()
     if here < 0:
@@ -638,6 +644,7 @@ def _here(first, *tensors):
     for x in tensors:
         if x is not None and x.get_device() != here:
             _on_gpu(x)
+    return here
 
 
 def _turn(shape, rope, norm, types):
@@ -658,8 +665,8 @@ def spork_qk_rope(shape, rope, norm, positions, q, k, q_out, k_out, stream=None)
     rope_ref, norm_ref, tensors = _turn(shape, rope, norm, types)
     args = (_want("positions", positions, 4, n), n, *_heads("q", q, of_q, types), *_heads("k", k, of_k, types),
             *_heads("q_out", q_out, of_q, types), *_heads("k_out", k_out, of_k, types))
-    _here(k if q is None else q, k, q_out, k_out, positions, *tensors)
-    _check(lib().spork_qk_rope(ctypes.byref(shape), rope_ref, norm_ref, *args, _stream(stream)))
+    here = _here(k if q is None else q, k, q_out, k_out, positions, *tensors)
+    _check(lib().spork_qk_rope(ctypes.byref(shape), rope_ref, norm_ref, *args, _stream_at(stream, here)))
 
 
 def _check_kvq(shape, cache):
@@ -677,16 +684,16 @@ def spork_kvq_write(shape, cache, rope, norm, slots, positions, q, k, v, q_out, 
     args = (_want("slots", slots, 8, n), _want("positions", positions, 4, n), n, *_heads("q", q, of_q, types),
             *_heads("k", k, of_k, types), *_heads("v", v, of_k, types), *_heads("q_out", q_out, of_q, types),
             _want("bad_slots", bad_slots, 4, 1))
-    _here(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
-    _check(lib().spork_kvq_write(ctypes.byref(shape), cache.ref, rope_ref, norm_ref, *args, _stream(stream)))
+    here = _here(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
+    _check(lib().spork_kvq_write(ctypes.byref(shape), cache.ref, rope_ref, norm_ref, *args, _stream_at(stream, here)))
 
 
 def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
     most = copies.shape[0]
     _check_kvq(shape, cache)
     args = (_want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1), most)
-    _here(*cache.tensors, copies, n_copies)
-    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), cache.ref, *args, _stream(stream)))
+    here = _here(*cache.tensors, copies, n_copies)
+    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), cache.ref, *args, _stream_at(stream, here)))
 
 
 def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace, stream=None):
@@ -700,9 +707,9 @@ def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace,
         raise ValueError("out must be [rows, hq, head_dim] of the shape's dtype")
     if lse is not None and (lse.shape != of_q[:2] or lse.dtype not in _types(SPORK_DTYPE_F32)):
         raise ValueError("lse must be [rows, hq] float32")
-    _here(*cache.tensors, q, table, row_off, kv_len, out, lse, workspace)
+    here = _here(*cache.tensors, q, table, row_off, kv_len, out, lse, workspace)
     _check(lib().spork_kvq_attn(ctypes.byref(shape), *args, _ptr(out), _ptr(lse), _ptr(workspace), _bytes(workspace),
-                                _stream(stream)))
+                                _stream_at(stream, here)))
 
 
 # ---- measurement aid --------------------------------------------------------
