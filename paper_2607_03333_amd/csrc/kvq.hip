@@ -377,7 +377,7 @@ __device__ __forceinline__ void write_queries(const KvqWriteArgs& a, int64_t num
       float w[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) w[i] = weight[i / 8].get(i % 8);
-      norm_head<D>(x, w, static_cast<float>(a.turn.eps));
+      norm_head<D>(x, w, a.turn.eps);
     }
     if (at.turns) {
       if (a.turn.interleaved) turn_pairs(x, cs, true);
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(64 * kWriteWaves) kvq_write_kernel(KvqWriteArg
   const int head_groups = (a.hkv + kWriteWaves - 1) / kWriteWaves;
   const int64_t groups = static_cast<int64_t>(a.phases) * a.stretch * head_groups;  // of keys, and of values
   const int64_t group = blockIdx.x;
-  if (group >= 2 * groups) {
+  if (kTurn && group >= 2 * groups) {  // (there are none without)
     write_queries<T, D>(a, static_cast<int64_t>(a.pools.num_blocks) * BS, (group - 2 * groups) * kWriteWaves + wave,
                         reinterpret_cast<float2*>(memory) + 64 * wave, lane);
     return;

@@ -5,7 +5,7 @@
 // many heads take as long). They are loaded before the angles are computed: one pair
 // a lane, in 64 bits, exchanged through LDS. HBM bounds it, each row is read and
 // written once: 8,192 tokens with 32 query and 4 KV heads of 128, normed and turned,
-// 32.5 us for 151 MB (4.65 TB/s); 32,768 with 64 and 8 heads 217 us for 1.21 GB (5.6; a
+// 31.1 us for 151 MB (4.85 TB/s); 32,768 with 64 and 8 heads 211 us for 1.21 GB (5.7; a
 // copy of 512 MB has 5.1). A few tokens cost a launch: one 8.1 us, 96 with 72 heads 8.7.
 #include "turn.h"
 
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(64 * kRopeWaves) qk_rope_kernel(RopeArgs a, in
     float w[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) w[i] = wr[i / 8].get(i % 8);
-    norm_head<D>(x, w, static_cast<float>(a.turn.eps));
+    norm_head<D>(x, w, a.turn.eps);
   }
   if (at.turns) {
     if (a.turn.interleaved) turn_pairs(x, cs, true);

@@ -93,25 +93,49 @@ __device__ __forceinline__ double lane_xor(double x) {
   return __builtin_bit_cast(double, static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo));
 }
 
-__device__ __forceinline__ float inv_sqrt(float x) { return 1.0f / sqrtf(x); }
-__device__ __forceinline__ double inv_sqrt(double x) { return 1.0 / sqrt(x); }
-
-// 1 / sqrt(mean(x^2) + eps) of a head, from the lane's sum of squares.
+// The sum over a head's lanes.
 template <int D, typename F>
-__device__ __forceinline__ F norm_factor(F s, F eps) {
+__device__ __forceinline__ F head_sum(F s) {
   s += lane_xor<1>(s);
   s += lane_xor<2>(s);
   if constexpr (D == 128) s += lane_xor<4>(s);
-  return inv_sqrt(s * (F(1) / D) + eps);
+  return s;
 }
 
-// The head's norm, in F: w holds the lane's weights.
-template <int D, typename F>
-__device__ __forceinline__ void norm_head(F (&x)[16], const F (&w)[16], F eps) {
-  F s = 0;
+// 1 / sqrt(mean(x^2) + eps) of a head, from the lane's sum of squares.
+template <int D>
+__device__ __forceinline__ double norm_factor(double s, double eps) {
+  return 1.0 / sqrt(head_sum<D>(s) * (1.0 / D) + eps);
+}
+
+// The head's norm, in 32 bits: w holds the lane's weights. Where the sum of squares is so
+// small or large that some of them may be lost, the head is scaled by a power of two first.
+// (8,192 tokens take 31.1 us so, 35.4 in 64 bits for all heads, 34.5 with 64 bits there.)
+template <int D>
+__device__ __forceinline__ void norm_head(float (&x)[16], const float (&w)[16], double eps) {
+  float s = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s += x[i] * x[i];
-  const F r = norm_factor<D>(s, eps);
+  s = head_sum<D>(s);
+  float r = 1.0f / sqrtf(s * (1.0f / D) + static_cast<float>(eps));
+  const bool safe = s >= 0x1p-80f && s <= 0x1p120f;
+  if (__builtin_expect(__ballot(!safe) != 0, 0)) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = fmaxf(top, lane_xor<1>(top));
+    top = fmaxf(top, lane_xor<2>(top));
+    if constexpr (D == 128) top = fmaxf(top, lane_xor<4>(top));
+    const int e = safe || top == 0.0f ? 0 : static_cast<int>(__float_as_uint(top) >> 23) - 126;
+    float t = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = ldexpf(x[i], -e);
+      t += x[i] * x[i];
+    }
+    const double mean = head_sum<D>(t) * (1.0 / D);
+    if (!safe) r = static_cast<float>(1.0 / sqrt(mean + ldexp(eps, -2 * e)));
+  }
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
 }

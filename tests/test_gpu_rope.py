@@ -137,6 +137,29 @@ def test_outputs_side_by_side_in_wider_rows():
     assert (wide[:, :64] == 7.5).all() and (wide[:, 11 * 64:] == 7.5).all()
 
 
+@pytest.mark.parametrize("eps", (0.0, 1e-50, 1e-6))
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_norms_of_very_small_and_very_large_heads(dtype, d, eps):
+    """Squares that 32 bits don't hold, beside heads whose squares they do, and heads that hold both. (Factor and products in
+    64 bits: well inside the bound of 32.)"""
+    tops = [1e-44 if dtype == F32 else 1e-39, 1e-38, 1e-30, 3e-20, 1e-13, 2e-12, 1.0, 1e12, 5e17, 1e19, 1e30, 2e38]
+    c = Case(dtype, 4, 2, d, len(tops), d, gain=0.3)
+    for i, top in enumerate(tops):
+        c.rows[i, :2 * d] = (c.rows[i, :2 * d].double().clamp(-1, 1) * top).to(dtype)
+        c.rows[i, 4 * d:5 * d] = (c.rows[i, 4 * d:5 * d].double().clamp(-1, 1) * top).to(dtype)
+        c.rows[i, 2 * d + 5] = top
+    # (a head of zeros has no norm without eps)
+    for x, w in zip((c.q, c.k), c.weights):
+        assert (x.double().abs().amax(-1) > 0).all() and w is not None
+    norm = spork.make_qk_norm(*c.weights, eps)
+    ref = []
+    for x, w in ((c.q, c.weights[0]), (c.k, c.weights[1])):
+        want, size = turned(to_f64(x), to_f64(w), eps, c.pos, c.inv_freq, 1.0, False)
+        ref.append((want, turn_bound(want, size, d, dtype == BF16)))
+    spork.spork_qk_rope(c.shape, c.rope, norm, c.positions, c.q, c.k, c.q_out, c.k_out)
+    c.check(f"eps {eps}", ref)
+
+
 def test_zero_rows_infinities_and_nan():
     """A row of zeros has a norm by eps alone; a head that holds an infinity or a NaN spoils itself and no other."""
     c = Case(BF16, 4, 2, 128, 3, 128)
