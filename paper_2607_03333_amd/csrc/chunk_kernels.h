@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstddef>
 #include <cstdint>
 
@@ -11,6 +12,17 @@ namespace spork {
 
 constexpr int kChunkSlices = 256;    // workgroups of the attention launch: one per compute unit
 constexpr int kChunkTileRows = 256;  // packed rows (query row x head of a KV head's group) of a tile
+constexpr int kChunkWaves = 8;       // of a workgroup: a unit (a KV head and a row tile of 32 packed rows) each
+
+// KV heads that a tile of so many row tiles takes together, `most` (a power of two) in its
+// batch. Tiles of more than NARROW row tiles, whose waves share their stages, are of one head.
+template <int NARROW>
+constexpr int chunk_heads(int most, int row_tiles) {
+  if constexpr (2 * (NARROW + 1) <= kChunkWaves) {  // (else the waves don't suffice for a second head)
+    if (row_tiles > NARROW) return 1;
+  }
+  return std::min(most, kChunkWaves / row_tiles);
+}
 
 // A tile whose tokens are split over slices `first` .. `last`, as the slice
 // that holds its first token notes it for the merge; n_rows 0: none.

@@ -365,7 +365,14 @@ struct CodeEngine<__bf16, D, BS, WIDE> {
   static constexpr bool kWide = WIDE;
   // Row tiles of a tile that isn't wide: 16 sequences of 9 rows over 8,000 positions, 64
   // heads in groups of 8 (three row tiles) 111 us with stages of each wave's own, 98 with
-  // shared ones; in groups of 4 (two) 74 and 88.
+  // shared ones; in groups of 4 (two) 74 and 88. Wide tiles are of one KV head; where the
+  // batch has tiles enough for two heads each (chunk_tile_heads), tiles of three and four
+  // row tiles could take them instead, with stages of each wave's own. With one wide and with
+  // two, us: 64 such sequences 330 and 380 (two heads a tile at most), 128 over 4,000 341 and
+  // 385 (four); 64 verify rows of 9 beside 128 tokens over 8,000, 32 heads in groups of 8, 379
+  // and 386; 192 forks of 8 to 50 rows 342 and 433; 128 chunks of 32 rows over 3,000, groups
+  // of 4, 309 and 319; 64 of 96 rows over 2,000, 16 heads of 64, 129 and 143. Short contexts
+  // alone lose: 128 of 16 rows over 100 58 and 38, 64 of 128 rows over 200 47 and 38.
   static constexpr int kNarrowTiles = 2;
   static constexpr int kD = D, kBlock = BS;
   static constexpr int kTokens = 32;             // of a stage

@@ -35,7 +35,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
-constexpr int kWaves = 8;
+constexpr int kWaves = kChunkWaves;
 constexpr int kDies = 8;
 // Cache policy of keys and values: non-temporal where one wave reads them, kept
 // where several row tiles do (24 prompts of up to 777 tokens with 16 heads of 64
@@ -112,7 +112,7 @@ __device__ __forceinline__ SeqOf<E::kTile> seq_of(const ChunkArgs& a, int off, i
   s.per = a.tile_rows;
   s.tiles = s.rows <= s.per ? s.rows > 0 : (s.rows + s.per - 1) / s.per;
   const int row_tiles = (min(s.rows, s.per) * a.group + 31) / 32;
-  s.heads = s.tiles == 1 ? min(a.most_heads, kWaves / row_tiles) : 1;
+  s.heads = s.tiles == 1 ? chunk_heads<E::kNarrowTiles>(a.most_heads, row_tiles) : 1;
   s.groups = (a.hkv + s.heads - 1) / s.heads;
   s.cost = E::token_cost(a, row_tiles, s.heads);
   s.group_cost = s.tiles <= 1 ? s.tiles * s.tile_cost(0) : s.first(s.tiles);
@@ -360,6 +360,7 @@ __global__ void __launch_bounds__(64 * kWaves, 1) chunk_attn_kernel(ChunkArgs a)
   __shared__ int64_t wave_sum[kWaves];
   __shared__ Start start;
   static_assert(E::kSlot >= kFloat4s * 64, "a wave's slot holds its accumulator");
+  static_assert(!kWide || chunk_heads<E::kNarrowTiles>(kWaves, E::kNarrowTiles + 1) == 1, "waves that share stages are of one KV head");
   const int tid = threadIdx.x, wave = uniform(tid >> 6);
   const int group = a.group;  // query heads of a KV head
   const int per_die = kChunkSlices / kDies;
