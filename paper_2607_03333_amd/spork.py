@@ -575,7 +575,6 @@ def make_rope(inv_freq, layout=SPORK_ROPE_HALF, magnitude=1.0):
         raise ValueError("inv_freq must be a contiguous float64 tensor of one dimension")
     r = spork_rope(2 * inv_freq.shape[0], layout, magnitude, inv_freq.data_ptr())
     r.tensors = (inv_freq,)
-    r.ref = ctypes.byref(r)
     return r
 
 
@@ -585,7 +584,6 @@ def make_qk_norm(q_weight, k_weight, eps):
         raise ValueError("the norms' weights must be contiguous tensors of one dimension")
     n = spork_qk_norm(_ptr(q_weight), _ptr(k_weight), eps)
     n.tensors = tuple(w for w in (q_weight, k_weight) if w is not None)
-    n.ref = ctypes.byref(n)
     return n
 
 
@@ -606,7 +604,6 @@ def make_kvq(k_codes, v_codes, k_scale, v_scale):
     c = spork_kvq(blocks, k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
     c.tensors = (k_codes, v_codes, k_scale, v_scale)
     c.blocks_of = (hkv, bs, d)
-    c.ref = ctypes.byref(c)
     return c
 
 
@@ -648,13 +645,13 @@ def _here(first, *tensors):
 
 
 def _turn(shape, rope, norm, types):
-    """References to rope and norm for a call (None passes), and their tensors."""
+    """The tensors of rope and norm (None passes)."""
     if norm is None:
-        return (None, None, ()) if rope is None else (rope.ref, None, rope.tensors)
+        return () if rope is None else rope.tensors
     for w in norm.tensors:
         if w.shape[0] != shape.head_dim or w.dtype not in types:
             raise ValueError("the norms' weights must have head_dim elements of the shape's dtype")
-    return (None, norm.ref, norm.tensors) if rope is None else (rope.ref, norm.ref, rope.tensors + norm.tensors)
+    return norm.tensors if rope is None else rope.tensors + norm.tensors
 
 
 def spork_qk_rope(shape, rope, norm, positions, q, k, q_out, k_out, stream=None):
@@ -662,11 +659,11 @@ def spork_qk_rope(shape, rope, norm, positions, q, k, q_out, k_out, stream=None)
     rows, and so may the outputs; q_out may be q, k_out k."""
     n, d, types = (k if q is None else q).shape[0], shape.head_dim, _types(shape.dtype)
     of_q, of_k = (n, shape.hq, d), (n, shape.hkv, d)
-    rope_ref, norm_ref, tensors = _turn(shape, rope, norm, types)
+    tensors = _turn(shape, rope, norm, types)
     args = (_want("positions", positions, 4, n), n, *_heads("q", q, of_q, types), *_heads("k", k, of_k, types),
             *_heads("q_out", q_out, of_q, types), *_heads("k_out", k_out, of_k, types))
     here = _here(k if q is None else q, k, q_out, k_out, positions, *tensors)
-    _check(lib().spork_qk_rope(ctypes.byref(shape), rope_ref, norm_ref, *args, _stream_at(stream, here)))
+    _check(lib().spork_qk_rope(ctypes.byref(shape), rope, norm, *args, _stream_at(stream, here)))
 
 
 def _check_kvq(shape, cache):
@@ -680,12 +677,12 @@ def spork_kvq_write(shape, cache, rope, norm, slots, positions, q, k, v, q_out, 
     n, d, types = slots.shape[0], shape.head_dim, _types(shape.dtype)
     of_q, of_k = (n, shape.hq, d), (n, shape.hkv, d)
     _check_kvq(shape, cache)
-    rope_ref, norm_ref, tensors = _turn(shape, rope, norm, types)
+    tensors = _turn(shape, rope, norm, types)
     args = (_want("slots", slots, 8, n), _want("positions", positions, 4, n), n, *_heads("q", q, of_q, types),
             *_heads("k", k, of_k, types), *_heads("v", v, of_k, types), *_heads("q_out", q_out, of_q, types),
             _want("bad_slots", bad_slots, 4, 1))
     here = _here(*cache.tensors, slots, positions, q, k, v, q_out, bad_slots, *tensors)
-    _check(lib().spork_kvq_write(ctypes.byref(shape), cache.ref, rope_ref, norm_ref, *args, _stream_at(stream, here)))
+    _check(lib().spork_kvq_write(ctypes.byref(shape), cache, rope, norm, *args, _stream_at(stream, here)))
 
 
 def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
@@ -693,7 +690,7 @@ def spork_kvq_copy_batch(shape, cache, copies, n_copies, stream=None):
     _check_kvq(shape, cache)
     args = (_want("copies", copies, 4, most, 3), _want("n_copies", n_copies, 4, 1), most)
     here = _here(*cache.tensors, copies, n_copies)
-    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), cache.ref, *args, _stream_at(stream, here)))
+    _check(lib().spork_kvq_copy_batch(ctypes.byref(shape), cache, *args, _stream_at(stream, here)))
 
 
 def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace, stream=None):
@@ -701,7 +698,7 @@ def spork_kvq_attn(shape, q, cache, table, row_off, kv_len, out, lse, workspace,
     n_rows, (n_seqs, max_blocks) = q.shape[0], table.shape
     _check_kvq(shape, cache)
     types, of_q = _types(shape.dtype), (n_rows, shape.hq, shape.head_dim)
-    args = (*_heads("q", q, of_q, types), cache.ref, _want("table", table, 4, n_seqs, max_blocks), max_blocks,
+    args = (*_heads("q", q, of_q, types), cache, _want("table", table, 4, n_seqs, max_blocks), max_blocks,
             _want("row_off", row_off, 4, n_seqs + 1), _want("kv_len", kv_len, 4, n_seqs), n_seqs, n_rows)
     if out.shape != of_q or out.dtype not in types:
         raise ValueError("out must be [rows, hq, head_dim] of the shape's dtype")
