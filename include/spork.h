@@ -549,7 +549,7 @@ typedef struct spork_rope {
 typedef struct spork_qk_norm {
   const void* q_weight;
   const void* k_weight;
-  double eps; /* finite, >= 0 */
+  double eps; /* 0 .. 2^100 */
 } spork_qk_norm;
 
 /* How frequencies are scaled for contexts longer than the one trained on.
@@ -585,9 +585,11 @@ int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_sca
  * [Hkv][D], k_stride), q_out, k_out likewise; k and k_out, or q and q_out, may be
  * NULL. Rows 16-byte aligned: the parts of a fused projection's rows will do.
  * q_out may be q, and k_out k, at the same stride; else outputs must not overlap
- * each other or the inputs (SPORK_E_INVAL). bf16 rows: computed in float32 (a
- * head whose squares that doesn't hold is scaled first), rounded once. Hq * D must be below 2^30 and n_rows * ((Hq + Hkv + 7) / 8) below
- * 2^26 - 4 (SPORK_E_UNSUPPORTED). One launch. */
+ * each other or the inputs (SPORK_E_INVAL). Computed in float32 (a head whose
+ * squares that doesn't hold is scaled first; a channel that its head's root brings
+ * below 2^-126 keeps what float32 holds there), rounded to bf16 rows once.
+ * Hq * D must be below 2^30 and n_rows * ((Hq + Hkv + 7) / 8) below 2^26 - 4
+ * (SPORK_E_UNSUPPORTED). One launch. */
 int spork_qk_rope(const spork_shape* shape, const spork_rope* rope, const spork_qk_norm* norm,
                   const int32_t* positions, int32_t n_rows, const void* q, int64_t q_stride,
                   const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,

@@ -22,6 +22,8 @@ constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
 // for keys and values some 1,500, or from windows of 16 rows on (n_rows / 16 + 2) (hkv + 3) / 2
 // at most, and n_rows (hq + 15) / 64 + 1 for queries.
 constexpr int64_t kMostHeadRows = int64_t{1} << 25;
+// Of norms: far past any use, and where factors in 32 bits are exact enough (norm_head, turn.h).
+constexpr double kMostEps = 0x1p100;
 // Positions run a few stages past a context's end, in 32 bits.
 constexpr int64_t kHeadroom = 4096;
 
@@ -71,7 +73,7 @@ int check_turn(const spork_shape* shape, const spork_rope* rope, const spork_qk_
       return fail(SPORK_E_INVAL, "a norm's weight is NULL");
     if ((with_q && !aligned16(norm->q_weight)) || (with_k && !aligned16(norm->k_weight)))
       return fail(SPORK_E_INVAL, "the norms' weights must be 16-byte aligned");
-    if (!std::isfinite(norm->eps) || norm->eps < 0) return fail(SPORK_E_INVAL, "eps must be finite and >= 0");
+    if (!(norm->eps >= 0 && norm->eps <= kMostEps)) return fail(SPORK_E_INVAL, "eps must be from 0 to 2^100");
   }
   return SPORK_OK;
 }

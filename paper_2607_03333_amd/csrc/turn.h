@@ -108,17 +108,21 @@ __device__ __forceinline__ double norm_factor(double s, double eps) {
   return 1.0 / sqrt(head_sum<D>(s) * (1.0 / D) + eps);
 }
 
-// The head's norm, in 32 bits: w holds the lane's weights. Where the sum of squares is so
-// small or large that some of them may be lost, the head is scaled by a power of two first.
-// (8,192 tokens take 31.1 us so, 35.4 in 64 bits for all heads, 34.5 with 64 bits there.)
+// The head's norm, in 32 bits: w holds the lane's weights. Where some of the squares may be
+// lost (their sum is past 2^120, or so small that they and eps, which is at most 2^100,
+// count), the head is scaled by a power of two first. A channel times the factor is at most
+// sqrt(D), and then comes its weight: factor times weight may lie outside of 2^-126 .. 2^128
+// where the result does not. (8,192 tokens take 31.1 us so, 35.4 in 64 bits for all heads,
+// 34.5 with 64 bits there.)
 template <int D>
 __device__ __forceinline__ void norm_head(float (&x)[16], const float (&w)[16], double eps) {
   float s = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s += x[i] * x[i];
   s = head_sum<D>(s);
-  float r = 1.0f / sqrtf(s * (1.0f / D) + static_cast<float>(eps));
-  const bool safe = s >= 0x1p-80f && s <= 0x1p120f;
+  const float mean = s * (1.0f / D) + static_cast<float>(eps);
+  float r = 1.0f / sqrtf(mean);
+  const bool safe = mean >= 0x1p-87f && s <= 0x1p120f;
   if (__builtin_expect(__ballot(!safe) != 0, 0)) {
     float top = 0.0f;
 #pragma unroll
@@ -133,11 +137,12 @@ __device__ __forceinline__ void norm_head(float (&x)[16], const float (&w)[16], 
       x[i] = ldexpf(x[i], -e);
       t += x[i] * x[i];
     }
-    const double mean = head_sum<D>(t) * (1.0 / D);
-    if (!safe) r = static_cast<float>(1.0 / sqrt(mean + ldexp(eps, -2 * e)));
+    const double scaled = head_sum<D>(t) * (1.0 / D) + ldexp(eps, -2 * e);
+    // (a head of zeros stays one under any eps but 0, however small)
+    if (!safe) r = top == 0.0f && eps > 0.0 ? 1.0f : static_cast<float>(1.0 / sqrt(scaled));
   }
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+  for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
 }
 
 // The lane's eight pairs, by their cosines and sines (the magnitude is in them).
