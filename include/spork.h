@@ -539,7 +539,7 @@ int spork_chunk_attn(const spork_shape* shape, const void* q, int64_t q_stride, 
 typedef struct spork_rope {
   int32_t rotary_dim;     /* a multiple of 16, 16 .. head_dim */
   int32_t layout;         /* SPORK_ROPE_* */
-  double magnitude;       /* 1, unless a scaling asks for another */
+  double magnitude;       /* 1, unless a scaling asks for another; 0 or in float32's normal range */
   const double* inv_freq; /* device [rotary_dim / 2] radians per position, 16-byte aligned */
 } spork_rope;
 

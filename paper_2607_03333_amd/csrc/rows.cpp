@@ -64,7 +64,8 @@ int check_turn(const spork_shape* shape, const spork_rope* rope, const spork_qk_
       return fail(SPORK_E_UNSUPPORTED, "rotary_dim must be a multiple of 16 from 16 to head_dim");
     if (rope->layout != SPORK_ROPE_HALF && rope->layout != SPORK_ROPE_INTERLEAVED)
       return fail(SPORK_E_INVAL, "layout must be SPORK_ROPE_HALF or SPORK_ROPE_INTERLEAVED");
-    if (!std::isfinite(rope->magnitude)) return fail(SPORK_E_INVAL, "magnitude must be finite");
+    const double m = std::abs(rope->magnitude);  // (cosines and sines times it are kept in 32 bits)
+    if (m != 0 && !(m >= FLT_MIN && m <= FLT_MAX)) return fail(SPORK_E_INVAL, "magnitude must be 0 or in float32's normal range");
     if (rope->inv_freq == nullptr || !aligned16(rope->inv_freq))
       return fail(SPORK_E_INVAL, "inv_freq must be non-NULL and 16-byte aligned");
   }

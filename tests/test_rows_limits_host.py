@@ -5,7 +5,7 @@ import math
 import pytest
 
 from paper_2607_03333_amd import spork
-from test_rows_abi_host import INVAL, norm, turn, write
+from test_rows_abi_host import INVAL, norm, rope, turn, write
 
 
 def why(call, **kw):
@@ -20,3 +20,13 @@ def test_eps_up_to_2_100(call):
         assert b"eps" in why(call, norm=norm(eps=eps)), eps
     for eps in (0.0, 5e-324, 1e-6, 2.0 ** 100):
         assert b"positions" in why(call, norm=norm(eps=eps)), eps
+
+
+@pytest.mark.parametrize("call", (turn, write))
+def test_magnitudes_that_32_bits_hold(call):
+    """Cosines and sines are multiplied by the magnitude and kept in 32 bits: past them they would be infinities, below
+    them lose their places."""
+    for m in (3.5e38, -3.5e38, 1e300, -math.inf, math.nan, 1.1e-38, -1e-45, 5e-324):
+        assert b"magnitude" in why(call, rope=rope(magnitude=m)), m
+    for m in (0.0, 1.0, -0.5, 3.4e38, -3.4e38, 1.2e-38, -1.2e-38):
+        assert b"positions" in why(call, rope=rope(magnitude=m)), m
