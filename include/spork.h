@@ -651,9 +651,10 @@ int spork_kvq_copy_batch(const spork_shape* shape, const spork_kvq* cache, const
  * masks and empty rows, q and out of the shape's dtype, and the same workspace
  * (spork_chunk_workspace_bytes; calls that share it must not overlap). Codes
  * become bf16 (bf16 queries) or float32 exactly, so the result is that of
- * spork_chunk_attn over pools of these values. NaN codes of positions below
- * kv_len may show in rows that don't attend to them. out must not overlap q
- * (SPORK_E_INVAL). Two launches. */
+ * spork_chunk_attn over pools of these values; those that stand for 2^128 (what
+ * values of 248 * 2^120 and more are rounded to) become infinities. NaN codes and
+ * infinities of positions below kv_len may show in rows that don't attend to them.
+ * out must not overlap q (SPORK_E_INVAL). Two launches. */
 int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, const spork_kvq* cache,
                    const int32_t* table, int32_t max_blocks, const int32_t* row_off,
                    const int32_t* kv_len, int32_t n_seqs, int32_t n_rows, void* out, float* lse,
