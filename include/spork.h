@@ -651,8 +651,9 @@ int spork_kvq_copy_batch(const spork_shape* shape, const spork_kvq* cache, const
  * masks and empty rows, q and out of the shape's dtype, and the same workspace
  * (spork_chunk_workspace_bytes; calls that share it must not overlap). Codes
  * become bf16 (bf16 queries) or float32 exactly, so the result is that of
- * spork_chunk_attn over pools of these values; those that stand for 2^128 (what
- * values of 248 * 2^120 and more are rounded to) become infinities. NaN codes and
+ * spork_chunk_attn over pools of these values, probabilities rounded to bf16 for
+ * bf16 queries among it; codes that stand for 2^128 (what values of 248 * 2^120
+ * and more are rounded to) become infinities. NaN codes and
  * infinities of positions below kv_len may show in rows that don't attend to them.
  * out must not overlap q (SPORK_E_INVAL). Two launches. */
 int spork_kvq_attn(const spork_shape* shape, const void* q, int64_t q_stride, const spork_kvq* cache,

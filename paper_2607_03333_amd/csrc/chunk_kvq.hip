@@ -22,6 +22,12 @@
 // one it computes), as many bytes as they have. The blocks' entries and scales come 64 at a
 // time, a window ahead, into registers: loads beside the stages' would be counted
 // with them at every wait.
+//
+// Probabilities enter the second product in the queries' type (bf16: rounded to
+// nearest, at most 2^-8 of each, for the matrix instructions' rate; the row sum is of the
+// unrounded ones): outputs of bf16 queries are 0.0020 to 0.0023 (root mean square, of the
+// outputs') from those of 64 bits, where their own rounding makes 0.0017. Sums, reference
+// and accumulators are fp32.
 #include "chunk_wide.h"
 
 namespace spork {

@@ -1,6 +1,7 @@
 // Tiles of many row tiles: a workgroup's waves, each with a row tile of its own,
-// share the stages of keys and values, bf16 in LDS. How the stages come there is the
-// including file's (a Loader).
+// share the stages of keys and values, bf16 in LDS. So all of them are of one KV head
+// (chunk_heads, chunk_kernels.h). How the stages come there is the including file's (a
+// Loader).
 #pragma once
 #include "chunk_tiles.h"
 
@@ -8,10 +9,11 @@ namespace spork {
 namespace {
 
 // --------------------------------------------------------------------------
-// The wide path: bf16 tiles of more than 128 packed rows. Each wave owns one row
-// tile of 32 and all of them share every 32-token stage (16 KB for 128 channels),
-// which goes through a ring of eight in LDS; a barrier publishes two stages at a
-// time and frees the two that were read. The matrix cores bound a stage (D / 8
+// The wide path: tiles of bf16 queries with more row tiles than an engine's
+// kNarrowTiles (four over bf16 pools, two over codes). Each wave owns one row tile of 32
+// and all of them share every 32-token stage (16 KB for 128 channels), which goes
+// through a ring in LDS (Loader::kRing, eight stages, or six of converted codes); a
+// barrier publishes two stages at a time and frees the two that were read. The matrix cores bound a stage (D / 8
 // 32x32x16 products per wave, 32 cycles each, two waves to a SIMD), so beside the
 // softmax of stage s run the P.V products of stage s - 1 and the scores of stage
 // s + 1, one product and a few vector instructions at a time; operand reads are
@@ -56,7 +58,8 @@ struct StageLayout {
   }
 };
 
-// Every wave of the workgroup runs this for the same tile; on return e holds the
+// Every wave of the workgroup runs this for the same tile, w.head the same in all of
+// them: each loads a part of its keys and values for all; on return e holds the
 // wave's row tile (nothing where wave * 32 >= n_packed), and its rows' loads are
 // done. Loader: how stages come into the ring.
 template <int D, int BS, typename Loader, typename Rows>

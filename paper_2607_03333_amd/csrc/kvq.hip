@@ -23,8 +23,12 @@
 // query and 8 KV heads of 128, normed and turned, 92 MB, takes 22.8 us (4.05 TB/s; a
 // large copy has 5.1, which would be 18). The keys' arithmetic in 64 bits and their two
 // barriers a run go beside the queries' rows, two thirds of the bytes; registers
-// decide how many workgroups do (166 of them 24.4 us, 125 22.8). A step of few tokens
-// costs a launch and the waits for slots, rows and old codes: 96 tokens 9.9 us.
+// decide how many workgroups do (166 of them 24.4 us, 125 22.8; 101 with heads of 64, and
+// 161 and 125 in blocks of 32, where the prompt takes 3% longer; fp32 rows 129 to 213;
+// keys that come ready 64 to 125). A step of few tokens costs a launch and the waits for
+// slots, rows and old codes: 96 tokens 9.9 us. With fewer than four KV heads the waves of
+// keys and values that have none only find runs and wait: a prompt of 4,096 tokens with 16
+// query heads and one KV head 11.8 us for 37 MB (7.2 at a copy's rate).
 #include <algorithm>
 
 #include "turn.h"
