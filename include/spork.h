@@ -572,7 +572,8 @@ typedef struct spork_rope_scaling {
 
 /* Frequencies into inv_freq (host, rotary_dim / 2 doubles) and the magnitude
  * (host) of a spork_rope; the caller copies the frequencies to the device.
- * rotary_dim > 0 and even (BASE: above 2), base > 1; scaling NULL: none. */
+ * rotary_dim > 0 and even (BASE: above 2), base > 1; scaling NULL: none. A factor
+ * under which a frequency is not finite is refused (SPORK_E_INVAL). */
 int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_scaling* scaling,
                            double* inv_freq, double* magnitude);
 

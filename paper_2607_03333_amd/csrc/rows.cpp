@@ -156,7 +156,7 @@ int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_sca
       low = std::max(std::floor(pair(scaling->fast)), 0.0);
       high = std::min(std::ceil(pair(scaling->slow)), r - 1);
     }
-    for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+    const auto frequency = [&](int32_t i) {
       double f = std::pow(b, -2 * static_cast<double>(i) / r);
       double stretched = 0;  // how much of it is
       if (kind == SPORK_ROPE_SCALE_LINEAR) stretched = 1;
@@ -166,8 +166,11 @@ int spork_rope_frequencies(int32_t rotary_dim, double base, const spork_rope_sca
         stretched = 1 - std::min(std::max((turns - scaling->slow) / (scaling->fast - scaling->slow), 0.0), 1.0);
       }
       if (stretched > 0) f = f * (1 - stretched) + f / factor * stretched;
-      inv_freq[i] = f;
-    }
+      return f;
+    };
+    for (int32_t i = 0; i < rotary_dim / 2; ++i)
+      if (!std::isfinite(frequency(i))) return fail(SPORK_E_INVAL, "factor is so small that frequencies are not finite");
+    for (int32_t i = 0; i < rotary_dim / 2; ++i) inv_freq[i] = frequency(i);
     *magnitude = kind == SPORK_ROPE_SCALE_PARTS && factor > 1 ? 0.1 * std::log(factor) + 1 : 1.0;
     return SPORK_OK;
   });
